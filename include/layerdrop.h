@@ -398,6 +398,82 @@ int ld_attn_decode(int32_t n_seq, int32_t n_heads, int32_t d_head, int32_t alibi
                    const void* qkv, const void* kv, int32_t s_max, void* o, void* ws, size_t ws_bytes,
                    void* stream);
 
+/* ---------------------------------------------- 8-bit key/value cache
+ * Keys and values in 8 bits with a scale for each block of positions of one
+ * head's keys or values: half the bytes of the bf16 cache, and decode
+ * attention takes the time of its bytes.  n_kv_heads may divide n_heads: query
+ * head h reads key/value head h / (n_heads / n_kv_heads).
+ *   format: LD_KV8_E4M3, 8-bit floats (1 sign, 4 exponent, 3 mantissa bits,
+ *           no infinities; largest Q = 448), or LD_KV8_INT8, integers
+ *           -127..127 (Q = 127).
+ *   block:  positions that share a scale: 16, 32, 64 or 128.
+ *   d_head: 64 or 128.  s_max >= 1 positions.  n_seq, 2 n_kv_heads <= 65535.
+ *   codes:  device, ld_kv8_code_bytes, 16-byte aligned.  With S16 = s_max
+ *           rounded up to 16, sequence b's head h has at
+ *           ((b n_kv_heads + h) 2) S16 d_head its keys [S16][d_head], then its
+ *           values [S16 / 16][d_head][16] (position 16 t + i at [t][.][i]).
+ *   scales: device float32 [n_seq][n_kv_heads][2][ceil(s_max / block)]
+ *           (ld_kv8_scale_bytes), keys' then values'.
+ * A value is its code times its block's scale.  A scale is a power of two, so
+ * both the division before rounding and this product are exact (in bf16 too).
+ * The scale a set of rows needs is the smallest 2^e, e >= -100, with
+ * max|x| <= Q 2^e, or NaN if an element is not finite: such a block reads as
+ * NaN as a whole, so that overflow upstream stays visible.
+ * The memory need not be initialised: a block's scale is set when its first
+ * position is written, and nothing is read behind the last one. */
+typedef enum { LD_KV8_E4M3 = 0, LD_KV8_INT8 = 1 } ld_kv8_format;
+
+typedef struct {
+  int32_t format, block, n_seq, n_kv_heads, d_head, s_max;
+  void* codes;
+  float* scales;
+} ld_kv8;
+
+/* Bytes of codes and of scales (the pointers are not used; 0 on an invalid
+ * descriptor). */
+size_t ld_kv8_code_bytes(const ld_kv8* kv);
+size_t ld_kv8_scale_bytes(const ld_kv8* kv);
+
+/* Quantises the keys and values of qkv rows (device bf16 [n_seq * n_new,
+ * (n_heads + 2 n_kv_heads) d_head], 16-byte aligned, row b n_new + j: queries,
+ * keys, values) into the cache at position pos + j of sequence b.
+ *   seq_pos: NULL, or device int32[n_seq]: sequence b's rows go to positions
+ *   seq_pos[b] + j instead; pos must then be their largest value (a bound that
+ *   sizes the launch).  A sequence whose seq_pos is outside [0, pos] is left
+ *   out: nothing of it is read or written.
+ * A block whose first position the call writes takes the scale its new rows
+ * need; one that holds earlier positions the larger of that and its old scale,
+ * and where that grows, the earlier positions' codes are rounded again to it.
+ * A new code is x / scale rounded to nearest, ties to even.  Earlier positions
+ * of the first block must have been written (or be zeros, scale and codes);
+ * later positions of the last block are no longer valid.  n_new >= 1,
+ * pos + n_new <= s_max. */
+int ld_kv8_store(const ld_kv8* kv, int32_t n_heads, int32_t n_new, int32_t pos, const int32_t* seq_pos,
+                 const void* qkv, void* stream);
+
+/* Positions pos .. pos + n - 1 of every sequence back to bf16, exactly (a value
+ * whose 8 bits stand for 2^128, as the largest bf16's do, is infinite):
+ *   out: device bf16 [n_seq, n, 2 n_kv_heads d_head], 16-byte aligned, keys
+ *   (head h at h d_head), then values, as in the bf16 cache; with pos = 0 and
+ *   n = s_max it is one.
+ *   seq_len: NULL, or device int32[n_seq]: rows of positions at or behind
+ *   seq_len[b] are not written.
+ * n >= 1, pos + n <= s_max. */
+int ld_kv8_load(const ld_kv8* kv, int32_t pos, int32_t n, const int32_t* seq_len, void* out, void* stream);
+
+/* ld_attn_decode over an 8-bit cache: the queries of qkv rows b n_new + j
+ * (layout and seq_pos as in ld_kv8_store) at position pos + j over positions
+ * 0 .. pos + j of the cache, which must already hold the new rows.  Causal,
+ * with the ALiBi bias of n_heads heads when alibi = 1.  Scores, softmax and
+ * sums in float32; a probability times its value scale is held to 2^-16.
+ *   o: device bf16 [n_seq * n_new, n_heads d_head]; rows of sequences left
+ *   out are zeros.  1 <= n_new <= 8.
+ *   ws: device scratch of ld_attn_decode_kv8_ws_bytes(kv, n_heads, n_new)
+ *   bytes (enough for every pos; 0 on invalid arguments), 16-byte aligned. */
+size_t ld_attn_decode_kv8_ws_bytes(const ld_kv8* kv, int32_t n_heads, int32_t n_new);
+int ld_attn_decode_kv8(const ld_kv8* kv, int32_t n_heads, int32_t alibi, int32_t pos, const int32_t* seq_pos,
+                       int32_t n_new, const void* qkv, void* o, void* ws, size_t ws_bytes, void* stream);
+
 /* Causal multi-head attention over n_seq independent sequences.
  *   qkv: device [n_seq*S, 3*H*dh] as produced by x W_qkv^T;
  *   o:   device [n_seq*S, H*dh]; o[s, h] = softmax_j<=s(q_s.k_j / sqrt(dh)

@@ -25,6 +25,7 @@ Modules
   rows      bit-level definitions of the isolated gather and scatter-add.
   infer     evaluation form over a static active-layer set (early exit,
             layer skipping) and KV-cached incremental decoding.
+  kv8       the 8-bit key/value cache and attention over it.
 
 Parity status: every function here is pinned by a CPU test against
 something other than itself (numpy's own Philox, closed forms printed in the
@@ -32,4 +33,4 @@ paper, torch float64 autograd of the dense block, finite differences,
 special cases p=0 and p=1).  No function is "parity unpinned".
 """
 
-from . import philox, schedule, masks, block, stack, rows, infer  # noqa: F401
+from . import philox, schedule, masks, block, stack, rows, infer, kv8  # noqa: F401

@@ -16,6 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblayerdrop.so")
 
 LD_F32, LD_BF16 = 0, 1
+LD_KV8_E4M3, LD_KV8_INT8 = 0, 1
 LD_GRAN_LAYER_SEQ, LD_GRAN_SUBLAYER_SEQ, LD_GRAN_LAYER_BATCH, LD_GRAN_SUBLAYER_BATCH = 0, 1, 2, 3
 UNIFORM, ILD, ALD = 0, 1, 2
 CONSTANT, ITS, DTS = 0, 1, 2
@@ -36,6 +37,11 @@ class ld_config(C.Structure):
                 ("block_kind", C.c_int32), ("granularity", C.c_int32)]
 
 
+class ld_kv8(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("format", "block", "n_seq", "n_kv_heads", "d_head", "s_max")] + \
+               [("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
 class ld_weights(C.Structure):
     _fields_ = [(k, C.c_void_p) for k in WEIGHT_KEYS]
 
@@ -50,6 +56,7 @@ _lib = C.CDLL(LIB_PATH)
 
 _vp, _i32, _i64, _u64, _f32, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_float, C.c_size_t
 _PCFG = C.POINTER(ld_config)
+_PKV8 = C.POINTER(ld_kv8)
 _SIGS = {
     "ld_status_string": (C.c_char_p, [C.c_int]),
     "ld_last_error": (C.c_char_p, []),
@@ -101,6 +108,12 @@ _SIGS = {
     "ld_attn_decode_ws_bytes": (_sz, [_i32, _i32, _i32, _i32]),
     "ld_attn_decode": (C.c_int, [_i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _sz,
                                  _vp]),
+    "ld_kv8_code_bytes": (_sz, [_PKV8]),
+    "ld_kv8_scale_bytes": (_sz, [_PKV8]),
+    "ld_kv8_store": (C.c_int, [_PKV8, _i32, _i32, _i32, _vp, _vp, _vp]),
+    "ld_kv8_load": (C.c_int, [_PKV8, _i32, _i32, _vp, _vp, _vp]),
+    "ld_attn_decode_kv8_ws_bytes": (_sz, [_PKV8, _i32, _i32]),
+    "ld_attn_decode_kv8": (C.c_int, [_PKV8, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
     "ld_prof_start": (C.c_int, [C.c_char_p]),
     "ld_prof_stop": (C.c_int, []),
     "ld_prof_result": (C.c_int, [C.POINTER(_i64), C.POINTER(C.c_double), C.POINTER(C.c_double),
@@ -403,6 +416,73 @@ def ld_attn_decode_ws_bytes(n_seq, n_heads, d_head, s_max):
 def ld_attn_decode(n_seq, n_heads, d_head, pos, n_new, qkv, kv, s_max, o, ws, alibi=0, stream=None):
     _check(_lib.ld_attn_decode(n_seq, n_heads, d_head, alibi, pos, n_new, _ptr(qkv), _ptr(kv), s_max,
                                _ptr(o), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def kv8(codes, scales, format, block, n_seq, n_kv_heads, d_head, s_max):
+    """ld_kv8 over device tensors: codes (uint8) and scales (float32), of
+    ld_kv8_code_bytes and ld_kv8_scale_bytes bytes; None for a descriptor that
+    only those two are asked about.  It keeps the tensors."""
+    kv = ld_kv8(format, block, n_seq, n_kv_heads, d_head, s_max)
+    if codes is not None or scales is not None:
+        n, m = ld_kv8_code_bytes(kv), ld_kv8_scale_bytes(kv)
+        if n:   # an invalid descriptor is refused by the call that takes it
+            _need(codes, "codes", torch.uint8, n)
+            _need(scales, "scales", torch.float32, m // 4)
+        kv.codes, kv.scales = _ptr(codes, "codes"), _ptr(scales, "scales")
+        kv.tensors = (codes, scales)
+    return kv
+
+
+def ld_kv8_code_bytes(kv):
+    return _lib.ld_kv8_code_bytes(C.byref(kv))
+
+
+def ld_kv8_scale_bytes(kv):
+    return _lib.ld_kv8_scale_bytes(C.byref(kv))
+
+
+def _kv8_here(kv, *named):
+    """The tensors of a call live on the current device, as its stream does."""
+    for name, t in (*zip(("codes", "scales"), getattr(kv, "tensors", ())), *named):
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name}: on {t.device}, which is not the current device")
+
+
+def _kv8_rows(kv, n_heads, n_new, qkv, seq_pos):
+    _need(qkv, "qkv", torch.bfloat16, kv.n_seq * n_new * (n_heads + 2 * kv.n_kv_heads) * kv.d_head)
+    _need(seq_pos, "seq_pos", torch.int32, kv.n_seq)
+
+
+def ld_kv8_store(kv, n_heads, n_new, pos, qkv, seq_pos=None, stream=None):
+    """Quantise the keys and values of qkv rows into the cache at positions
+    pos (or seq_pos[b] <= pos) onwards."""
+    _kv8_rows(kv, n_heads, n_new, qkv, seq_pos)
+    _kv8_here(kv, ("qkv", qkv), ("seq_pos", seq_pos))
+    _check(_lib.ld_kv8_store(C.byref(kv), n_heads, n_new, pos, _ptr(seq_pos, "seq_pos"), _ptr(qkv, "qkv"),
+                             _stream(stream)))
+
+
+def ld_kv8_load(kv, pos, n, out, seq_len=None, stream=None):
+    """Positions pos .. pos + n - 1 back to bfloat16 rows [n_seq, n, 2 n_kv_heads d_head]."""
+    _need(out, "out", torch.bfloat16, kv.n_seq * n * 2 * kv.n_kv_heads * kv.d_head)
+    _need(seq_len, "seq_len", torch.int32, kv.n_seq)
+    _kv8_here(kv, ("out", out), ("seq_len", seq_len))
+    _check(_lib.ld_kv8_load(C.byref(kv), pos, n, _ptr(seq_len, "seq_len"), _ptr(out, "out"), _stream(stream)))
+
+
+def ld_attn_decode_kv8_ws_bytes(kv, n_heads, n_new):
+    return _lib.ld_attn_decode_kv8_ws_bytes(C.byref(kv), n_heads, n_new)
+
+
+def ld_attn_decode_kv8(kv, n_heads, pos, n_new, qkv, o, ws, seq_pos=None, alibi=0, stream=None):
+    """Attention of n_new rows per sequence at positions pos (or seq_pos[b])
+    onwards over the cache, which already holds them."""
+    _kv8_rows(kv, n_heads, n_new, qkv, seq_pos)
+    _need(o, "o", torch.bfloat16, kv.n_seq * n_new * n_heads * kv.d_head)
+    _kv8_here(kv, ("qkv", qkv), ("o", o), ("ws", ws), ("seq_pos", seq_pos))
+    _check(_lib.ld_attn_decode_kv8(C.byref(kv), n_heads, int(alibi), pos, _ptr(seq_pos, "seq_pos"), n_new,
+                                   _ptr(qkv, "qkv"), _ptr(o, "o"), _ptr(ws, "ws"), ws.numel() * ws.element_size(),
+                                   _stream(stream)))
 
 
 def ld_rmsnorm_fwd(x, g, y, rstd, eps=1e-5, stream=None):

@@ -19,7 +19,7 @@ LIB = os.path.join(HERE, "liblayerdrop.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
-SOURCES = ["k_rows.hip", "k_gemm.hip", "k_attn.hip", "k_decode.hip", "api.cpp"]
+SOURCES = ["k_rows.hip", "k_gemm.hip", "k_attn.hip", "k_decode.hip", "k_kv8.hip", "api.cpp"]
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
     # packed fp32 instructions are kept out of every kernel
@@ -40,7 +40,7 @@ def _compile(src):
 
 def build(verbose=False):
     os.makedirs(BUILD, exist_ok=True)
-    with cf.ThreadPoolExecutor(max_workers=min(4, len(SOURCES))) as ex:
+    with cf.ThreadPoolExecutor(max_workers=min(6, len(SOURCES))) as ex:
         objs = list(ex.map(_compile, SOURCES))
     tmp = LIB + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp]

@@ -1216,6 +1216,8 @@ bool dec_split_k(int64_t M, int64_t d) {
   return M <= kSkinnyMaxM && (!dec_gemm_fuses_norm(M, d) || (M > 32 && d <= 1024));
 }
 
+constexpr int32_t kMaxGridYZ = 65535;  // of HIP launches
+
 int64_t dec_chunks(int64_t keys) { return (keys + kDecKeys - 1) / kDecKeys; }
 
 DecLayout dec_layout(const Dims& D, int64_t n_new, int64_t s_max) {
@@ -1251,6 +1253,64 @@ struct KvOut {
   void* kv;
   int32_t d, n, s_max, pos;
 };
+
+// An 8-bit cache's descriptor, without its pointers.
+int check_kv8(const ld_kv8* kv, Kv8View* out) {
+  if (!kv) return fail(LD_E_INVALID, "NULL kv");
+  if (kv->format != LD_KV8_E4M3 && kv->format != LD_KV8_INT8) return fail(LD_E_INVALID, "unknown kv8 format");
+  if (kv->block != 16 && kv->block != 32 && kv->block != 64 && kv->block != 128)
+    return fail(LD_E_UNSUPPORTED, "kv8 block must be 16, 32, 64 or 128");
+  if (kv->d_head != 64 && kv->d_head != 128) return fail(LD_E_UNSUPPORTED, "d_head must be 64 or 128");
+  if (kv->n_seq < 1 || kv->n_kv_heads < 1 || kv->s_max < 1) return fail(LD_E_SHAPE, "n_seq, n_kv_heads, s_max must be >= 1");
+  if (kv->n_seq > kMaxGridYZ || kv->n_kv_heads > kMaxGridYZ / 2)
+    return fail(LD_E_SHAPE, "n_seq or 2 n_kv_heads above %d", kMaxGridYZ);
+  if (kv->s_max > INT32_MAX - 512) return fail(LD_E_SHAPE, "s_max too large");
+  Kv8View v{};
+  v.codes = static_cast<uint8_t*>(kv->codes);
+  v.scales = kv->scales;
+  v.format = kv->format;
+  v.block = kv->block;
+  v.shift = kv->block == 16 ? 4 : kv->block == 32 ? 5 : kv->block == 64 ? 6 : 7;
+  v.n_seq = kv->n_seq;
+  v.KV = kv->n_kv_heads;
+  v.dh = kv->d_head;
+  v.s16 = (kv->s_max + 15) / 16 * 16;
+  v.nb = (kv->s_max + kv->block - 1) / kv->block;
+  *out = v;
+  return LD_OK;
+}
+
+int check_kv8_buffers(const ld_kv8* kv, Kv8View* out) {
+  if (int rc = check_kv8(kv, out)) return rc;
+  if (!kv->codes || !kv->scales) return fail(LD_E_INVALID, "NULL codes or scales");
+  if (reinterpret_cast<uintptr_t>(kv->codes) & 15) return fail(LD_E_INVALID, "codes must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(kv->scales) & 3) return fail(LD_E_INVALID, "scales must be 4-byte aligned");
+  return LD_OK;
+}
+
+int check_kv8_heads(const ld_kv8* kv, int32_t n_heads) {
+  if (n_heads < 1 || n_heads % kv->n_kv_heads) return fail(LD_E_SHAPE, "n_heads must be a multiple of n_kv_heads");
+  if (n_heads > kMaxGridYZ) return fail(LD_E_SHAPE, "n_heads above %d", kMaxGridYZ);
+  return LD_OK;
+}
+
+// The new rows of a call and where they stand.
+int check_kv8_rows(const ld_kv8* kv, int32_t n_heads, int32_t n_new, int32_t pos, const void* qkv,
+                   const int32_t* seq_pos) {
+  if (int rc = check_kv8_heads(kv, n_heads)) return rc;
+  if (n_new < 1) return fail(LD_E_SHAPE, "n_new must be >= 1");
+  if (pos < 0 || static_cast<int64_t>(pos) + n_new > kv->s_max) return fail(LD_E_SHAPE, "positions outside the cache");
+  if (!qkv) return fail(LD_E_INVALID, "NULL pointer");
+  if (reinterpret_cast<uintptr_t>(qkv) & 15) return fail(LD_E_INVALID, "qkv must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(seq_pos) & 3) return fail(LD_E_INVALID, "seq_pos must be 4-byte aligned");
+  return LD_OK;
+}
+
+// Partial rows of ld_attn_decode_kv8 over any number of keys up to s_max.
+size_t kv8_part_rows(const Kv8View& v, int64_t n_heads, int64_t n_new) {
+  const int64_t tiles = (n_heads / v.KV * n_new + 15) / 16;
+  return static_cast<size_t>(v.n_seq) * n_heads * n_new * attn_kv8_max_chunks(v.n_seq * v.KV * tiles, v.s16);
+}
 
 // C[M, N] = (R ? R : 0) + alpha * A W^T on the general GEMM kernels, for
 // decoding steps of more than kSkinnyMaxM rows.
@@ -2044,6 +2104,88 @@ int ld_attn_decode(int32_t n_seq, int32_t n_heads, int32_t d_head, int32_t alibi
   at.alibi = alibi;
   hipError_t e = launch_attn_decode(at, as_stream(stream));
   if (e != hipSuccess) return fail(LD_E_HIP, "attn decode: %s", hipGetErrorString(e));
+  return LD_OK;
+}
+
+size_t ld_kv8_code_bytes(const ld_kv8* kv) {
+  Kv8View v;
+  if (check_kv8(kv, &v)) return 0;
+  return static_cast<size_t>(v.n_seq) * v.KV * 2 * v.s16 * v.dh;
+}
+
+size_t ld_kv8_scale_bytes(const ld_kv8* kv) {
+  Kv8View v;
+  if (check_kv8(kv, &v)) return 0;
+  return static_cast<size_t>(v.n_seq) * v.KV * 2 * v.nb * 4;
+}
+
+int ld_kv8_store(const ld_kv8* kv, int32_t n_heads, int32_t n_new, int32_t pos, const int32_t* seq_pos,
+                 const void* qkv, void* stream) {
+  t_err.clear();
+  Kv8StoreArgs a{};
+  if (int rc = check_kv8_buffers(kv, &a.kv)) return rc;
+  if (int rc = check_kv8_rows(kv, n_heads, n_new, pos, qkv, seq_pos)) return rc;
+  a.qkv = qkv;
+  a.ld_qkv = (static_cast<int64_t>(n_heads) + 2ll * kv->n_kv_heads) * kv->d_head;
+  a.H = n_heads;
+  a.n = n_new;
+  a.pos = pos;
+  a.seq_pos = seq_pos;
+  hipError_t e = launch_kv8_store(a, as_stream(stream));
+  if (e != hipSuccess) return fail(LD_E_HIP, "kv8 store: %s", hipGetErrorString(e));
+  return LD_OK;
+}
+
+int ld_kv8_load(const ld_kv8* kv, int32_t pos, int32_t n, const int32_t* seq_len, void* out, void* stream) {
+  t_err.clear();
+  Kv8LoadArgs a{};
+  if (int rc = check_kv8_buffers(kv, &a.kv)) return rc;
+  if (n < 1) return fail(LD_E_SHAPE, "n must be >= 1");
+  if (pos < 0 || static_cast<int64_t>(pos) + n > kv->s_max) return fail(LD_E_SHAPE, "positions outside the cache");
+  if (!out) return fail(LD_E_INVALID, "NULL pointer");
+  if (reinterpret_cast<uintptr_t>(out) & 15) return fail(LD_E_INVALID, "out must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(seq_len) & 3) return fail(LD_E_INVALID, "seq_len must be 4-byte aligned");
+  a.out = out;
+  a.pos = pos;
+  a.n = n;
+  a.seq_len = seq_len;
+  hipError_t e = launch_kv8_load(a, as_stream(stream));
+  if (e != hipSuccess) return fail(LD_E_HIP, "kv8 load: %s", hipGetErrorString(e));
+  return LD_OK;
+}
+
+size_t ld_attn_decode_kv8_ws_bytes(const ld_kv8* kv, int32_t n_heads, int32_t n_new) {
+  Kv8View v;
+  if (check_kv8(kv, &v) || check_kv8_heads(kv, n_heads) || n_new < 1 || n_new > kDecMaxRows) return 0;
+  const size_t rows = kv8_part_rows(v, n_heads, n_new);
+  return up(4 * rows * v.dh) + up(4 * rows * 2);
+}
+
+int ld_attn_decode_kv8(const ld_kv8* kv, int32_t n_heads, int32_t alibi, int32_t pos, const int32_t* seq_pos,
+                       int32_t n_new, const void* qkv, void* o, void* ws, size_t ws_bytes, void* stream) {
+  t_err.clear();
+  Kv8AttnArgs a{};
+  if (int rc = check_kv8_buffers(kv, &a.kv)) return rc;
+  if (n_new < 1 || n_new > kDecMaxRows) return fail(LD_E_INVALID, "n_new outside [1, %d]", kDecMaxRows);
+  if (alibi != 0 && alibi != 1) return fail(LD_E_INVALID, "alibi must be 0 or 1");
+  if (int rc = check_kv8_rows(kv, n_heads, n_new, pos, qkv, seq_pos)) return rc;
+  if (!o || !ws) return fail(LD_E_INVALID, "NULL pointer");
+  if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(LD_E_INVALID, "ws must be 16-byte aligned");
+  const size_t need = ld_attn_decode_kv8_ws_bytes(kv, n_heads, n_new);
+  if (ws_bytes < need) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+  a.qkv = qkv;
+  a.ld_qkv = (static_cast<int64_t>(n_heads) + 2ll * kv->n_kv_heads) * kv->d_head;
+  a.out = o;
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + up(4 * kv8_part_rows(a.kv, n_heads, n_new) * a.kv.dh));
+  a.H = n_heads;
+  a.n_new = n_new;
+  a.pos = pos;
+  a.seq_pos = seq_pos;
+  a.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(kv->d_head)));
+  a.alibi = alibi;
+  hipError_t e = launch_attn_decode_kv8(a, as_stream(stream));
+  if (e != hipSuccess) return fail(LD_E_HIP, "attn decode kv8: %s", hipGetErrorString(e));
   return LD_OK;
 }
 
