@@ -40,6 +40,8 @@ class ld_config(C.Structure):
 class ld_kv8(C.Structure):
     _fields_ = [(k, C.c_int32) for k in ("format", "block", "n_seq", "n_kv_heads", "d_head", "s_max")] + \
                [("codes", C.c_void_p), ("scales", C.c_void_p)]
+    device = None     # the tensors' GPU, where kv8() was given tensors
+    tensors = ()
 
 
 class ld_weights(C.Structure):
@@ -199,8 +201,17 @@ def _check_layer_tensors(cfg, w=None, dw=None, acts=()):
         _need(t, name, dt, cfg.batch * cfg.seq * cfg.d_model)
 
 
-def _stream(stream):
+# torch.cuda.current_stream() builds a Stream object, 2.8 us of a call's 9; its
+# handle alone takes 0.1
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(stream, device=None):
+    """The hipStream_t of a stream argument: None is the current one (of the
+    current device, whose index the caller may give)."""
     if stream is None:
+        if device is not None and _current_raw_stream is not None:
+            return _current_raw_stream(device)
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -429,6 +440,10 @@ def kv8(codes, scales, format, block, n_seq, n_kv_heads, d_head, s_max):
             _need(codes, "codes", torch.uint8, n)
             _need(scales, "scales", torch.float32, m // 4)
         kv.codes, kv.scales = _ptr(codes, "codes"), _ptr(scales, "scales")
+        if isinstance(codes, torch.Tensor) and isinstance(scales, torch.Tensor):
+            if codes.device != scales.device:
+                raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
+            kv.device = codes.device.index
         kv.tensors = (codes, scales)
     return kv
 
@@ -441,33 +456,44 @@ def ld_kv8_scale_bytes(kv):
     return _lib.ld_kv8_scale_bytes(C.byref(kv))
 
 
-def _kv8_here(kv, *named):
-    """The tensors of a call live on the current device, as its stream does."""
-    for name, t in (*zip(("codes", "scales"), getattr(kv, "tensors", ())), *named):
-        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+def _kv8_device(kv):
+    """The current device, on which the cache and the stream have to be; None
+    for a cache given by addresses."""
+    if kv.device is not None and kv.device != torch.cuda.current_device():
+        raise ValueError(f"codes: on cuda:{kv.device}, which is not the current device")
+    return kv.device
+
+
+def _kv8_ptr(t, name, device, dtype=None, numel=None):
+    """_need and _ptr of an argument on `device`."""
+    if isinstance(t, torch.Tensor):
+        if dtype is not None and (t.dtype != dtype or t.numel() != numel):
+            _need(t, name, dtype, numel)
+        if t.is_cuda and t.device.index != (torch.cuda.current_device() if device is None else device):
             raise ValueError(f"{name}: on {t.device}, which is not the current device")
+    return _ptr(t, name)
 
 
-def _kv8_rows(kv, n_heads, n_new, qkv, seq_pos):
-    _need(qkv, "qkv", torch.bfloat16, kv.n_seq * n_new * (n_heads + 2 * kv.n_kv_heads) * kv.d_head)
-    _need(seq_pos, "seq_pos", torch.int32, kv.n_seq)
+def _kv8_rows(kv, n_heads, n_new, qkv, device):
+    return _kv8_ptr(qkv, "qkv", device, torch.bfloat16,
+                    kv.n_seq * n_new * (n_heads + 2 * kv.n_kv_heads) * kv.d_head)
 
 
 def ld_kv8_store(kv, n_heads, n_new, pos, qkv, seq_pos=None, stream=None):
     """Quantise the keys and values of qkv rows into the cache at positions
     pos (or seq_pos[b] <= pos) onwards."""
-    _kv8_rows(kv, n_heads, n_new, qkv, seq_pos)
-    _kv8_here(kv, ("qkv", qkv), ("seq_pos", seq_pos))
-    _check(_lib.ld_kv8_store(C.byref(kv), n_heads, n_new, pos, _ptr(seq_pos, "seq_pos"), _ptr(qkv, "qkv"),
-                             _stream(stream)))
+    dev = _kv8_device(kv)
+    _check(_lib.ld_kv8_store(C.byref(kv), n_heads, n_new, pos,
+                             _kv8_ptr(seq_pos, "seq_pos", dev, torch.int32, kv.n_seq),
+                             _kv8_rows(kv, n_heads, n_new, qkv, dev), _stream(stream, dev)))
 
 
 def ld_kv8_load(kv, pos, n, out, seq_len=None, stream=None):
     """Positions pos .. pos + n - 1 back to bfloat16 rows [n_seq, n, 2 n_kv_heads d_head]."""
-    _need(out, "out", torch.bfloat16, kv.n_seq * n * 2 * kv.n_kv_heads * kv.d_head)
-    _need(seq_len, "seq_len", torch.int32, kv.n_seq)
-    _kv8_here(kv, ("out", out), ("seq_len", seq_len))
-    _check(_lib.ld_kv8_load(C.byref(kv), pos, n, _ptr(seq_len, "seq_len"), _ptr(out, "out"), _stream(stream)))
+    dev = _kv8_device(kv)
+    _check(_lib.ld_kv8_load(C.byref(kv), pos, n, _kv8_ptr(seq_len, "seq_len", dev, torch.int32, kv.n_seq),
+                            _kv8_ptr(out, "out", dev, torch.bfloat16, kv.n_seq * n * 2 * kv.n_kv_heads * kv.d_head),
+                            _stream(stream, dev)))
 
 
 def ld_attn_decode_kv8_ws_bytes(kv, n_heads, n_new):
@@ -477,12 +503,12 @@ def ld_attn_decode_kv8_ws_bytes(kv, n_heads, n_new):
 def ld_attn_decode_kv8(kv, n_heads, pos, n_new, qkv, o, ws, seq_pos=None, alibi=0, stream=None):
     """Attention of n_new rows per sequence at positions pos (or seq_pos[b])
     onwards over the cache, which already holds them."""
-    _kv8_rows(kv, n_heads, n_new, qkv, seq_pos)
-    _need(o, "o", torch.bfloat16, kv.n_seq * n_new * n_heads * kv.d_head)
-    _kv8_here(kv, ("qkv", qkv), ("o", o), ("ws", ws), ("seq_pos", seq_pos))
-    _check(_lib.ld_attn_decode_kv8(C.byref(kv), n_heads, int(alibi), pos, _ptr(seq_pos, "seq_pos"), n_new,
-                                   _ptr(qkv, "qkv"), _ptr(o, "o"), _ptr(ws, "ws"), ws.numel() * ws.element_size(),
-                                   _stream(stream)))
+    dev = _kv8_device(kv)
+    _check(_lib.ld_attn_decode_kv8(C.byref(kv), n_heads, int(alibi), pos,
+                                   _kv8_ptr(seq_pos, "seq_pos", dev, torch.int32, kv.n_seq), n_new,
+                                   _kv8_rows(kv, n_heads, n_new, qkv, dev),
+                                   _kv8_ptr(o, "o", dev, torch.bfloat16, kv.n_seq * n_new * n_heads * kv.d_head),
+                                   _kv8_ptr(ws, "ws", dev), ws.numel() * ws.element_size(), _stream(stream, dev)))
 
 
 def ld_rmsnorm_fwd(x, g, y, rstd, eps=1e-5, stream=None):
