@@ -18,6 +18,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kKv8Waves = 8;  // of an attention workgroup
+constexpr int kCus = 256;
 
 // ------------------------------------------------------------- conversions
 
@@ -35,6 +37,8 @@ __device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t a, uint32_t b) {
     r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false);
     r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
   } else {
+    // (opaque, or the loads' registers are split into bytes as they arrive)
+    asm("" : "+v"(a), "+v"(b));
     const uint32_t w[2] = {a, b};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {  // a float of 7 bits is its upper half
@@ -254,29 +258,35 @@ __global__ __launch_bounds__(256) void ld_kv8_load_k(Kv8LoadArgs a) {
 
 // --------------------------------------------------------------- attention
 
-// A workgroup of four waves takes a chunk of keys of one key/value head for 16
-// rows (of its query heads' new rows); a wave 64 keys at a time, with its own
-// running maximum and sum.
+// A workgroup of eight waves takes a chunk of keys of one key/value head for 16
+// rows (of its query heads' new rows); a wave 32 keys at a time, with its own
+// running maximum and sum; they meet once, to add up.
 //
 // Scores S^T = K Q^T and output O^T = V^T P^T on the matrix cores (16x16x32
-// bf16).  The A rows of score product T are the keys 16 g + 4 T + r (row 4 g + r),
-// so lane group g = lane / 16 of the result holds keys 16 g + 4 T + r, T, r < 4, of
-// its query row: 16 neighbouring keys, one tile of the cache's values and one
-// scale.  They are the B operand of O^T as they stand, and 16 bytes of a value
+// bf16).  The A rows of score product t are the keys 8 g + 4 t + r (row 4 g + r),
+// so lane group g = lane / 16 of the result holds keys 8 g + 4 t + r, t < 2, r < 4, of
+// its query row: 8 neighbouring keys, half a tile of the cache's values, of one
+// scale.  They are the B operand of O^T as they stand, and 8 bytes of a value
 // tile's row the A operand.
 //
 // Codes are exact in bf16.  A probability, times its value scale, is split in
 // two bf16 parts, which leave 2^-16 of it.
+//
+// Bound by the cache stream.  A wave asks for its keys and values at once (8 KB)
+// and waits; 16 waves a CU at 128 registers hold 128 KB in flight.
 template <int DH, int FMT, int NQ>
-__global__ __launch_bounds__(256) void ld_attn_decode_kv8_k(Kv8AttnArgs a) {
-  constexpr int NS = DH / 64, MT = DH / 16;
-  __shared__ float ml[4][NQ][2];
-  __shared__ __align__(16) float red[4][NQ][DH];
+__global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8AttnArgs a) {
+  constexpr int NS = DH / 64, MT = DH / 16, NW = kKv8Waves, TT = 2, LK = 4 * TT, WK = 16 * TT;
+  __shared__ float ml[NW][NQ][2];
+  __shared__ __align__(16) float red[NW][NQ][DH];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
   const Kv8View& c = a.kv;
-  const int chunk = blockIdx.x, h = static_cast<int>(blockIdx.y) % c.KV, rt = static_cast<int>(blockIdx.y) / c.KV;
-  const int b = blockIdx.z;
+  const int h = static_cast<int>(blockIdx.y) % c.KV, rt = static_cast<int>(blockIdx.y) / c.KV, b = blockIdx.z;
+  // Workgroups go round the XCDs by their number: turned by the head, or a number
+  // of chunks that shares a factor with the XCDs' would leave those of the last
+  // chunks, which short sequences do not fill, with little to do.
+  const int chunk = static_cast<int>((blockIdx.x + blockIdx.y + blockIdx.z) % gridDim.x);
   const int G = a.H / c.KV, R = G * a.n_new;
   int p = a.pos;
   if (a.seq_pos) {
@@ -288,7 +298,7 @@ __global__ __launch_bounds__(256) void ld_attn_decode_kv8_k(Kv8AttnArgs a) {
   const int64_t d = static_cast<int64_t>(a.H) * DH;
   if (k_first >= nk) {
     if (chunk == 0 && a.n_chunks == 1) {  // left out: its rows are zeros (the combine's else)
-      for (int e = tid; e < rows * DH; e += 256) {
+      for (int e = tid; e < rows * DH; e += 64 * NW) {
         const int r = rt * 16 + e / DH;
         static_cast<bf16*>(a.out)[(static_cast<int64_t>(b) * a.n_new + r % a.n_new) * d +
                                   (h * G + r / a.n_new) * static_cast<int64_t>(DH) + e % DH] = static_cast<bf16>(0.f);
@@ -303,50 +313,68 @@ __global__ __launch_bounds__(256) void ld_attn_decode_kv8_k(Kv8AttnArgs a) {
   const float* ks = c.scales + head * 2 * c.nb;
   const float* vs = ks + c.nb;
 
+  // Keys k0 .. k0 + WK - 1 (past the last key: key 0, masked later): row n of
+  // product t, dimensions 64 s + 16 g + 0..15.
+  const int krow = LK * (n >> 2) + (n & 3);
+  typedef uint32_t VRaw __attribute__((ext_vector_type(TT)));
+  u32x4 kr[TT][NS];
+  VRaw vr[MT];
+  float sk = 0.f, sv = 0.f;
+  auto load_keys = [&](int k0) {
+    if (k0 + WK <= nk) {
+      const uint8_t* at = kc + static_cast<int64_t>(k0 + krow) * DH + 16 * g;
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) kr[t][s] = *reinterpret_cast<const u32x4*>(at + 4 * t * DH + 64 * s);
+    } else {
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        const int kk = k0 + krow + 4 * t;
+        const uint8_t* at = kc + static_cast<int64_t>(kk < nk ? kk : 0) * DH + 16 * g;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) kr[t][s] = *reinterpret_cast<const u32x4*>(at + 64 * s);
+      }
+    }
+    const int f = k0 + LK * g;
+    sk = ks[(f < nk ? f : 0) >> c.shift];
+  };
+  auto load_values = [&](int k0) {
+    const int f = k0 + LK * g, fc = f < nk ? f : 0;
+    const uint8_t* at = vc + static_cast<int64_t>(fc & ~15) * DH + n * 16 + (fc & 15);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) vr[i] = *reinterpret_cast<const VRaw*>(at + 256 * i);
+    sv = vs[fc >> c.shift];
+  };
+
+  int k0 = k_first + wave * WK;
   const int row = rt * 16 + min(n, rows - 1), qh = h * G + row / a.n_new, j = row % a.n_new, qpos = p + j;
-  const float al2 = a.alibi ? alibi_slope(qh, a.H) * kLog2e : 0.f, sl2 = a.scale * kLog2e;
-  const bf16* q = static_cast<const bf16*>(a.qkv) + (static_cast<int64_t>(b) * a.n_new + j) * a.ld_qkv +
-                  static_cast<int64_t>(qh) * DH;
   bf16x8 qf[NS][2];
+  {
+    const bf16* q = static_cast<const bf16*>(a.qkv) + (static_cast<int64_t>(b) * a.n_new + j) * a.ld_qkv +
+                    static_cast<int64_t>(qh) * DH;
 #pragma unroll
-  for (int s = 0; s < NS; ++s)
+    for (int s = 0; s < NS; ++s)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) qf[s][e] = *reinterpret_cast<const bf16x8*>(q + 64 * s + 16 * g + 8 * e);
+      for (int e = 0; e < 2; ++e)
+        qf[s][e] = *reinterpret_cast<const bf16x8*>(q + 64 * s + 16 * g + 8 * e);
+  }
+  const float al2 = a.alibi ? alibi_slope(qh, a.H) * kLog2e : 0.f, sl2 = a.scale * kLog2e;
 
   float m = -INFINITY, l = 0.f;
   floatx4 o[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  for (int k0 = k_first + wave * 64; k0 < k_end; k0 += 256) {
-    u32x4 kr[4][NS], vr[MT];
+  for (; k0 < k_end; k0 += WK * NW) {
+    load_keys(k0);
+    load_values(k0);
+    __builtin_amdgcn_sched_barrier(0);
+    const int f = k0 + LK * g;  // the lane's keys
+    const float ss = sk * sl2;
+    float x[TT][4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int kk = k0 + 16 * (n >> 2) + 4 * t + (n & 3);
-      const uint8_t* at = kc + static_cast<int64_t>(kk < nk ? kk : 0) * DH + 16 * g;
-#pragma unroll
-      for (int s = 0; s < NS; ++s) kr[t][s] = *reinterpret_cast<const u32x4*>(at + 64 * s);
-    }
-    const int f = k0 + 16 * g;  // the lane's 16 keys
-    const int fc = f < nk ? f : 0;
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-      vr[i] = *reinterpret_cast<const u32x4*>(vc + static_cast<int64_t>(fc) * DH + (16 * i + n) * 16);
-    const float sk = ks[fc >> c.shift] * sl2, sv = vs[fc >> c.shift];
-    if (k0 + 64 > nk) {  // codes behind the last key may be anything, NaN too
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int have = nk - f - 4 * w;  // keys of this dword
-        const uint32_t mask = have <= 0 ? 0u : have >= 4 ? ~0u : (1u << (8 * have)) - 1u;
-#pragma unroll
-        for (int i = 0; i < MT; ++i) vr[i][w] &= mask;
-      }
-    }
-
-    float x[4][4];
-    float mn = m;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < TT; ++t) {
       floatx4 s4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
@@ -354,35 +382,77 @@ __global__ __launch_bounds__(256) void ld_attn_decode_kv8_k(Kv8AttnArgs a) {
         s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16<FMT>(kr[t][s][2], kr[t][s][3]), qf[s][1], s4, 0, 0, 0);
       }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int kk = f + 4 * t + r;
-        x[t][r] = kk <= qpos ? s4[r] * sk - al2 * static_cast<float>(qpos - kk) : -INFINITY;
-        mn = fmaxf(mn, x[t][r]);
-      }
+      for (int r = 0; r < 4; ++r) x[t][r] = s4[r] * ss;
+      __builtin_amdgcn_sched_barrier(0);
     }
+    if (a.alibi) {
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[t][r] -= al2 * static_cast<float>(qpos - (f + 4 * t + r));
+    }
+    const bool cut = k0 + WK - 1 > p;  // some of the keys may be behind a row, or behind the last one
+    if (cut) {
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (f + 4 * t + r > qpos) x[t][r] = -INFINITY;
+    }
+    float mn = m;
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mn = fmaxf(mn, x[t][r]);
     mn = fmaxf(mn, __shfl_xor(mn, 16, 64));
     mn = fmaxf(mn, __shfl_xor(mn, 32, 64));
-    const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-    m = mn;
-    l *= keep;
-    bf16x8 ph[2], pl[2];
+    const float mz = mn == -INFINITY ? 0.f : mn;  // of nothing but -inf, whose weights are 0
+    const float keep = __builtin_amdgcn_exp2f(m - mz);
+    if (__any(mn != m)) {
+      l *= keep;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+      for (int i = 0; i < MT; ++i) o[i] *= keep;
+    }
+    m = mn;
+    bf16x8 ph[TT / 2], pl[TT / 2];
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const bool in = x[t][r] != -INFINITY;  // a NaN score stays one
-        const float e = in ? __builtin_amdgcn_exp2f(x[t][r] - m) : 0.f;
+        const float e = __builtin_amdgcn_exp2f(x[t][r] - mz);
         l += e;
-        const float w = in ? e * sv : 0.f;
-        const bf16 whi = static_cast<bf16>(w);
-        ph[t >> 1][4 * (t & 1) + r] = whi;
-        pl[t >> 1][4 * (t & 1) + r] = static_cast<bf16>(w - static_cast<float>(whi));
+        x[t][r] = e * sv;
       }
+    if (cut) {  // nothing of a masked position, whose scale may be NaN
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (f + 4 * t + r > qpos) x[t][r] = 0.f;
+    }
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const bf16 whi = static_cast<bf16>(x[t][r]);
+        ph[t >> 1][4 * (t & 1) + r] = whi;
+        pl[t >> 1][4 * (t & 1) + r] = static_cast<bf16>(x[t][r] - static_cast<float>(whi));
+      }
+    if (k0 + WK > nk) {  // codes behind the last key may be anything, NaN too
+#pragma unroll
+      for (int w = 0; w < TT; ++w) {
+        const int have = nk - f - 4 * w;  // keys of this dword
+        const uint32_t mask = have <= 0 ? 0u : have >= 4 ? ~0u : (1u << (8 * have)) - 1u;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) vr[i][w] &= mask;
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      o[i] *= keep;
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < TT / 2; ++u) {
         const bf16x8 v8 = codes_to_bf16<FMT>(vr[i][2 * u], vr[i][2 * u + 1]);
         o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, ph[u], o[i], 0, 0, 0);
         o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, pl[u], o[i], 0, 0, 0);
@@ -401,15 +471,18 @@ __global__ __launch_bounds__(256) void ld_attn_decode_kv8_k(Kv8AttnArgs a) {
   __syncthreads();
 
   // sum over the waves, in wave order, each scaled to the chunk's maximum
-  for (int e = tid; e < rows * DH; e += 256) {
+  for (int e = tid; e < rows * DH; e += 64 * NW) {
     const int i = e / DH, col = e % DH, r = rt * 16 + i;
-    float M = -INFINITY, L = 0.f, s = 0.f;
+    float mw[NW], M = -INFINITY, L = 0.f, s = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[w][i][0]);
+    for (int w = 0; w < NW; ++w) {
+      mw[w] = ml[w][i][0];
+      M = fmaxf(M, mw[w]);
+    }
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       // (a wave whose every score was NaN has no maximum, but NaN sums: 0 times them is NaN)
-      const float wgt = ml[w][i][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w][i][0] - M);
+      const float wgt = mw[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[w] - M);
       L = __builtin_fmaf(wgt, ml[w][i][1], L);
       s = __builtin_fmaf(wgt, red[w][i][col], s);
     }
@@ -427,14 +500,19 @@ __global__ __launch_bounds__(256) void ld_attn_decode_kv8_k(Kv8AttnArgs a) {
   }
 }
 
-// One wave per (sequence, query head, new row): merge the chunks its keys fill.
-template <int DH>
-__global__ __launch_bounds__(256) void ld_attn_decode_kv8_combine(Kv8AttnArgs a) {
+// W waves per (sequence, query head, new row) merge the chunks its keys fill: each
+// every W-th, 16 at once so that their partial rows are all in flight; then the
+// waves' sums, in their order.
+template <int DH, int W>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void ld_attn_decode_kv8_combine(Kv8AttnArgs a) {
   constexpr int CL = DH / 64, U = 16;
   typedef float FRow __attribute__((ext_vector_type(CL)));
-  const int lane = threadIdx.x & 63;
-  const int64_t r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  __shared__ float ml[W][2];
+  __shared__ __align__(16) FRow red[W][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t r = W == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + wave : blockIdx.x;
   if (r >= static_cast<int64_t>(a.kv.n_seq) * a.H * a.n_new) return;
+  const int w = W == 1 ? 0 : wave;
   const int G = a.H / a.kv.KV, R = G * a.n_new;
   const int64_t head = r / R, b = head / a.kv.KV;
   const int i = static_cast<int>(r % R), h = static_cast<int>(head % a.kv.KV) * G + i / a.n_new, j = i % a.n_new;
@@ -448,16 +526,17 @@ __global__ __launch_bounds__(256) void ld_attn_decode_kv8_combine(Kv8AttnArgs a)
   const float* pm = a.part_ml + r * a.n_chunks * 2;
   float M = -INFINITY, L = 0.f;
   FRow acc = 0.f;
-  for (int c0 = 0; c0 < chunks; c0 += U) {
+  for (int c0 = w; c0 < chunks; c0 += U * W) {
     FRow v[U];
     float mc[U], lc[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {  // past the last chunk: the last again, dropped below
-      const int64_t c = min(c0 + u, chunks - 1);
+      const int64_t c = min(c0 + u * W, chunks - 1);
       v[u] = *reinterpret_cast<const FRow*>(po + c * DH);
       mc[u] = pm[c * 2];
       lc[u] = pm[c * 2 + 1];
     }
+    __builtin_amdgcn_sched_barrier(0);
     float m = M;
 #pragma unroll
     for (int u = 0; u < U; ++u) m = fmaxf(m, mc[u]);
@@ -467,10 +546,30 @@ __global__ __launch_bounds__(256) void ld_attn_decode_kv8_combine(Kv8AttnArgs a)
     M = m;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool in = c0 + u < chunks;
+      const bool in = c0 + u * W < chunks;  // else selected out: 0 times an infinity in v would be NaN
       const float wgt = !in || mc[u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc[u] - m);
       L = __builtin_fmaf(wgt, in ? lc[u] : 0.f, L);
       acc += wgt * (in ? v[u] : FRow(0.f));
+    }
+  }
+  if constexpr (W > 1) {
+    if (lane == 0) {
+      ml[w][0] = M;
+      ml[w][1] = L;
+    }
+    red[w][lane] = acc;
+    __syncthreads();
+    if (w) return;
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < W; ++u) m = fmaxf(m, ml[u][0]);
+    L = 0.f;
+    acc = 0.f;
+#pragma unroll
+    for (int u = 0; u < W; ++u) {
+      const float wgt = ml[u][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[u][0] - m);
+      L = __builtin_fmaf(wgt, ml[u][1], L);
+      acc += wgt * red[u][lane];
     }
   }
   if (chunks > 0) acc *= 1.f / L;
@@ -504,15 +603,20 @@ hipError_t load_t(const Kv8LoadArgs& a, hipStream_t s) {
 template <int DH, int FMT>
 hipError_t attn_t(const Kv8AttnArgs& a, hipStream_t s) {
   const int R = a.H / a.kv.KV * a.n_new;
-  const dim3 grid(a.n_chunks, a.kv.KV * ((R + 15) / 16), a.kv.n_seq);
+  const dim3 grid(a.n_chunks, a.kv.KV * ((R + 15) / 16), a.kv.n_seq), block(64 * kKv8Waves);
   if (R == 1)
-    hipLaunchKernelGGL((ld_attn_decode_kv8_k<DH, FMT, 1>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((ld_attn_decode_kv8_k<DH, FMT, 1>), grid, block, 0, s, a);
+  else if (R <= 8)
+    hipLaunchKernelGGL((ld_attn_decode_kv8_k<DH, FMT, 8>), grid, block, 0, s, a);
   else
-    hipLaunchKernelGGL((ld_attn_decode_kv8_k<DH, FMT, 16>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((ld_attn_decode_kv8_k<DH, FMT, 16>), grid, block, 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_chunks == 1) return e;
   const int64_t rows = static_cast<int64_t>(a.kv.n_seq) * a.H * a.n_new;
-  hipLaunchKernelGGL(ld_attn_decode_kv8_combine<DH>, dim3((rows + 3) / 4), dim3(256), 0, s, a);
+  if (a.n_chunks > 8 && rows <= 8192)
+    hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 8>), dim3(rows), dim3(512), 0, s, a);
+  else
+    hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 1>), dim3((rows + 3) / 4), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -530,22 +634,44 @@ hipError_t launch_kv8_load(const Kv8LoadArgs& a, hipStream_t s) {
   return a.kv.format == LD_KV8_E4M3 ? load_t<64, LD_KV8_E4M3>(a, s) : load_t<64, LD_KV8_INT8>(a, s);
 }
 
-// Chunks of whole 256-key turns of a workgroup, about three workgroups a CU's
-// worth of them.
-int64_t attn_kv8_chunk_keys(int64_t heads, int64_t keys) {
-  const int64_t turns = (keys + 255) / 256, most = (768 + heads - 1) / heads;
-  return (turns + most - 1) / most * 256;
+namespace {
+constexpr int64_t kKv8MinChunk = 512, kKv8RaggedWgs = 16 * kCus;
+}
+
+// Keys of a chunk, for `heads` (sequence, head, 16 rows).  Lengths that the host
+// knows: what costs least, rounds of one workgroup per CU, each its keys and
+// about 128 more, and a second launch like 500.  Otherwise (`ragged`, keys being
+// the longest a sequence can have) about 16 workgroups a CU, so that whatever the
+// lengths are spreads evenly.
+int64_t attn_kv8_chunk(int64_t heads, int64_t keys, bool ragged) {
+  const int64_t most = keys <= 1024 ? 1 : keys / kKv8MinChunk;
+  int64_t best = 1;
+  if (ragged) {
+    best = (kKv8RaggedWgs + heads - 1) / heads;
+    if (best > most) best = most;
+  } else {
+    int64_t best_cost = INT64_MAX;
+    for (int64_t n = 1; n <= most && (n == 1 || heads * (n - 1) < 4 * kCus); ++n) {
+      const int64_t cost = (heads * n + kCus - 1) / kCus * ((keys + n - 1) / n + 128) + (n > 1 ? 500 : 0);
+      if (cost < best_cost) {
+        best = n;
+        best_cost = cost;
+      }
+    }
+  }
+  return ((keys + best - 1) / best + 63) / 64 * 64;
 }
 
 int64_t attn_kv8_max_chunks(int64_t heads, int64_t keys) {
-  const int64_t turns = (keys + 255) / 256, most = (768 + heads - 1) / heads;
-  return turns < most ? turns : most;
+  const int64_t by_keys = (keys + kKv8MinChunk - 1) / kKv8MinChunk, by_wgs = (kKv8RaggedWgs + heads - 1) / heads;
+  return by_keys < by_wgs ? by_keys : by_wgs;
 }
 
 hipError_t launch_attn_decode_kv8(Kv8AttnArgs a, hipStream_t s) {
   const int64_t keys = static_cast<int64_t>(a.pos) + a.n_new;
   const int64_t R = static_cast<int64_t>(a.H / a.kv.KV) * a.n_new;
-  a.chunk_keys = static_cast<int32_t>(attn_kv8_chunk_keys(static_cast<int64_t>(a.kv.n_seq) * a.kv.KV * ((R + 15) / 16), keys));
+  const int64_t heads = static_cast<int64_t>(a.kv.n_seq) * a.kv.KV * ((R + 15) / 16);
+  a.chunk_keys = static_cast<int32_t>(attn_kv8_chunk(heads, keys, a.seq_pos != nullptr));
   a.n_chunks = static_cast<int32_t>((keys + a.chunk_keys - 1) / a.chunk_keys);
   if (a.kv.dh == 128)
     return a.kv.format == LD_KV8_E4M3 ? attn_t<128, LD_KV8_E4M3>(a, s) : attn_t<128, LD_KV8_INT8>(a, s);
