@@ -14,6 +14,7 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -91,168 +92,254 @@ __device__ __forceinline__ float scale_needed(uint32_t amax) {
   return __builtin_bit_cast(float, static_cast<uint32_t>(e + 127) << 23);
 }
 
-// ------------------------------------------------------------------- store
+// Four dwords of four bytes, transposed.
+__device__ __forceinline__ void transpose4(const uint32_t (&in)[4], uint32_t (&out)[4]) {
+  const uint32_t a = __builtin_amdgcn_perm(in[1], in[0], 0x05010400u), b = __builtin_amdgcn_perm(in[1], in[0], 0x07030602u);
+  const uint32_t c = __builtin_amdgcn_perm(in[3], in[2], 0x05010400u), d = __builtin_amdgcn_perm(in[3], in[2], 0x07030602u);
+  out[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+  out[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+  out[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+  out[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
 
-// A workgroup takes a tile of TT positions (whole blocks) of one head's keys
-// or values.  Every thread holds 8 dimensions of TT DH / 2048 rows.
-template <int DH, int FMT, int TT>
-__global__ __launch_bounds__(256) void ld_kv8_store_k(Kv8StoreArgs a) {
-  constexpr int PT = DH / 8, TPP = 256 / PT, NP = TT / TPP, TW = 64 / PT;  // threads a row, rows a pass (a wave's: TW)
-  __shared__ uint32_t amax_s[NP * 4];
-  __shared__ float inv_s[TT / 16], ratio_s;
-  __shared__ __align__(16) uint8_t ct[TT][DH];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int part = blockIdx.y & 1, h = blockIdx.y >> 1, b = blockIdx.z;
+// ---------------------------------------------------------- store and load
+
+// A wave takes a unit of U = 16 positions (32 for heads of 64) of one head's keys or
+// values.  Lane l has dimensions 8 (l % PT) .. + 7, PT = DH / 8 lanes a row, of rows
+// 4 (l / PT) + i, i < 4: four neighbouring positions, so that a 4x4 byte transpose in
+// registers turns between rows and the values' tiles, and a load or store
+// instruction still takes whole rows.  A tile's 16 bytes of a dimension come from
+// four lanes and meet in LDS (rows of 16 bytes, 16 more after each 8: the lanes'
+// dwords fall on different banks).
+//
+// Bound by memory.  Prompts of 8 x 2048 rows, 16 heads of 128: store 36.9 us for 201
+// MB (5.4 TB/s; units of 64 positions a wave, four times fewer waves, 44.9, and
+// loads that stay in the caches 41.2), load 30.2 us (6.7 TB/s, the codes still in the
+// memory-side cache; stores that push them out 39.9).  A new row of 32 sequences:
+// 5.9 us, its value bytes alone (16 lines a head); whole tiles read and written 6.9.
+template <int DH>
+struct Kv8Lanes {
+  static constexpr int PT = DH / 8, U = 4 * 64 / PT, TILES = U / 16;  // a unit: U rows, TILES tiles
+  static constexpr int TILE_LDS = DH * 16 + DH * 2;                   // bytes
+  static __device__ __forceinline__ int lds_row(int d) { return d * 16 + (d >> 3) * 16; }
+};
+
+// Piece number -> (sequence, piece of it, head, part), heads and parts first:
+// neighbours read neighbouring columns of the same rows.
+struct Kv8Unit {
+  int b, piece, h, part;
+};
+__device__ __forceinline__ Kv8Unit kv8_unit(uint32_t id, uint32_t KV, uint32_t pieces) {
+  const uint32_t head = id >> 1, at = head / KV;
+  return Kv8Unit{static_cast<int>(at / pieces), static_cast<int>(at % pieces), static_cast<int>(head % KV),
+                 static_cast<int>(id & 1)};
+}
+
+// A workgroup of W waves takes a piece of W U positions (whole blocks) of one
+// head's keys or values, a wave a unit; the waves of a block exchange their maxima.
+template <int DH, int FMT, int W>
+__global__ __launch_bounds__(64 * W) void ld_kv8_store_k(Kv8StoreArgs a) {
+  using LN = Kv8Lanes<DH>;
+  constexpr int PT = LN::PT, U = LN::U, PP = U * W;
+  __shared__ __align__(16) uint8_t lds[W][LN::TILES * LN::TILE_LDS];
+  __shared__ uint32_t mu_s[W];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Kv8View& c = a.kv;
+  const Kv8Unit w = kv8_unit(blockIdx.x, c.KV, a.pieces);
   int p = a.pos;
   if (a.seq_pos) {
-    p = a.seq_pos[b];
+    p = a.seq_pos[w.b];
     if (p < 0 || p > a.pos) return;
   }
-  const int lo = p, hi = p + a.n;
-  const int t0 = (p / TT + static_cast<int>(blockIdx.x)) * TT;
-  if (t0 >= hi) return;
-  const int tr = tid / PT, d8 = (tid % PT) * 8;
-  const bf16* src = static_cast<const bf16*>(a.qkv) + static_cast<int64_t>(b) * a.n * a.ld_qkv +
-                    (a.H + part * c.KV + h) * static_cast<int64_t>(DH) + d8;
-  const int64_t head = static_cast<int64_t>(b) * c.KV + h;
-  uint8_t* codes = c.codes + (head * 2 + part) * c.s16 * DH;
-  float* scales = c.scales + (head * 2 + part) * c.nb;
+  const int lo = p, hi = p + a.n, p0 = (p / PP + w.piece) * PP;
+  if (p0 >= hi) return;
+  const int f = p0 + U * wave;  // the wave's unit
+  const int grp = lane / PT, d8 = lane % PT * 8;
+  const int64_t head = static_cast<int64_t>(w.b) * c.KV + w.h;
+  uint8_t* codes = c.codes + (head * 2 + w.part) * c.s16 * DH;
+  float* scales = c.scales + (head * 2 + w.part) * c.nb;
+  // the first block may hold earlier rows: its scale can only rise
+  const int first = (max(lo, p0) >> c.shift) << c.shift;
+  const bool goes_on = first < lo;
+  const float old = goes_on ? scales[first >> c.shift] : 0.f;
+  const bf16* src = static_cast<const bf16*>(a.qkv) + static_cast<int64_t>(w.b) * a.n * a.ld_qkv +
+                    (a.H + w.part * c.KV + w.h) * static_cast<int64_t>(DH) + d8;
 
-  bf16x8 v[NP];
+  union Row {
+    bf16x8 v;
+    ushortx2 u[4];
+  };
+  Row v[4];
 #pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int t = t0 + i * TPP + tr;
-    v[i] = static_cast<bf16>(0.f);
-    if (t >= lo && t < hi) v[i] = *reinterpret_cast<const bf16x8*>(src + static_cast<int64_t>(t - lo) * a.ld_qkv);
+  for (int i = 0; i < 4; ++i) {
+    const int t = f + 4 * grp + i;
+    v[i].v = static_cast<bf16>(0.f);
+    if (t >= lo && t < hi)
+      v[i].v = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(src + static_cast<int64_t>(t - lo) * a.ld_qkv));
   }
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    union {
-      bf16x8 v;
-      uint16_t u[8];
-    } x{v[i]};
-    uint32_t m = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m = max(m, static_cast<uint32_t>(x.u[e] & 0x7fff));
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o, 64)));
-    if (lane == 0) amax_s[i * 4 + wave] = m;
-  }
-  if (tid == 0) ratio_s = 1.f;
-  __syncthreads();
-  const int per = c.block / TW;  // entries of amax_s per block
-  if (tid < TT / c.block) {
-    const int s0 = t0 + tid * c.block;
-    float inv = 0.f;
-    if (s0 < hi && s0 + c.block > lo) {
-      uint32_t m = 0;
-      for (int i = 0; i < per; ++i) m = max(m, amax_s[tid * per + i]);
-      float s = scale_needed<FMT>(m);
-      if (s0 < lo) {  // holds earlier rows: its scale can only rise
-        const float old = scales[s0 / c.block];
-        if (s == s && !(old <= s)) s = old;
-        if (old != s) ratio_s = old / s;
-      }
-      scales[s0 / c.block] = s;
-      inv = 1.f / s;
-    }
-    inv_s[tid] = inv;
-  }
-  __syncthreads();
-  const float ratio = ratio_s;
-  const bool again = ratio < 1.f;  // never for a NaN: such a block's codes say nothing
-  const int b0 = max(t0, lo / c.block * c.block);  // earlier rows to round again: b0..lo-1
 
-  // codes: keys to the cache at once, values to LDS for their transpose
+  // largest absolute value of the lane's block, as bf16 bits
+  ushortx2 m2{0, 0};
 #pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int t = t0 + i * TPP + tr;
-    if (t >= lo && t < hi) {
-      const float inv = inv_s[(t - t0) / c.block];
-      float x[8];
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = inv == inv ? static_cast<float>(v[i][e]) * inv : 0.f;
-      u32x2 q{pack_codes<FMT>(x[0], x[1], x[2], x[3]), pack_codes<FMT>(x[4], x[5], x[6], x[7])};
-      if (part == 0)
-        *reinterpret_cast<u32x2*>(codes + static_cast<int64_t>(t) * DH + d8) = q;
-      else
-        *reinterpret_cast<u32x2*>(&ct[t - t0][d8]) = q;
-    } else if (part == 0 && again && t >= b0 && t < lo) {
+    for (int e = 0; e < 4; ++e) m2 = __builtin_elementwise_max(m2, v[i].u[e] & static_cast<unsigned short>(0x7fff));
+  uint32_t mu = max(m2[0], m2[1]);
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) {
+    if (x == 32 && c.block < U) break;  // two blocks of 16 in a unit of 32: half a wave each
+    mu = max(mu, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mu), x, 64)));
+  }
+  if (c.block > U) {
+    if (lane == 0) mu_s[wave] = mu;
+    __syncthreads();
+    const int of = c.block / U, w0 = wave / of * of;
+    mu = 0;
+#pragma unroll
+    for (int x = 0; x < W; ++x) mu = max(mu, x >= w0 && x < w0 + of ? mu_s[x] : 0u);
+  }
+  const int blk = (f + 4 * grp) >> c.shift, bf = blk << c.shift;  // the lane's block
+  float s = scale_needed<FMT>(mu), ratio = 1.f;                   // ratio < 1: earlier rows are rounded again
+  if (goes_on && bf == first) {
+    if (s == s && !(old <= s)) s = old;
+    if (old < s) ratio = old / s;
+  }
+  if (lane % (64 / LN::TILES) == 0 && bf == f + 16 * (lane / 32) && bf < hi && bf + c.block > lo) scales[blk] = s;
+  const float inv = s == s ? 1.f / s : 0.f;  // 0 for NaN: such a block's codes are zeros
+  const bool again = __any(ratio < 1.f);
+  if (c.block < U) ratio = fminf(ratio, __shfl_xor(ratio, 32, 64));
+  const int from = again ? first : lo;
+  if (f >= hi || f + U <= from) return;
+
+  uint32_t q[4][2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = inv != 0.f ? static_cast<float>(v[i].v[e]) * inv : 0.f;
+    q[i][0] = pack_codes<FMT>(x[0], x[1], x[2], x[3]);
+    q[i][1] = pack_codes<FMT>(x[4], x[5], x[6], x[7]);
+  }
+  if (w.part == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = f + 4 * grp + i;
       u32x2* at = reinterpret_cast<u32x2*>(codes + static_cast<int64_t>(t) * DH + d8);
-      const u32x2 q = *at;
-      *at = u32x2{rescale4<FMT>(q[0], ratio), rescale4<FMT>(q[1], ratio)};
-    }
-  }
-  if (part == 0) return;
-  __syncthreads();
-  // 16 positions of one dimension per thread and turn
-  for (int r = tid; r < TT / 16 * DH; r += 256) {
-    const int tile = r / DH, d = r % DH, f = t0 + 16 * tile;
-    if (f >= hi || f + 16 <= (again ? b0 : lo)) continue;
-    u32x4* at = reinterpret_cast<u32x4*>(codes + static_cast<int64_t>(f) * DH + d * 16);
-    union {
-      u32x4 v;
-      uint8_t u[16];
-    } q;
-    if (f < lo || f + 16 > hi) {
-      q.v = *at;
-      if (again) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) q.v[i] = rescale4<FMT>(q.v[i], ratio);
+      if (t >= lo && t < hi) {
+        *at = u32x2{q[i][0], q[i][1]};
+      } else if (t >= from && t < lo) {
+        const u32x2 r = *at;
+        *at = u32x2{rescale4<FMT>(r[0], ratio), rescale4<FMT>(r[1], ratio)};
       }
     }
+    return;
+  }
+  if (!again && a.n < 16) {  // no whole tile: the new bytes alone
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (f + i >= lo && f + i < hi) q.u[i] = ct[16 * tile + i][d];
-    *at = q.v;
+    for (int i = 0; i < 4; ++i) {
+      const int t = f + 4 * grp + i;
+      if (t < lo || t >= hi) continue;
+      uint8_t* at = codes + static_cast<int64_t>(t & ~15) * DH + d8 * 16 + (t & 15);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) at[16 * e] = static_cast<uint8_t>(q[i][e >> 2] >> (8 * (e & 3)));
+    }
+    return;
+  }
+  uint8_t* tile = lds[wave] + (LN::TILES == 2 ? (grp >> 2) * LN::TILE_LDS : 0);
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const uint32_t in[4] = {q[0][e], q[1][e], q[2][e], q[3][e]};
+    uint32_t out[4];
+    transpose4(in, out);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<uint32_t*>(tile + LN::lds_row(d8 + 4 * e + i) + 4 * (grp & 3)) = out[i];
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int d = (lane + 64 * i) % DH, x = (lane + 64 * i) / DH, ft = f + 16 * x;
+    if (ft >= hi || ft + 16 <= from) continue;
+    u32x4* at = reinterpret_cast<u32x4*>(codes + static_cast<int64_t>(ft) * DH + d * 16);
+    u32x4 r = *reinterpret_cast<const u32x4*>(lds[wave] + x * LN::TILE_LDS + LN::lds_row(d));
+    if (ft < lo || ft + 16 > hi) {  // the other positions' bytes stay (rounded again)
+      u32x4 was = *at;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t mask = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (ft + 4 * k + e >= lo && ft + 4 * k + e < hi) mask |= 0xffu << (8 * e);
+        if (again) was[k] = rescale4<FMT>(was[k], ratio);
+        r[k] = (r[k] & mask) | (was[k] & ~mask);
+      }
+    }
+    *at = r;
   }
 }
 
-// -------------------------------------------------------------------- load
-
-// A workgroup takes 64 positions of one head's keys or values.
+// A wave takes a unit, lanes as in the store.  The rows written are not read here
+// again: stored past the caches, they leave the codes in them.
 template <int DH, int FMT>
 __global__ __launch_bounds__(256) void ld_kv8_load_k(Kv8LoadArgs a) {
-  __shared__ __align__(16) uint8_t ct[4][DH][16];
-  const int tid = threadIdx.x, part = blockIdx.y & 1, h = blockIdx.y >> 1, b = blockIdx.z;
+  using LN = Kv8Lanes<DH>;
+  constexpr int PT = LN::PT, U = LN::U;
+  __shared__ __align__(16) uint8_t lds[4][LN::TILES * LN::TILE_LDS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Kv8View& c = a.kv;
-  const int t0 = (a.pos / 64 + static_cast<int>(blockIdx.x)) * 64;
+  const Kv8Unit w = kv8_unit(blockIdx.x * 4 + wave, c.KV, a.pieces);
+  if (w.b >= c.n_seq) return;
+  const int f = (a.pos / U + w.piece) * U;
   int hi = a.pos + a.n;
-  if (a.seq_len) hi = min(hi, a.seq_len[b]);
-  if (t0 >= hi) return;
-  const int64_t head = static_cast<int64_t>(b) * c.KV + h;
-  const uint8_t* codes = c.codes + (head * 2 + part) * c.s16 * DH;
-  const float* scales = c.scales + (head * 2 + part) * c.nb;
-  if (part) {
-    for (int r = tid; r < 4 * DH; r += 256) {
-      const int f = t0 + 16 * (r / DH);
-      if (f < hi) *reinterpret_cast<u32x4*>(&ct[r / DH][r % DH][0]) = *reinterpret_cast<const u32x4*>(codes + static_cast<int64_t>(f) * DH + (r % DH) * 16);
-    }
-    __syncthreads();
-  }
-  bf16* out = static_cast<bf16*>(a.out) + static_cast<int64_t>(b) * a.n * 2 * c.KV * DH +
-              (static_cast<int64_t>(part) * c.KV + h) * DH;
-  for (int r = tid; r < 64 * (DH / 8); r += 256) {
-    const int i = r / (DH / 8), d8 = r % (DH / 8) * 8, t = t0 + i;
-    if (t < a.pos || t >= hi) continue;
-    u32x2 q;
-    if (part) {
-      union {
-        u32x2 v;
-        uint8_t u[8];
-      } x;
+  if (a.seq_len) hi = min(hi, a.seq_len[w.b]);
+  if (f >= hi) return;
+  const int grp = lane / PT, d8 = lane % PT * 8, t0 = f + 4 * grp;
+  const int64_t head = static_cast<int64_t>(w.b) * c.KV + w.h;
+  const uint8_t* codes = c.codes + (head * 2 + w.part) * c.s16 * DH;
+  const float s = t0 < hi ? c.scales[(head * 2 + w.part) * c.nb + (t0 >> c.shift)] : 0.f;
+  uint32_t q[4][2];
+  if (w.part == 0) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x.u[e] = ct[i / 16][d8 + e][i % 16];
-      q = x.v;
-    } else {
-      q = *reinterpret_cast<const u32x2*>(codes + static_cast<int64_t>(t) * DH + d8);
+    for (int i = 0; i < 4; ++i) {
+      u32x2 r{0, 0};
+      if (t0 + i >= a.pos && t0 + i < hi) r = *reinterpret_cast<const u32x2*>(codes + static_cast<int64_t>(t0 + i) * DH + d8);
+      q[i][0] = r[0];
+      q[i][1] = r[1];
     }
-    const float s = scales[t / c.block];
-    bf16x8 v = codes_to_bf16<FMT>(q[0], q[1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int d = (lane + 64 * i) % DH, x = (lane + 64 * i) / DH, ft = f + 16 * x;
+      u32x4 r{0, 0, 0, 0};
+      if (ft < hi) r = *reinterpret_cast<const u32x4*>(codes + static_cast<int64_t>(ft) * DH + d * 16);
+      *reinterpret_cast<u32x4*>(lds[wave] + x * LN::TILE_LDS + LN::lds_row(d)) = r;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const uint8_t* tile = lds[wave] + (LN::TILES == 2 ? (grp >> 2) * LN::TILE_LDS : 0);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      uint32_t in[4], out[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        in[i] = *reinterpret_cast<const uint32_t*>(tile + LN::lds_row(d8 + 4 * e + i) + 4 * (grp & 3));
+      transpose4(in, out);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i][e] = out[i];
+    }
+  }
+  const int64_t ld = 2ll * c.KV * DH;
+  bf16* out = static_cast<bf16*>(a.out) + static_cast<int64_t>(w.b) * a.n * ld +
+              (static_cast<int64_t>(w.part) * c.KV + w.h) * DH + d8;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int t = t0 + i;
+    if (t < a.pos || t >= hi) continue;
+    bf16x8 v = codes_to_bf16<FMT>(q[i][0], q[i][1]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = static_cast<bf16>(static_cast<float>(v[e]) * s);
-    *reinterpret_cast<bf16x8*>(out + static_cast<int64_t>(t - a.pos) * 2 * c.KV * DH + d8) = v;
+    __builtin_nontemporal_store(v, reinterpret_cast<bf16x8*>(out + (t - a.pos) * ld));
   }
 }
 
@@ -580,23 +667,26 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void ld_attn_decode_kv8_comb
 }
 
 template <int DH, int FMT>
-hipError_t store_t(const Kv8StoreArgs& a, hipStream_t s) {
-  const int tt = a.kv.block > 64 ? 128 : 64;
-  // tiles of any sequence: from the one that holds its first row
-  const int64_t tiles = a.seq_pos ? (static_cast<int64_t>(a.n) + tt - 2) / tt + 1
-                                  : (static_cast<int64_t>(a.pos) + a.n - 1) / tt - a.pos / tt + 1;
-  const dim3 grid(tiles, 2 * a.kv.KV, a.kv.n_seq);
-  if (tt == 64)
-    hipLaunchKernelGGL((ld_kv8_store_k<DH, FMT, 64>), grid, dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((ld_kv8_store_k<DH, FMT, 128>), grid, dim3(256), 0, s, a);
+hipError_t store_t(Kv8StoreArgs a, hipStream_t s) {
+  constexpr int U = Kv8Lanes<DH>::U;
+  const int waves = a.kv.block > 4 * U ? 8 : 4, pp = waves * U;
+  // pieces of any sequence: from the one that holds its first row
+  a.pieces = static_cast<int32_t>(a.seq_pos ? (static_cast<int64_t>(a.n) + pp - 2) / pp + 1
+                                            : (static_cast<int64_t>(a.pos) + a.n - 1) / pp - a.pos / pp + 1);
+  const int64_t wgs = 2ll * a.kv.KV * a.kv.n_seq * a.pieces;
+  if (waves == 4)
+    hipLaunchKernelGGL((ld_kv8_store_k<DH, FMT, 4>), dim3(wgs), dim3(256), 0, s, a);
+  else if constexpr (DH == 128)
+    hipLaunchKernelGGL((ld_kv8_store_k<DH, FMT, 8>), dim3(wgs), dim3(512), 0, s, a);
   return hipGetLastError();
 }
 
 template <int DH, int FMT>
-hipError_t load_t(const Kv8LoadArgs& a, hipStream_t s) {
-  const dim3 grid((static_cast<int64_t>(a.pos) + a.n - 1) / 64 - a.pos / 64 + 1, 2 * a.kv.KV, a.kv.n_seq);
-  hipLaunchKernelGGL((ld_kv8_load_k<DH, FMT>), grid, dim3(256), 0, s, a);
+hipError_t load_t(Kv8LoadArgs a, hipStream_t s) {
+  constexpr int U = Kv8Lanes<DH>::U;
+  a.pieces = static_cast<int32_t>((static_cast<int64_t>(a.pos) + a.n - 1) / U - a.pos / U + 1);
+  const int64_t units = 2ll * a.kv.KV * a.kv.n_seq * a.pieces;
+  hipLaunchKernelGGL((ld_kv8_load_k<DH, FMT>), dim3((units + 3) / 4), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

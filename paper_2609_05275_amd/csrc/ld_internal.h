@@ -372,6 +372,7 @@ struct Kv8StoreArgs {
   int64_t ld_qkv;
   int32_t H, n, pos;
   const int32_t* seq_pos;
+  int32_t pieces;  // of a sequence's rows, the launch's choice
 };
 
 // Positions pos .. pos + n - 1 (below seq_len[b] where given) to bf16 rows
@@ -381,6 +382,7 @@ struct Kv8LoadArgs {
   void* out;
   int32_t pos, n;
   const int32_t* seq_len;
+  int32_t pieces;
 };
 
 // Queries of rows b n_new + j of qkv over positions 0 .. p + j, p = pos or

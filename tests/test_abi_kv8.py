@@ -52,7 +52,8 @@ BAD_DESC = [(dict(format=2), INVALID), (dict(format=-1), INVALID), (dict(block=8
             (dict(block=48), UNSUPPORTED), (dict(block=256), UNSUPPORTED), (dict(block=0), UNSUPPORTED),
             (dict(d_head=96), UNSUPPORTED), (dict(d_head=256), UNSUPPORTED), (dict(n_seq=0), SHAPE),
             (dict(n_kv_heads=0), SHAPE), (dict(s_max=0), SHAPE), (dict(n_seq=65536), SHAPE),
-            (dict(n_kv_heads=32768), SHAPE), (dict(s_max=2 ** 31 - 1), SHAPE)]
+            (dict(n_kv_heads=32768), SHAPE), (dict(s_max=2 ** 31 - 1), SHAPE),
+            (dict(n_seq=60000, n_kv_heads=30000), SHAPE)]
 
 
 @pytest.mark.parametrize("kw,code", BAD_DESC, ids=[str(k) for k, _ in BAD_DESC])
