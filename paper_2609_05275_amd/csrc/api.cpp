@@ -1293,6 +1293,7 @@ int check_kv8_buffers(const ld_kv8* kv, Kv8View* out) {
 int check_kv8_heads(const ld_kv8* kv, int32_t n_heads) {
   if (n_heads < 1 || n_heads % kv->n_kv_heads) return fail(LD_E_SHAPE, "n_heads must be a multiple of n_kv_heads");
   if (n_heads > kMaxGridYZ) return fail(LD_E_SHAPE, "n_heads above %d", kMaxGridYZ);
+  if (static_cast<int64_t>(kv->n_seq) * n_heads * kDecMaxRows > INT32_MAX) return fail(LD_E_SHAPE, "n_seq n_heads too large");
   return LD_OK;
 }
 
@@ -1310,8 +1311,7 @@ int check_kv8_rows(const ld_kv8* kv, int32_t n_heads, int32_t n_new, int32_t pos
 
 // Partial rows of ld_attn_decode_kv8 over any number of keys up to s_max.
 size_t kv8_part_rows(const Kv8View& v, int64_t n_heads, int64_t n_new) {
-  const int64_t tiles = (n_heads / v.KV * n_new + 15) / 16;
-  return static_cast<size_t>(v.n_seq) * n_heads * n_new * attn_kv8_max_chunks(v.n_seq * v.KV * tiles, v.s16);
+  return static_cast<size_t>(v.n_seq) * n_heads * n_new * attn_kv8_max_chunks(attn_kv8_heads(v, n_heads, n_new), v.s16);
 }
 
 // C[M, N] = (R ? R : 0) + alpha * A W^T on the general GEMM kernels, for

@@ -13,6 +13,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -22,21 +23,23 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kKv8Waves = 8;  // of an attention workgroup
 constexpr int kCus = 256;
 
+
 // ------------------------------------------------------------- conversions
 
 // 8 codes (two dwords) to bf16, exact: e4m3 has 4 significant bits, int8 seven.
+// With a scale (a power of two; e4m3 only) times it.
 template <int FMT>
-__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t a, uint32_t b) {
+__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t a, uint32_t b, float scale = 1.f) {
   union {
     bf16x8 v;
     bf16x2 p[4];
     uint32_t u[4];
   } r;
   if constexpr (FMT == LD_KV8_E4M3) {
-    r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false);
-    r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
-    r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false);
-    r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
+    r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false);
+    r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+    r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false);
+    r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
   } else {
     // (opaque, or the loads' registers are split into bytes as they arrive)
     asm("" : "+v"(a), "+v"(b));
@@ -346,15 +349,15 @@ __global__ __launch_bounds__(256) void ld_kv8_load_k(Kv8LoadArgs a) {
 // --------------------------------------------------------------- attention
 
 // A workgroup of eight waves takes a chunk of keys of one key/value head for 16
-// rows (of its query heads' new rows); a wave 32 keys at a time, with its own
-// running maximum and sum; they meet once, to add up.
+// rows (of its query heads' new rows); a wave 32 keys at a time (64 for heads of
+// 64), with its own running maximum and sum; they meet once, to add up.
 //
 // Scores S^T = K Q^T and output O^T = V^T P^T on the matrix cores (16x16x32
-// bf16).  The A rows of score product t are the keys 8 g + 4 t + r (row 4 g + r),
-// so lane group g = lane / 16 of the result holds keys 8 g + 4 t + r, t < 2, r < 4, of
-// its query row: 8 neighbouring keys, half a tile of the cache's values, of one
-// scale.  They are the B operand of O^T as they stand, and 8 bytes of a value
-// tile's row the A operand.
+// bf16).  The A rows of score product t are the keys LK g + 4 t + r (row 4 g + r), LK =
+// 8 (16), so lane group g = lane / 16 of the result holds keys LK g + 4 t + r, r < 4, of
+// its query row: LK neighbouring keys, half a tile (a tile) of the cache's values,
+// of one scale.  They are the B operand of O^T as they stand, and LK bytes of a
+// value tile's row the A operand.
 //
 // Codes are exact in bf16.  A probability, times its value scale, is split in
 // two bf16 parts, which leave 2^-16 of it.
@@ -363,34 +366,44 @@ __global__ __launch_bounds__(256) void ld_kv8_load_k(Kv8LoadArgs a) {
 // and waits; 16 waves a CU at 128 registers hold 128 KB in flight.
 template <int DH, int FMT, int NQ>
 __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8AttnArgs a) {
-  constexpr int NS = DH / 64, MT = DH / 16, NW = kKv8Waves, TT = 2, LK = 4 * TT, WK = 16 * TT;
+  constexpr int NS = DH / 64, MT = DH / 16, NW = kKv8Waves, TT = DH == 64 ? 4 : 2, LK = 4 * TT, WK = 16 * TT;
   __shared__ float ml[NW][NQ][2];
   __shared__ __align__(16) float red[NW][NQ][DH];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
   const Kv8View& c = a.kv;
-  const int h = static_cast<int>(blockIdx.y) % c.KV, rt = static_cast<int>(blockIdx.y) / c.KV, b = blockIdx.z;
-  // Workgroups go round the XCDs by their number: turned by the head, or a number
-  // of chunks that shares a factor with the XCDs' would leave those of the last
-  // chunks, which short sequences do not fill, with little to do.
-  const int chunk = static_cast<int>((blockIdx.x + blockIdx.y + blockIdx.z) % gridDim.x);
-  const int G = a.H / c.KV, R = G * a.n_new;
+  // Workgroups go round the 8 XCDs by their number.  Chunks are turned by the
+  // head, or a number of chunks that shares a factor with the XCDs' would leave
+  // those of the last chunks, which short sequences do not fill, with little to do.
+  // Several row tiles: a sequence's (head, chunk) go in sets of 8, a set's tiles one
+  // after the other, so that a chunk's tiles read it through one L2 at about one time.
+  const int b = blockIdx.z;
+  int h = blockIdx.y, chunk = blockIdx.x, r0 = 0;  // r0: the workgroup's first row
+  if (a.tiles > 1) {
+    const uint32_t nc = a.n_chunks, units = c.KV * nc, set = blockIdx.x / (8 * a.tiles), of = blockIdx.x % (8 * a.tiles);
+    const uint32_t n8 = min(units - 8 * set, 8u), unit = 8 * set + of % n8;
+    h = __builtin_amdgcn_readfirstlane(unit / nc);
+    chunk = __builtin_amdgcn_readfirstlane(unit % nc);
+    r0 = __builtin_amdgcn_readfirstlane(of / n8 * 16);
+  }
+  chunk = (chunk + h + b) % a.n_chunks;
+  const int G = a.group, R = G * a.n_new;
   int p = a.pos;
   if (a.seq_pos) {
     p = a.seq_pos[b];
     if (p < 0 || p > a.pos) p = -a.n_new;  // left out: no keys
   }
   const int nk = p + a.n_new, k_first = chunk * a.chunk_keys;
-  const int rows = min(R - rt * 16, 16);
+  const int rows = min(R - r0, 16);
   const int64_t d = static_cast<int64_t>(a.H) * DH;
+  // where row r of the head goes in the output
+  auto out_at = [&](uint32_t r) {
+    return static_cast<bf16*>(a.out) + (static_cast<int64_t>(b) * a.n_new + r % static_cast<uint32_t>(a.n_new)) * d +
+           (h * G + r / static_cast<uint32_t>(a.n_new)) * static_cast<int64_t>(DH);
+  };
   if (k_first >= nk) {
-    if (chunk == 0 && a.n_chunks == 1) {  // left out: its rows are zeros (the combine's else)
-      for (int e = tid; e < rows * DH; e += 64 * NW) {
-        const int r = rt * 16 + e / DH;
-        static_cast<bf16*>(a.out)[(static_cast<int64_t>(b) * a.n_new + r % a.n_new) * d +
-                                  (h * G + r / a.n_new) * static_cast<int64_t>(DH) + e % DH] = static_cast<bf16>(0.f);
-      }
-    }
+    if (chunk == 0 && a.n_chunks == 1)  // left out: its rows are zeros (the combine's else)
+      for (int e = tid; e < rows * DH; e += 64 * NW) out_at(r0 + e / DH)[e % DH] = static_cast<bf16>(0.f);
     return;
   }
   const int k_end = min(k_first + a.chunk_keys, nk);
@@ -434,8 +447,8 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
     sv = vs[fc >> c.shift];
   };
 
-  int k0 = k_first + wave * WK;
-  const int row = rt * 16 + min(n, rows - 1), qh = h * G + row / a.n_new, j = row % a.n_new, qpos = p + j;
+  const uint32_t row = r0 + min(n, rows - 1), j = row % static_cast<uint32_t>(a.n_new);
+  const int qh = h * G + row / static_cast<uint32_t>(a.n_new), qpos = p + j;
   bf16x8 qf[NS][2];
   {
     const bf16* q = static_cast<const bf16*>(a.qkv) + (static_cast<int64_t>(b) * a.n_new + j) * a.ld_qkv +
@@ -443,8 +456,7 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
-        qf[s][e] = *reinterpret_cast<const bf16x8*>(q + 64 * s + 16 * g + 8 * e);
+      for (int e = 0; e < 2; ++e) qf[s][e] = *reinterpret_cast<const bf16x8*>(q + 64 * s + 16 * g + 8 * e);
   }
   const float al2 = a.alibi ? alibi_slope(qh, a.H) * kLog2e : 0.f, sl2 = a.scale * kLog2e;
 
@@ -453,30 +465,30 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
 #pragma unroll
   for (int i = 0; i < MT; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  for (; k0 < k_end; k0 += WK * NW) {
+  for (int k0 = k_first + wave * WK; k0 < k_end; k0 += WK * NW) {
     load_keys(k0);
     load_values(k0);
     __builtin_amdgcn_sched_barrier(0);
     const int f = k0 + LK * g;  // the lane's keys
-    const float ss = sk * sl2;
-    float x[TT][4];
+    float ss = sk * sl2;        // of a product to a base-2 score
+    floatx4 x[TT];
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
-      floatx4 s4{0.f, 0.f, 0.f, 0.f};
+      x[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
-        s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16<FMT>(kr[t][s][0], kr[t][s][1]), qf[s][0], s4, 0, 0, 0);
-        s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16<FMT>(kr[t][s][2], kr[t][s][3]), qf[s][1], s4, 0, 0, 0);
+        x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16<FMT>(kr[t][s][0], kr[t][s][1]), qf[s][0], x[t], 0, 0, 0);
+        x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16<FMT>(kr[t][s][2], kr[t][s][3]), qf[s][1], x[t], 0, 0, 0);
       }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) x[t][r] = s4[r] * ss;
-      __builtin_amdgcn_sched_barrier(0);
     }
     if (a.alibi) {
+      const float far = al2 * static_cast<float>(qpos - f);
 #pragma unroll
       for (int t = 0; t < TT; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[t][r] -= al2 * static_cast<float>(qpos - (f + 4 * t + r));
+        for (int r = 0; r < 4; ++r)
+          x[t][r] = __builtin_fmaf(x[t][r], ss, __builtin_fmaf(al2, static_cast<float>(4 * t + r), -far));
+      ss = 1.f;
     }
     const bool cut = k0 + WK - 1 > p;  // some of the keys may be behind a row, or behind the last one
     if (cut) {
@@ -486,31 +498,29 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
         for (int r = 0; r < 4; ++r)
           if (f + 4 * t + r > qpos) x[t][r] = -INFINITY;
     }
-    float mn = m;
+    // the largest score: of the lane's products (their scale is positive), then of all
+    float mn = x[0][0];
 #pragma unroll
     for (int t = 0; t < TT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) mn = fmaxf(mn, x[t][r]);
+    mn = fmaxf(m, mn * ss);
     mn = fmaxf(mn, __shfl_xor(mn, 16, 64));
     mn = fmaxf(mn, __shfl_xor(mn, 32, 64));
     const float mz = mn == -INFINITY ? 0.f : mn;  // of nothing but -inf, whose weights are 0
-    const float keep = __builtin_amdgcn_exp2f(m - mz);
     if (__any(mn != m)) {
+      const float keep = __builtin_amdgcn_exp2f(m - mz);
       l *= keep;
 #pragma unroll
       for (int i = 0; i < MT; ++i) o[i] *= keep;
     }
     m = mn;
-    bf16x8 ph[TT / 2], pl[TT / 2];
 #pragma unroll
     for (int t = 0; t < TT; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float e = __builtin_amdgcn_exp2f(x[t][r] - mz);
-        l += e;
-        x[t][r] = e * sv;
-      }
-    if (cut) {  // nothing of a masked position, whose scale may be NaN
+      for (int r = 0; r < 4; ++r)
+        x[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], ss, -mz));  // of a NaN score NaN
+    if (cut) {  // a masked position's key scale may be NaN
 #pragma unroll
       for (int t = 0; t < TT; ++t)
 #pragma unroll
@@ -520,10 +530,36 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
 #pragma unroll
     for (int t = 0; t < TT; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const bf16 whi = static_cast<bf16>(x[t][r]);
-        ph[t >> 1][4 * (t & 1) + r] = whi;
-        pl[t >> 1][4 * (t & 1) + r] = static_cast<bf16>(x[t][r] - static_cast<float>(whi));
+      for (int r = 0; r < 4; ++r) l += x[t][r];
+    // Times the value scale, which e4m3 takes with the values' conversion.  NaN, which
+    // masked positions must not see, goes with the weights alone.
+    const bool bad = sv != sv;
+    const float sv1 = bad ? 1.f : sv;
+    if constexpr (FMT == LD_KV8_INT8) {
+#pragma unroll
+      for (int t = 0; t < TT; ++t) x[t] *= sv1;
+    }
+    if (__any(bad)) {
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (bad && f + 4 * t + r <= qpos) x[t][r] = sv;
+    }
+    bf16x8 ph[TT / 2], pl[TT / 2];
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        const floatx2 w{x[t][r], x[t][r + 1]};
+        const bf16x2 hi = __builtin_convertvector(w, bf16x2);
+        const uint32_t hb = __builtin_bit_cast(uint32_t, hi);
+        const floatx2 rest{w[0] - __builtin_bit_cast(float, hb << 16), w[1] - __builtin_bit_cast(float, hb & 0xffff0000u)};
+        const bf16x2 lo = __builtin_convertvector(rest, bf16x2);
+        ph[t >> 1][4 * (t & 1) + r] = hi[0];
+        ph[t >> 1][4 * (t & 1) + r + 1] = hi[1];
+        pl[t >> 1][4 * (t & 1) + r] = lo[0];
+        pl[t >> 1][4 * (t & 1) + r + 1] = lo[1];
       }
     if (k0 + WK > nk) {  // codes behind the last key may be anything, NaN too
 #pragma unroll
@@ -534,13 +570,11 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
         for (int i = 0; i < MT; ++i) vr[i][w] &= mask;
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int u = 0; u < TT / 2; ++u) {
-        const bf16x8 v8 = codes_to_bf16<FMT>(vr[i][2 * u], vr[i][2 * u + 1]);
+        const bf16x8 v8 = codes_to_bf16<FMT>(vr[i][2 * u], vr[i][2 * u + 1], sv1);
         o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, ph[u], o[i], 0, 0, 0);
         o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, pl[u], o[i], 0, 0, 0);
       }
@@ -559,7 +593,7 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
 
   // sum over the waves, in wave order, each scaled to the chunk's maximum
   for (int e = tid; e < rows * DH; e += 64 * NW) {
-    const int i = e / DH, col = e % DH, r = rt * 16 + i;
+    const int i = e / DH, col = e % DH, r = r0 + i;
     float mw[NW], M = -INFINITY, L = 0.f, s = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
@@ -574,8 +608,7 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
       s = __builtin_fmaf(wgt, red[w][i][col], s);
     }
     if (a.n_chunks == 1) {
-      static_cast<bf16*>(a.out)[(static_cast<int64_t>(b) * a.n_new + r % a.n_new) * d +
-                                (h * G + r / a.n_new) * static_cast<int64_t>(DH) + col] = static_cast<bf16>(s * (1.f / L));
+      out_at(r)[col] = static_cast<bf16>(s * (1.f / L));
     } else {
       const int64_t pr = (head * R + r) * a.n_chunks + chunk;
       a.part_o[pr * DH + col] = s;
@@ -597,12 +630,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void ld_attn_decode_kv8_comb
   __shared__ float ml[W][2];
   __shared__ __align__(16) FRow red[W][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t r = W == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + wave : blockIdx.x;
-  if (r >= static_cast<int64_t>(a.kv.n_seq) * a.H * a.n_new) return;
+  const uint32_t id = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x, HN = a.H * a.n_new;
+  if (id >= a.kv.n_seq * HN) return;
   const int w = W == 1 ? 0 : wave;
-  const int G = a.H / a.kv.KV, R = G * a.n_new;
-  const int64_t head = r / R, b = head / a.kv.KV;
-  const int i = static_cast<int>(r % R), h = static_cast<int>(head % a.kv.KV) * G + i / a.n_new, j = i % a.n_new;
+  const int64_t r = id, b = id / HN;
+  const uint32_t h = id % HN / a.n_new, j = id % a.n_new;  // (HN is a multiple of n_new)
   int p = a.pos;
   if (a.seq_pos) {
     p = a.seq_pos[b];
@@ -692,8 +724,10 @@ hipError_t load_t(Kv8LoadArgs a, hipStream_t s) {
 
 template <int DH, int FMT>
 hipError_t attn_t(const Kv8AttnArgs& a, hipStream_t s) {
-  const int R = a.H / a.kv.KV * a.n_new;
-  const dim3 grid(a.n_chunks, a.kv.KV * ((R + 15) / 16), a.kv.n_seq), block(64 * kKv8Waves);
+  const int R = a.group * a.n_new;
+  const dim3 block(64 * kKv8Waves);
+  const dim3 grid = a.tiles == 1 ? dim3(a.n_chunks, a.kv.KV, a.kv.n_seq)
+                                 : dim3(a.kv.KV * a.n_chunks * a.tiles, 1, a.kv.n_seq);
   if (R == 1)
     hipLaunchKernelGGL((ld_attn_decode_kv8_k<DH, FMT, 1>), grid, block, 0, s, a);
   else if (R <= 8)
@@ -722,6 +756,11 @@ hipError_t launch_kv8_load(const Kv8LoadArgs& a, hipStream_t s) {
   if (a.kv.dh == 128)
     return a.kv.format == LD_KV8_E4M3 ? load_t<128, LD_KV8_E4M3>(a, s) : load_t<128, LD_KV8_INT8>(a, s);
   return a.kv.format == LD_KV8_E4M3 ? load_t<64, LD_KV8_E4M3>(a, s) : load_t<64, LD_KV8_INT8>(a, s);
+}
+
+int64_t attn_kv8_heads(const Kv8View& kv, int64_t H, int64_t n_new) {
+  const int64_t R = H / kv.KV * n_new;
+  return static_cast<int64_t>(kv.n_seq) * kv.KV * ((R + 15) / 16);
 }
 
 namespace {
@@ -759,8 +798,9 @@ int64_t attn_kv8_max_chunks(int64_t heads, int64_t keys) {
 
 hipError_t launch_attn_decode_kv8(Kv8AttnArgs a, hipStream_t s) {
   const int64_t keys = static_cast<int64_t>(a.pos) + a.n_new;
-  const int64_t R = static_cast<int64_t>(a.H / a.kv.KV) * a.n_new;
-  const int64_t heads = static_cast<int64_t>(a.kv.n_seq) * a.kv.KV * ((R + 15) / 16);
+  a.group = a.H / a.kv.KV;
+  a.tiles = (a.group * a.n_new + 15) / 16;
+  const int64_t heads = attn_kv8_heads(a.kv, a.H, a.n_new);
   a.chunk_keys = static_cast<int32_t>(attn_kv8_chunk(heads, keys, a.seq_pos != nullptr));
   a.n_chunks = static_cast<int32_t>((keys + a.chunk_keys - 1) / a.chunk_keys);
   if (a.kv.dh == 128)

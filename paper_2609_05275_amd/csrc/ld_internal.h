@@ -394,7 +394,8 @@ struct Kv8AttnArgs {
   void* out;       // [n_seq * n_new, H * dh]
   float* part_o;   // [n_seq][H * n_new rows of the heads in turn][n_chunks][dh]
   float* part_ml;  // [n_seq][H * n_new][n_chunks][2]: base-2 max, sum
-  int32_t H, n_new, pos, n_chunks, chunk_keys;
+  int32_t H, n_new, pos, group, n_chunks, chunk_keys;  // group = H / KV
+  uint32_t tiles;  // of 16 rows a key/value head
   const int32_t* seq_pos;
   float scale;
   int32_t alibi;
@@ -431,7 +432,9 @@ hipError_t launch_kv_store(const KvArgs& a, hipStream_t s);
 hipError_t launch_attn_decode(const DecAttnArgs& a, hipStream_t s);
 hipError_t launch_kv8_store(const Kv8StoreArgs& a, hipStream_t s);
 hipError_t launch_kv8_load(const Kv8LoadArgs& a, hipStream_t s);
-// Chunks of `keys` keys for `heads` workgroups a chunk; grows with keys.
+// Workgroups a chunk of an attention launch, and the most chunks of `keys` keys (it
+// grows with keys).
+int64_t attn_kv8_heads(const Kv8View& kv, int64_t H, int64_t n_new);
 int64_t attn_kv8_max_chunks(int64_t heads, int64_t keys);
 hipError_t launch_attn_decode_kv8(Kv8AttnArgs a, hipStream_t s);
 hipError_t launch_gather(int dtype, const RowsArgs& a, hipStream_t s);
