@@ -402,7 +402,7 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
            (h * G + r / static_cast<uint32_t>(a.n_new)) * static_cast<int64_t>(DH);
   };
   if (k_first >= nk) {
-    if (chunk == 0 && a.n_chunks == 1)  // left out: its rows are zeros (the combine's else)
+    if (chunk == 0)  // left out: its rows are zeros
       for (int e = tid; e < rows * DH; e += 64 * NW) out_at(r0 + e / DH)[e % DH] = static_cast<bf16>(0.f);
     return;
   }
@@ -592,6 +592,7 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
   __syncthreads();
 
   // sum over the waves, in wave order, each scaled to the chunk's maximum
+  const bool only = nk <= a.chunk_keys;  // the sequence's one chunk: its rows are the result
   for (int e = tid; e < rows * DH; e += 64 * NW) {
     const int i = e / DH, col = e % DH, r = r0 + i;
     float mw[NW], M = -INFINITY, L = 0.f, s = 0.f;
@@ -607,7 +608,7 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
       L = __builtin_fmaf(wgt, ml[w][i][1], L);
       s = __builtin_fmaf(wgt, red[w][i][col], s);
     }
-    if (a.n_chunks == 1) {
+    if (only) {
       out_at(r)[col] = static_cast<bf16>(s * (1.f / L));
     } else {
       const int64_t pr = (head * R + r) * a.n_chunks + chunk;
@@ -620,9 +621,12 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
   }
 }
 
-// W waves per (sequence, query head, new row) merge the chunks its keys fill: each
-// every W-th, 16 at once so that their partial rows are all in flight; then the
-// waves' sums, in their order.
+// W waves per (sequence, query head, new row) merge the chunks its keys fill, where
+// they are several: each every W-th, 16 at once so that their partial rows are all
+// in flight; then the waves' sums, in their order.  A launch of its own, about 4.5
+// us of a call: the last workgroup of a row doing it instead needs device-scope
+// release and acquire, which write back and empty the XCDs' L2s (a verify step over
+// 1506 keys 15.2 -> 44 us).
 template <int DH, int W>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void ld_attn_decode_kv8_combine(Kv8AttnArgs a) {
   constexpr int CL = DH / 64, U = 16;
@@ -641,6 +645,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void ld_attn_decode_kv8_comb
     if (p < 0 || p > a.pos) p = -a.n_new;
   }
   const int chunks = (p + a.n_new + a.chunk_keys - 1) / a.chunk_keys;
+  if (chunks <= 1) return;  // written by the attention kernel
   const float* po = a.part_o + r * a.n_chunks * DH + lane * CL;
   const float* pm = a.part_ml + r * a.n_chunks * 2;
   float M = -INFINITY, L = 0.f;
@@ -691,7 +696,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void ld_attn_decode_kv8_comb
       acc += wgt * red[u][lane];
     }
   }
-  if (chunks > 0) acc *= 1.f / L;
+  acc *= 1.f / L;
   bf16* out = static_cast<bf16*>(a.out) + (b * a.n_new + j) * (static_cast<int64_t>(a.H) * DH) +
               static_cast<int64_t>(h) * DH + lane * CL;
 #pragma unroll
