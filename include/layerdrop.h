@@ -292,6 +292,61 @@ int ld_stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w,
                     const float* r_eval, void* x, void* const* kv, int32_t s_max, int32_t pos,
                     int32_t n_new, void* ws, size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------- 8-bit key/value cache
+ * Keys and values in 8 bits with a scale for each block of positions of one
+ * head's keys or values: half the bytes of the bf16 cache, and decode
+ * attention takes the time of its bytes.  n_kv_heads may divide n_heads: query
+ * head h reads key/value head h / (n_heads / n_kv_heads).
+ *   format: LD_KV8_E4M3, 8-bit floats (1 sign, 4 exponent, 3 mantissa bits,
+ *           no infinities; largest Q = 448), or LD_KV8_INT8, integers
+ *           -127..127 (Q = 127).
+ *   block:  positions that share a scale: 16, 32, 64 or 128.
+ *   d_head: 64 or 128.  s_max >= 1 positions.  n_seq, 2 n_kv_heads <= 65535.
+ *   codes:  device, ld_kv8_code_bytes, 16-byte aligned.  With S16 = s_max
+ *           rounded up to 16, sequence b's head h has at
+ *           ((b n_kv_heads + h) 2) S16 d_head its keys [S16][d_head], then its
+ *           values [S16 / 16][d_head][16] (position 16 t + i at [t][.][i]).
+ *   scales: device float32 [n_seq][n_kv_heads][2][ceil(s_max / block)]
+ *           (ld_kv8_scale_bytes), keys' then values'.
+ * A value is its code times its block's scale.  A scale is a power of two, so
+ * both the division before rounding and this product are exact (in bf16 too).
+ * The scale a set of rows needs is the smallest 2^e, e >= -100, with
+ * max|x| <= Q 2^e, or NaN if an element is not finite: such a block reads as
+ * NaN as a whole, so that overflow upstream stays visible.
+ * The memory need not be initialised: a block's scale is set when its first
+ * position is written, and nothing is read behind the last one. */
+typedef enum { LD_KV8_E4M3 = 0, LD_KV8_INT8 = 1 } ld_kv8_format;
+
+typedef struct {
+  int32_t format, block, n_seq, n_kv_heads, d_head, s_max;
+  void* codes;
+  float* scales;
+} ld_kv8;
+
+/* ld_stack_eval with the keys and values of positions 0..S-1 written to 8-bit
+ * caches (bf16 only).  kv: host array of n_layers descriptors, of active layers
+ * of cfg->batch sequences and cfg->n_heads heads, s_max >= S (inactive layers' are
+ * not looked at).  The layers' own attention is over the keys and values as
+ * projected, so x is ld_stack_eval's. */
+int ld_stack_eval_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
+                      const float* r_eval, void* x, const ld_kv8* kv, void* ws, size_t ws_bytes, void* stream);
+
+/* Bytes of scratch ld_stack_decode_kv8 needs for n_new rows per sequence and
+ * caches of at most s_max positions (0 on invalid arguments). */
+size_t ld_decode_kv8_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max);
+
+/* ld_stack_decode over 8-bit caches: each active layer writes the new rows'
+ * keys and values as ld_kv8_store does and attends as ld_attn_decode_kv8 does.
+ * kv as in ld_stack_eval_kv8, pos + n_new <= every s_max.  seq_pos: NULL, or
+ * device int32[batch], each sequence's first new position, with pos their largest
+ * (see ld_kv8_store); the launches do not depend on its values, so a captured
+ * graph of this call decodes on as the caller advances them.  A sequence left out
+ * (seq_pos outside [0, pos]) writes no cache, and its rows of x are what the
+ * layers make of them without attention. */
+int ld_stack_decode_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
+                        const float* r_eval, void* x, const ld_kv8* kv, int32_t pos, const int32_t* seq_pos,
+                        int32_t n_new, void* ws, size_t ws_bytes, void* stream);
+
 /* ------------------------------------------- kernel-level entry points
  * The single kernels the layer is built from, exposed for isolated parity
  * tests and roofline measurements.  dtype is an ld_dtype; all row counts are
@@ -397,37 +452,6 @@ size_t ld_attn_decode_ws_bytes(int32_t n_seq, int32_t n_heads, int32_t d_head, i
 int ld_attn_decode(int32_t n_seq, int32_t n_heads, int32_t d_head, int32_t alibi, int32_t pos, int32_t n_new,
                    const void* qkv, const void* kv, int32_t s_max, void* o, void* ws, size_t ws_bytes,
                    void* stream);
-
-/* ---------------------------------------------- 8-bit key/value cache
- * Keys and values in 8 bits with a scale for each block of positions of one
- * head's keys or values: half the bytes of the bf16 cache, and decode
- * attention takes the time of its bytes.  n_kv_heads may divide n_heads: query
- * head h reads key/value head h / (n_heads / n_kv_heads).
- *   format: LD_KV8_E4M3, 8-bit floats (1 sign, 4 exponent, 3 mantissa bits,
- *           no infinities; largest Q = 448), or LD_KV8_INT8, integers
- *           -127..127 (Q = 127).
- *   block:  positions that share a scale: 16, 32, 64 or 128.
- *   d_head: 64 or 128.  s_max >= 1 positions.  n_seq, 2 n_kv_heads <= 65535.
- *   codes:  device, ld_kv8_code_bytes, 16-byte aligned.  With S16 = s_max
- *           rounded up to 16, sequence b's head h has at
- *           ((b n_kv_heads + h) 2) S16 d_head its keys [S16][d_head], then its
- *           values [S16 / 16][d_head][16] (position 16 t + i at [t][.][i]).
- *   scales: device float32 [n_seq][n_kv_heads][2][ceil(s_max / block)]
- *           (ld_kv8_scale_bytes), keys' then values'.
- * A value is its code times its block's scale.  A scale is a power of two, so
- * both the division before rounding and this product are exact (in bf16 too).
- * The scale a set of rows needs is the smallest 2^e, e >= -100, with
- * max|x| <= Q 2^e, or NaN if an element is not finite: such a block reads as
- * NaN as a whole, so that overflow upstream stays visible.
- * The memory need not be initialised: a block's scale is set when its first
- * position is written, and nothing is read behind the last one. */
-typedef enum { LD_KV8_E4M3 = 0, LD_KV8_INT8 = 1 } ld_kv8_format;
-
-typedef struct {
-  int32_t format, block, n_seq, n_kv_heads, d_head, s_max;
-  void* codes;
-  float* scales;
-} ld_kv8;
 
 /* Bytes of codes and of scales (the pointers are not used; 0 on an invalid
  * descriptor). */

@@ -110,6 +110,10 @@ _SIGS = {
     "ld_attn_decode_ws_bytes": (_sz, [_i32, _i32, _i32, _i32]),
     "ld_attn_decode": (C.c_int, [_i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _sz,
                                  _vp]),
+    "ld_stack_eval_kv8": (C.c_int, [_PCFG, _i32, C.POINTER(ld_weights), _vp, _vp, _vp, _PKV8, _vp, _sz, _vp]),
+    "ld_decode_kv8_ws_bytes": (_sz, [_PCFG, _i32, _i32]),
+    "ld_stack_decode_kv8": (C.c_int, [_PCFG, _i32, C.POINTER(ld_weights), _vp, _vp, _vp, _PKV8, _i32, _vp, _i32,
+                                      _vp, _sz, _vp]),
     "ld_kv8_code_bytes": (_sz, [_PKV8]),
     "ld_kv8_scale_bytes": (_sz, [_PKV8]),
     "ld_kv8_store": (C.c_int, [_PKV8, _i32, _i32, _i32, _vp, _vp, _vp]),
@@ -509,6 +513,43 @@ def ld_attn_decode_kv8(kv, n_heads, pos, n_new, qkv, o, ws, seq_pos=None, alibi=
                                    _kv8_rows(kv, n_heads, n_new, qkv, dev),
                                    _kv8_ptr(o, "o", dev, torch.bfloat16, kv.n_seq * n_new * n_heads * kv.d_head),
                                    _kv8_ptr(ws, "ws", dev), ws.numel() * ws.element_size(), _stream(stream, dev)))
+
+
+def _kv8_array(kv, n):
+    """Descriptors of n layers; None (an inactive layer's) as an empty one."""
+    if len(kv) != n:
+        raise ValueError(f"{n} layers of weights, {len(kv)} of caches")
+    for k in kv:
+        if k is not None:
+            _kv8_device(k)
+    return (ld_kv8 * n)(*[k if k is not None else ld_kv8() for k in kv])
+
+
+def ld_stack_eval_kv8(cfg, ws_list, x, ws, kv, active=None, r_eval=None, stream=None):
+    """ld_stack_eval that writes 8-bit caches; kv: a kv8() per layer (None
+    allowed for inactive layers)."""
+    L = len(ws_list)
+    wa = (ld_weights * L)(*[weights(w) for w in ws_list])
+    act, rr, kk = _u8_array(active, L), _f32_array(r_eval, L), _kv8_array(kv, L)
+    _check(_lib.ld_stack_eval_kv8(C.byref(cfg), L, wa, act, rr, _ptr(x), kk, _ptr(ws),
+                                  ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def ld_decode_kv8_ws_bytes(cfg, n_new, s_max):
+    return _lib.ld_decode_kv8_ws_bytes(C.byref(cfg), n_new, s_max)
+
+
+def ld_stack_decode_kv8(cfg, ws_list, x, kv, pos, n_new, ws, seq_pos=None, active=None, r_eval=None,
+                        stream=None):
+    """ld_stack_decode over 8-bit caches; seq_pos: int32 [batch] positions on
+    the device (at most pos), where they differ or the call is captured."""
+    L = len(ws_list)
+    _need(x, "x", torch.bfloat16, cfg.batch * n_new * cfg.d_model)
+    _need(seq_pos, "seq_pos", torch.int32, cfg.batch)
+    wa = (ld_weights * L)(*[weights(w) for w in ws_list])
+    act, rr, kk = _u8_array(active, L), _f32_array(r_eval, L), _kv8_array(kv, L)
+    _check(_lib.ld_stack_decode_kv8(C.byref(cfg), L, wa, act, rr, _ptr(x), kk, pos, _ptr(seq_pos, "seq_pos"),
+                                    n_new, _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def ld_rmsnorm_fwd(x, g, y, rstd, eps=1e-5, stream=None):

@@ -460,16 +460,36 @@ int run_gemm_pair(int dtype, GemmArgs g1, int64_t host_k1, int64_t max_k1, GemmA
 
 // ------------------------------------------------------------ one layer
 
+// The keys and values of qkv rows b n + i into an 8-bit cache at position pos + i
+// (or seq_pos[b] + i) of sequence b.
+int run_kv8_store(const Kv8View& kv, const void* qkv, int32_t n_heads, int32_t n, int32_t pos,
+                  const int32_t* seq_pos, hipStream_t s) {
+  Kv8StoreArgs a{};
+  a.kv = kv;
+  a.qkv = qkv;
+  a.ld_qkv = (static_cast<int64_t>(n_heads) + 2ll * kv.KV) * kv.dh;
+  a.H = n_heads;
+  a.n = n;
+  a.pos = pos;
+  a.seq_pos = seq_pos;
+  ProfScope ps("ld_kv8_store_k", s);
+  const hipError_t e = launch_kv8_store(a, s);
+  if (e != hipSuccess) return fail(LD_E_HIP, "kv8 store: %s", hipGetErrorString(e));
+  ps.end(0, 6.0 * kv.n_seq * n * kv.KV * kv.dh);
+  return LD_OK;
+}
+
 // Attention sub-block on the rows mv keeps.  hc: its kept count when
 // profiling (read back by the caller), else -1.  scatter = 0 leaves
 // Z = X + r f_attn(X) compacted in act (zk) for the FFN sub-block of the same
 // rows; scatter = 1 writes Z into the kept rows of x (sub-layer granularity,
 // where the FFN keeps its own rows).
 // kv: null, or a cache [B, s_max, 2d] that receives the keys and values of
-// positions 0..S-1 (evaluation form only: every sequence processed).
+// positions 0..S-1 (evaluation form only: every sequence processed); kv8: likewise,
+// in 8 bits.
 int attn_forward_part(const ld_config* cfg, const Dims& D, const ld_weights& w, const MaskView& mv,
                       const ActPtrs& act, Stream xs, int64_t hc, bool scatter, hipStream_t s,
-                      void* kv = nullptr, int32_t s_max = 0) {
+                      void* kv = nullptr, int32_t s_max = 0, const Kv8View* kv8 = nullptr) {
   const int dt = D.dtype;
   const int64_t T = D.T;
   const int64_t hm = hc * D.S;
@@ -536,6 +556,9 @@ int attn_forward_part(const ld_config* cfg, const Dims& D, const ld_weights& w, 
     if ((e = launch_kv_store(k, s)) != hipSuccess) return fail(LD_E_HIP, "kv store: %s", hipGetErrorString(e));
     ps.end(0, 2.0 * D.es * hm * 2 * D.d);
   }
+  if (kv8)
+    if (int rc = run_kv8_store(*kv8, act.at(act.L.qkv), static_cast<int32_t>(D.H), static_cast<int32_t>(D.S), 0, nullptr, s))
+      return rc;
   // causal attention on the kept sequences
   {
     AttnArgs a{};
@@ -1185,8 +1208,7 @@ int check_host_counts(const Dims& D, const LayerMasks& lm, const std::vector<int
 
 // ------------------------------------------------------ decoding helpers
 
-// Scratch of ld_stack_decode for n_new rows per sequence and caches of s_max
-// positions.
+// Scratch of a decoding step.
 struct DecLayout {
   size_t h, rstd, qkv, att, z, uv, s, part_o, part_ml, skp, skp_bytes, total;
 };
@@ -1220,7 +1242,13 @@ constexpr int32_t kMaxGridYZ = 65535;  // of HIP launches
 
 int64_t dec_chunks(int64_t keys) { return (keys + kDecKeys - 1) / kDecKeys; }
 
-DecLayout dec_layout(const Dims& D, int64_t n_new, int64_t s_max) {
+size_t dec_part_rows(const Dims& D, int64_t s_max) {
+  return static_cast<size_t>(D.B) * D.H * dec_chunks(s_max) * kDecMaxRows;
+}
+
+// Scratch of a decoding step of n_new rows per sequence.  pc: partial rows of the
+// attention (dec_part_rows, kv8_part_rows).
+DecLayout dec_layout(const Dims& D, int64_t n_new, size_t pc) {
   DecLayout L{};
   size_t o = 0;
   auto take = [&](size_t bytes) {
@@ -1236,7 +1264,6 @@ DecLayout dec_layout(const Dims& D, int64_t n_new, int64_t s_max) {
   L.z = take(es * M * D.d);
   L.uv = take(es * M * D.fw);
   L.s = take(es * M * D.f);
-  const size_t pc = static_cast<size_t>(D.B) * D.H * dec_chunks(s_max) * kDecMaxRows;
   L.part_o = take(4 * pc * D.dh);
   L.part_ml = take(4 * pc * 2);
   if (dec_split_k(M, D.d)) {
@@ -1312,6 +1339,42 @@ int check_kv8_rows(const ld_kv8* kv, int32_t n_heads, int32_t n_new, int32_t pos
 // Partial rows of ld_attn_decode_kv8 over any number of keys up to s_max.
 size_t kv8_part_rows(const Kv8View& v, int64_t n_heads, int64_t n_new) {
   return static_cast<size_t>(v.n_seq) * n_heads * n_new * attn_kv8_max_chunks(attn_kv8_heads(v, n_heads, n_new), v.s16);
+}
+
+// Attention of qkv rows b n_new + j at positions pos + j (or seq_pos[b] + j) over an
+// 8-bit cache; part_o and part_ml hold kv8_part_rows.
+int run_kv8_attn(const Kv8View& kv, const void* qkv, void* o, float* part_o, float* part_ml, int32_t n_heads,
+                 int32_t alibi, int32_t n_new, int32_t pos, const int32_t* seq_pos, hipStream_t s) {
+  Kv8AttnArgs a{};
+  a.kv = kv;
+  a.qkv = qkv;
+  a.ld_qkv = (static_cast<int64_t>(n_heads) + 2ll * kv.KV) * kv.dh;
+  a.out = o;
+  a.part_o = part_o;
+  a.part_ml = part_ml;
+  a.H = n_heads;
+  a.n_new = n_new;
+  a.pos = pos;
+  a.seq_pos = seq_pos;
+  a.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(kv.dh)));
+  a.alibi = alibi;
+  ProfScope ps("ld_attn_decode_kv8_k", s);
+  const hipError_t e = launch_attn_decode_kv8(a, s);
+  if (e != hipSuccess) return fail(LD_E_HIP, "attn decode kv8: %s", hipGetErrorString(e));
+  const double keys = static_cast<double>(pos) + n_new, rows = static_cast<double>(kv.n_seq) * n_new * n_heads * kv.dh;
+  ps.end(4.0 * rows * keys, 2.0 * kv.n_seq * keys * kv.KV * kv.dh + 4.0 * rows);
+  return LD_OK;
+}
+
+// The 8-bit cache of an active layer, with its pointers, against the
+// configuration.
+int check_kv8_layer(const Dims& D, const ld_kv8* kv, int32_t l, Kv8View* out) {
+  if (int rc = check_kv8_buffers(kv, out)) return rc;
+  if (kv->n_seq != D.B || kv->n_kv_heads != D.H || kv->d_head != D.dh)
+    return fail(LD_E_SHAPE, "kv[%d] is of %d sequences of %d heads of %d, the configuration of %lld, %lld, %lld", l,
+                kv->n_seq, kv->n_kv_heads, kv->d_head, static_cast<long long>(D.B), static_cast<long long>(D.H),
+                static_cast<long long>(D.dh));
+  return LD_OK;
 }
 
 // C[M, N] = (R ? R : 0) + alpha * A W^T on the general GEMM kernels, for
@@ -1663,21 +1726,36 @@ size_t ld_eval_ws_bytes(const ld_config* cfg) {
   return act_layout(D).total;
 }
 
-int ld_stack_eval(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
-                  const float* r_eval, void* x, void* const* kv, int32_t s_max, void* ws,
-                  size_t ws_bytes, void* stream) {
-  t_err.clear();
+}  // extern "C"
+
+namespace {
+
+// The caches of a stack's layers: bf16 ones, 8-bit ones, or (evaluation) none.
+struct StackCaches {
+  void* const* kv;     // with s_max positions each
+  int32_t s_max;
+  const ld_kv8* kv8;
+};
+
+int stack_eval(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
+               const float* r_eval, void* x, const StackCaches& c, void* ws, size_t ws_bytes, void* stream) {
   Dims D;
   if (int rc = check_cfg(cfg, &D)) return rc;
   if (n_layers < 1 || n_layers > 1024) return fail(LD_E_INVALID, "n_layers outside [1, 1024]");
   if (!w || !x || !ws) return fail(LD_E_INVALID, "NULL pointer");
-  if (kv && D.dtype != LD_BF16) return fail(LD_E_UNSUPPORTED, "KV caches are bf16 only");
-  if (kv && s_max < D.S) return fail(LD_E_SHAPE, "s_max %d < seq %lld", s_max, static_cast<long long>(D.S));
+  if ((c.kv || c.kv8) && D.dtype != LD_BF16) return fail(LD_E_UNSUPPORTED, "KV caches are bf16 only");
+  if (c.kv && c.s_max < D.S) return fail(LD_E_SHAPE, "s_max %d < seq %lld", c.s_max, static_cast<long long>(D.S));
   for (int32_t l = 0; l < n_layers; ++l) {
     if (active && !active[l]) continue;
     if (int rc = check_weights(&w[l])) return rc;
     if (r_eval && !std::isfinite(r_eval[l])) return fail(LD_E_INVALID, "r_eval[%d] not finite", l);
-    if (kv && !kv[l]) return fail(LD_E_INVALID, "kv[%d] is NULL for an active layer", l);
+    if (c.kv && !c.kv[l]) return fail(LD_E_INVALID, "kv[%d] is NULL for an active layer", l);
+    if (c.kv8) {
+      Kv8View v;
+      if (int rc = check_kv8_layer(D, &c.kv8[l], l, &v)) return rc;
+      if (c.kv8[l].s_max < D.S)
+        return fail(LD_E_SHAPE, "kv[%d]: s_max %d < seq %lld", l, c.kv8[l].s_max, static_cast<long long>(D.S));
+    }
   }
   const ActLayout al = act_layout(D);
   if (ws_bytes < al.total) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, al.total);
@@ -1687,38 +1765,85 @@ int ld_stack_eval(const ld_config* cfg, int32_t n_layers, const ld_weights* w, c
     if (active && !active[l]) continue;
     MaskView mv{nullptr, nullptr, nullptr, nullptr, r_eval ? r_eval[l] : 1.f};
     const Stream xs{x, D.dtype == LD_F32};
-    if (int rc = attn_forward_part(cfg, D, w[l], mv, act, xs, D.B, false, s, kv ? kv[l] : nullptr, s_max))
+    Kv8View v;
+    if (c.kv8)
+      if (int rc = check_kv8_layer(D, &c.kv8[l], l, &v)) return rc;
+    if (int rc = attn_forward_part(cfg, D, w[l], mv, act, xs, D.B, false, s, c.kv ? c.kv[l] : nullptr, c.s_max,
+                                   c.kv8 ? &v : nullptr))
       return rc;
     if (int rc = ffn_forward_part(cfg, D, w[l], mv, act, xs, D.B, false, s)) return rc;
   }
   return LD_OK;
 }
 
+}  // namespace
+
+extern "C" {
+
+int ld_stack_eval(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
+                  const float* r_eval, void* x, void* const* kv, int32_t s_max, void* ws,
+                  size_t ws_bytes, void* stream) {
+  t_err.clear();
+  return stack_eval(cfg, n_layers, w, active, r_eval, x, {kv, s_max, nullptr}, ws, ws_bytes, stream);
+}
+
+int ld_stack_eval_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
+                      const float* r_eval, void* x, const ld_kv8* kv, void* ws, size_t ws_bytes, void* stream) {
+  t_err.clear();
+  if (!kv) return fail(LD_E_INVALID, "NULL kv");
+  return stack_eval(cfg, n_layers, w, active, r_eval, x, {nullptr, 0, kv}, ws, ws_bytes, stream);
+}
+
 size_t ld_decode_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max) {
   Dims D;
   if (check_cfg(cfg, &D) || n_new < 1 || n_new > kDecMaxRows || s_max < 1) return 0;
-  return dec_layout(D, n_new, s_max).total;
+  return dec_layout(D, n_new, dec_part_rows(D, s_max)).total;
 }
 
-int ld_stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
-                    const float* r_eval, void* x, void* const* kv, int32_t s_max, int32_t pos,
-                    int32_t n_new, void* ws, size_t ws_bytes, void* stream) {
-  t_err.clear();
+size_t ld_decode_kv8_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max) {
+  Dims D;
+  if (check_cfg(cfg, &D) || n_new < 1 || n_new > kDecMaxRows || s_max < 1) return 0;
+  const ld_kv8 kv{LD_KV8_E4M3, 64, static_cast<int32_t>(D.B), static_cast<int32_t>(D.H), static_cast<int32_t>(D.dh),
+                  s_max, nullptr, nullptr};
+  Kv8View v;
+  if (check_kv8(&kv, &v)) return 0;
+  return dec_layout(D, n_new, kv8_part_rows(v, D.H, n_new)).total;
+}
+
+}  // extern "C"
+
+namespace {
+
+int stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
+                 const float* r_eval, void* x, const StackCaches& c, int32_t pos, const int32_t* seq_pos,
+                 int32_t n_new, void* ws, size_t ws_bytes, void* stream) {
   Dims D;
   if (int rc = check_cfg(cfg, &D)) return rc;
   if (D.dtype != LD_BF16) return fail(LD_E_UNSUPPORTED, "decoding is bf16 only");
   if (n_layers < 1 || n_layers > 1024) return fail(LD_E_INVALID, "n_layers outside [1, 1024]");
-  if (!w || !x || !kv || !ws) return fail(LD_E_INVALID, "NULL pointer");
+  if (!w || !x || (!c.kv && !c.kv8) || !ws) return fail(LD_E_INVALID, "NULL pointer");
   if (n_new < 1 || n_new > kDecMaxRows) return fail(LD_E_INVALID, "n_new outside [1, %d]", kDecMaxRows);
-  if (pos < 0 || s_max < 1 || static_cast<int64_t>(pos) + n_new > s_max)
-    return fail(LD_E_SHAPE, "positions %d..%d outside the cache of %d", pos, pos + n_new - 1, s_max);
+  if (pos < 0) return fail(LD_E_SHAPE, "pos %d < 0", pos);
+  if (reinterpret_cast<uintptr_t>(seq_pos) & 3) return fail(LD_E_INVALID, "seq_pos must be 4-byte aligned");
+  size_t part_rows = c.kv ? dec_part_rows(D, std::max(c.s_max, 1)) : 0;
+  auto inside = [&](int32_t s_max) { return s_max >= 1 && static_cast<int64_t>(pos) + n_new <= s_max; };
+  if (c.kv && !inside(c.s_max))
+    return fail(LD_E_SHAPE, "positions %d..%d outside the cache of %d", pos, pos + n_new - 1, c.s_max);
   for (int32_t l = 0; l < n_layers; ++l) {
     if (active && !active[l]) continue;
     if (int rc = check_weights(&w[l])) return rc;
     if (r_eval && !std::isfinite(r_eval[l])) return fail(LD_E_INVALID, "r_eval[%d] not finite", l);
-    if (!kv[l]) return fail(LD_E_INVALID, "kv[%d] is NULL for an active layer", l);
+    if (c.kv && !c.kv[l]) return fail(LD_E_INVALID, "kv[%d] is NULL for an active layer", l);
+    if (c.kv8) {
+      Kv8View v;
+      if (int rc = check_kv8_layer(D, &c.kv8[l], l, &v)) return rc;
+      if (!inside(c.kv8[l].s_max))
+        return fail(LD_E_SHAPE, "positions %d..%lld outside kv[%d] of %d", pos, static_cast<long long>(pos) + n_new - 1, l,
+                    c.kv8[l].s_max);
+      part_rows = std::max(part_rows, kv8_part_rows(v, D.H, n_new));
+    }
   }
-  const DecLayout L = dec_layout(D, n_new, s_max);
+  const DecLayout L = dec_layout(D, n_new, part_rows);
   if (ws_bytes < L.total) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, L.total);
   hipStream_t s = as_stream(stream);
   char* base = static_cast<char*>(ws);
@@ -1754,13 +1879,13 @@ int ld_stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w,
     const float r = r_eval ? r_eval[l] : 1.f;
     const ld_weights& wl = w[l];
     // h = RMSNorm(x); qkv = h W_qkv^T; new keys/values into the cache
-    const KvOut ko{kv[l], static_cast<int32_t>(d), n_new, s_max, pos};
+    const KvOut ko{c.kv ? c.kv[l] : nullptr, static_cast<int32_t>(d), n_new, c.s_max, pos};
     if (!fused && !h_ready)
       if (int rc = norm(x, wl.g_attn)) return rc;
     h_ready = false;
     if (fused) {
       if (int rc = dec_proj(x, d, wl.g_attn, cfg->rms_eps, wl.w_qkv, d, P(L.qkv), 3 * d, nullptr, 0, M, 3 * d, d, 1.f,
-                            kDecActNone, s, &ko))
+                            kDecActNone, s, c.kv ? &ko : nullptr))
         return rc;
     } else if (part_fused) {
       SkinnyArgs g = skinny_args(P(L.h), d, wl.w_qkv, d, M, 3 * d, d, 1.f);
@@ -1775,40 +1900,53 @@ int ld_stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w,
       if (int rc = run_skinny(g, ks, skp, L.skp_bytes, s)) return rc;
     } else {
       if (int rc = dec_gemm(P(L.h), d, wl.w_qkv, d, P(L.qkv), 3 * d, nullptr, 0, M, 3 * d, d, 1.f, s)) return rc;
-      KvArgs k{};
-      k.qkv = P(L.qkv);
-      k.ld_qkv = 3 * d;
-      k.cache = kv[l];
-      k.s_max = s_max;
-      k.d = static_cast<int32_t>(d);
-      k.n = n_new;
-      k.n_seq = static_cast<int32_t>(D.B);
-      k.pos = pos;
-      ProfScope ps("ld_kv_store_k", s);
-      if ((e = launch_kv_store(k, s)) != hipSuccess) return fail(LD_E_HIP, "kv store: %s", hipGetErrorString(e));
-      ps.end(0, 8.0 * M * d);
+      if (c.kv) {
+        KvArgs k{};
+        k.qkv = P(L.qkv);
+        k.ld_qkv = 3 * d;
+        k.cache = c.kv[l];
+        k.s_max = c.s_max;
+        k.d = static_cast<int32_t>(d);
+        k.n = n_new;
+        k.n_seq = static_cast<int32_t>(D.B);
+        k.pos = pos;
+        ProfScope ps("ld_kv_store_k", s);
+        if ((e = launch_kv_store(k, s)) != hipSuccess) return fail(LD_E_HIP, "kv store: %s", hipGetErrorString(e));
+        ps.end(0, 8.0 * M * d);
+      }
     }
     // attention of the new rows over positions 0..pos+n_new-1 of the cache
-    DecAttnArgs at{};
-    at.qkv = P(L.qkv);
-    at.ld_qkv = 3 * d;
-    at.cache = kv[l];
-    at.s_max = s_max;
-    at.out = P(L.att);
-    at.part_o = reinterpret_cast<float*>(base + L.part_o);
-    at.part_ml = reinterpret_cast<float*>(base + L.part_ml);
-    at.n_seq = static_cast<int32_t>(D.B);
-    at.H = static_cast<int32_t>(D.H);
-    at.dh = static_cast<int32_t>(D.dh);
-    at.n_new = n_new;
-    at.pos = pos;
-    at.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(D.dh)));
-    at.alibi = D.kind == LD_BLOCK_ALIBI_RELU2;
-    {
-      ProfScope ps("ld_attn_decode_bf16", s);
-      if ((e = launch_attn_decode(at, s)) != hipSuccess) return fail(LD_E_HIP, "attn decode: %s", hipGetErrorString(e));
-      const double keys = static_cast<double>(pos) + n_new;
-      ps.end(4.0 * M * d * keys, 2.0 * D.B * keys * 2 * d + 4.0 * M * d);
+    const int alibi = D.kind == LD_BLOCK_ALIBI_RELU2;
+    float* part_o = reinterpret_cast<float*>(base + L.part_o);
+    float* part_ml = reinterpret_cast<float*>(base + L.part_ml);
+    if (c.kv8) {
+      Kv8View v;
+      const int32_t H = static_cast<int32_t>(D.H);
+      if (int rc = check_kv8_layer(D, &c.kv8[l], l, &v)) return rc;
+      if (int rc = run_kv8_store(v, P(L.qkv), H, n_new, pos, seq_pos, s)) return rc;
+      if (int rc = run_kv8_attn(v, P(L.qkv), P(L.att), part_o, part_ml, H, alibi, n_new, pos, seq_pos, s)) return rc;
+    } else {
+      DecAttnArgs at{};
+      at.qkv = P(L.qkv);
+      at.ld_qkv = 3 * d;
+      at.cache = c.kv[l];
+      at.s_max = c.s_max;
+      at.out = P(L.att);
+      at.part_o = part_o;
+      at.part_ml = part_ml;
+      at.n_seq = static_cast<int32_t>(D.B);
+      at.H = static_cast<int32_t>(D.H);
+      at.dh = static_cast<int32_t>(D.dh);
+      at.n_new = n_new;
+      at.pos = pos;
+      at.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(D.dh)));
+      at.alibi = alibi;
+      {
+        ProfScope ps("ld_attn_decode_bf16", s);
+        if ((e = launch_attn_decode(at, s)) != hipSuccess) return fail(LD_E_HIP, "attn decode: %s", hipGetErrorString(e));
+        const double keys = static_cast<double>(pos) + n_new;
+        ps.end(4.0 * M * d * keys, 2.0 * D.B * keys * 2 * d + 4.0 * M * d);
+      }
     }
     // z = x + r (att W_o^T); h = RMSNorm(z); uv = h W_gate_up^T; s = act(uv)
     if (fused) {
@@ -1871,6 +2009,25 @@ int ld_stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w,
     if (int rc = dec_gemm(P(L.s), D.f, wl.w_down, D.f, x, d, P(L.z), d, M, d, D.f, r, s)) return rc;
   }
   return LD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ld_stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
+                    const float* r_eval, void* x, void* const* kv, int32_t s_max, int32_t pos,
+                    int32_t n_new, void* ws, size_t ws_bytes, void* stream) {
+  t_err.clear();
+  return stack_decode(cfg, n_layers, w, active, r_eval, x, {kv, s_max, nullptr}, pos, nullptr, n_new, ws, ws_bytes,
+                      stream);
+}
+
+int ld_stack_decode_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
+                        const float* r_eval, void* x, const ld_kv8* kv, int32_t pos, const int32_t* seq_pos,
+                        int32_t n_new, void* ws, size_t ws_bytes, void* stream) {
+  t_err.clear();
+  return stack_decode(cfg, n_layers, w, active, r_eval, x, {nullptr, 0, kv}, pos, seq_pos, n_new, ws, ws_bytes, stream);
 }
 
 // ------------------------------------------------------ kernel-level calls
@@ -2124,18 +2281,10 @@ size_t ld_kv8_scale_bytes(const ld_kv8* kv) {
 int ld_kv8_store(const ld_kv8* kv, int32_t n_heads, int32_t n_new, int32_t pos, const int32_t* seq_pos,
                  const void* qkv, void* stream) {
   t_err.clear();
-  Kv8StoreArgs a{};
-  if (int rc = check_kv8_buffers(kv, &a.kv)) return rc;
+  Kv8View v;
+  if (int rc = check_kv8_buffers(kv, &v)) return rc;
   if (int rc = check_kv8_rows(kv, n_heads, n_new, pos, qkv, seq_pos)) return rc;
-  a.qkv = qkv;
-  a.ld_qkv = (static_cast<int64_t>(n_heads) + 2ll * kv->n_kv_heads) * kv->d_head;
-  a.H = n_heads;
-  a.n = n_new;
-  a.pos = pos;
-  a.seq_pos = seq_pos;
-  hipError_t e = launch_kv8_store(a, as_stream(stream));
-  if (e != hipSuccess) return fail(LD_E_HIP, "kv8 store: %s", hipGetErrorString(e));
-  return LD_OK;
+  return run_kv8_store(v, qkv, n_heads, n_new, pos, seq_pos, as_stream(stream));
 }
 
 int ld_kv8_load(const ld_kv8* kv, int32_t pos, int32_t n, const int32_t* seq_len, void* out, void* stream) {
@@ -2151,8 +2300,10 @@ int ld_kv8_load(const ld_kv8* kv, int32_t pos, int32_t n, const int32_t* seq_len
   a.pos = pos;
   a.n = n;
   a.seq_len = seq_len;
+  ProfScope ps("ld_kv8_load_k", as_stream(stream));
   hipError_t e = launch_kv8_load(a, as_stream(stream));
   if (e != hipSuccess) return fail(LD_E_HIP, "kv8 load: %s", hipGetErrorString(e));
+  ps.end(0, 6.0 * kv->n_seq * n * kv->n_kv_heads * kv->d_head);
   return LD_OK;
 }
 
@@ -2166,8 +2317,8 @@ size_t ld_attn_decode_kv8_ws_bytes(const ld_kv8* kv, int32_t n_heads, int32_t n_
 int ld_attn_decode_kv8(const ld_kv8* kv, int32_t n_heads, int32_t alibi, int32_t pos, const int32_t* seq_pos,
                        int32_t n_new, const void* qkv, void* o, void* ws, size_t ws_bytes, void* stream) {
   t_err.clear();
-  Kv8AttnArgs a{};
-  if (int rc = check_kv8_buffers(kv, &a.kv)) return rc;
+  Kv8View v;
+  if (int rc = check_kv8_buffers(kv, &v)) return rc;
   if (n_new < 1 || n_new > kDecMaxRows) return fail(LD_E_INVALID, "n_new outside [1, %d]", kDecMaxRows);
   if (alibi != 0 && alibi != 1) return fail(LD_E_INVALID, "alibi must be 0 or 1");
   if (int rc = check_kv8_rows(kv, n_heads, n_new, pos, qkv, seq_pos)) return rc;
@@ -2175,20 +2326,9 @@ int ld_attn_decode_kv8(const ld_kv8* kv, int32_t n_heads, int32_t alibi, int32_t
   if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(LD_E_INVALID, "ws must be 16-byte aligned");
   const size_t need = ld_attn_decode_kv8_ws_bytes(kv, n_heads, n_new);
   if (ws_bytes < need) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
-  a.qkv = qkv;
-  a.ld_qkv = (static_cast<int64_t>(n_heads) + 2ll * kv->n_kv_heads) * kv->d_head;
-  a.out = o;
-  a.part_o = static_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + up(4 * kv8_part_rows(a.kv, n_heads, n_new) * a.kv.dh));
-  a.H = n_heads;
-  a.n_new = n_new;
-  a.pos = pos;
-  a.seq_pos = seq_pos;
-  a.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(kv->d_head)));
-  a.alibi = alibi;
-  hipError_t e = launch_attn_decode_kv8(a, as_stream(stream));
-  if (e != hipSuccess) return fail(LD_E_HIP, "attn decode kv8: %s", hipGetErrorString(e));
-  return LD_OK;
+  float* part_o = static_cast<float*>(ws);
+  float* part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + up(4 * kv8_part_rows(v, n_heads, n_new) * v.dh));
+  return run_kv8_attn(v, qkv, o, part_o, part_ml, n_heads, alibi, n_new, pos, seq_pos, as_stream(stream));
 }
 
 size_t ld_gemm_ws_bytes(int32_t dtype, int32_t a_kcontig, int32_t b_kcontig, int32_t M, int32_t N,
