@@ -769,35 +769,54 @@ int64_t attn_kv8_heads(const Kv8View& kv, int64_t H, int64_t n_new) {
 }
 
 namespace {
-constexpr int64_t kKv8MinChunk = 512, kKv8RaggedWgs = 16 * kCus;
-}
 
-// Keys of a chunk, for `heads` (sequence, head, 16 rows).  Lengths that the host
-// knows: what costs least, rounds of one workgroup per CU, each its keys and
-// about 128 more, and a second launch like 500.  Otherwise (`ragged`, keys being
-// the longest a sequence can have) about 16 workgroups a CU, so that whatever the
-// lengths are spreads evenly.
-int64_t attn_kv8_chunk(int64_t heads, int64_t keys, bool ragged) {
-  const int64_t most = keys <= 1024 ? 1 : keys / kKv8MinChunk;
-  int64_t best = 1;
-  if (ragged) {
-    best = (kKv8RaggedWgs + heads - 1) / heads;
-    if (best > most) best = most;
-  } else {
-    int64_t best_cost = INT64_MAX;
-    for (int64_t n = 1; n <= most && (n == 1 || heads * (n - 1) < 4 * kCus); ++n) {
-      const int64_t cost = (heads * n + kCus - 1) / kCus * ((keys + n - 1) / n + 128) + (n > 1 ? 500 : 0);
-      if (cost < best_cost) {
-        best = n;
-        best_cost = cost;
-      }
+constexpr int64_t kKv8MinChunk = 256, kKv8OneChunk = 1024, kKv8RaggedChunk = 576, kKv8FewChunk = 320, kKv8MaxWgs = 8192;
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Chunks of a head's keys where the host knows the lengths: what costs least, in
+// ns.  Workgroups come to the CUs in rounds of 256, and it takes 3 us to change
+// over.  In a full round a CU gets its share of 6 TB/s (of twice and two and a half
+// times that where two or more row tiles read a chunk through one L2); in the last,
+// more the fewer there are, up to the 36 (int8: 28) bytes a ns that one workgroup
+// takes in on its own.  Several chunks are a second launch, 3.5 us more.  (us at n
+// chunks: 24 heads of 128 over 43825 keys 49.4 at 8, 51 to 52.5 at 10 to 96; 140 heads
+// over 3682 30.2 at 1, 32 to 34 at 3 to 14; 120 over 4321, int8, 29.2 at 2, 30 to 31 at 4
+// to 16; 24 over 1217, six rows, int8, 13.8 at 1, 12.1 at 2, 9.9 at 4; 16 of 64 of 3
+// sequences over 13181 with 40 rows 43 at 1, 34 at 4, 30.4 at 5.)
+int64_t chunks_known(const Kv8AttnArgs& a, int64_t heads, int64_t keys) {
+  const int64_t most = keys <= kKv8OneChunk ? 1 : keys / kKv8MinChunk, lone = a.kv.format == LD_KV8_INT8 ? 28 : 36;
+  const int64_t twice = a.tiles > 2 ? 5 : 2 * a.tiles;  // 2 x tiles that share a reading
+  int64_t best = 1, best_cost = INT64_MAX;
+  for (int64_t n = 1; n <= most && (n == 1 || heads * (n - 1) < 4 * kCus); ++n) {
+    const int64_t bytes = div_up(keys, n) * 2 * a.kv.dh, wgs = heads * n, rest = wgs % kCus;
+    int64_t cost = wgs / kCus * (2 * bytes * kCus / (6000 * twice)) + (div_up(wgs, kCus) - 1) * 3000 + (n > 1 ? 3500 : 0);
+    if (rest) cost += bytes / (lone * rest < 3000 * twice ? lone : 3000 * twice / rest);
+    if (cost < best_cost) {
+      best = n;
+      best_cost = cost;
     }
   }
-  return ((keys + best - 1) / best + 63) / 64 * 64;
+  return best;
 }
 
+// Where it does not (keys being the most a sequence can have): chunks of about 576
+// keys, so that whatever the lengths are spreads evenly; shorter ones where those
+// would be few.  (32 heads of 16 sequences of 8 to 8192 keys: 57 us, in chunks of 1024
+// 61; 8 heads of 5, up to 8235, int8: 13.4 us with 384 keys, 16.0 with 1030.)
+int64_t chunks_ragged(int64_t heads, int64_t keys) {
+  if (keys <= kKv8OneChunk) return 1;
+  int64_t n = div_up(keys, kKv8RaggedChunk), few = 4 * kCus / heads;
+  if (few > keys / kKv8FewChunk) few = keys / kKv8FewChunk;
+  if (n < few) n = few;
+  const int64_t most = div_up(kKv8MaxWgs, heads);
+  return n < most ? n : most;
+}
+
+}  // namespace
+
 int64_t attn_kv8_max_chunks(int64_t heads, int64_t keys) {
-  const int64_t by_keys = (keys + kKv8MinChunk - 1) / kKv8MinChunk, by_wgs = (kKv8RaggedWgs + heads - 1) / heads;
+  const int64_t by_keys = div_up(keys, kKv8MinChunk), by_wgs = div_up(kKv8MaxWgs, heads);
   return by_keys < by_wgs ? by_keys : by_wgs;
 }
 
@@ -806,8 +825,9 @@ hipError_t launch_attn_decode_kv8(Kv8AttnArgs a, hipStream_t s) {
   a.group = a.H / a.kv.KV;
   a.tiles = (a.group * a.n_new + 15) / 16;
   const int64_t heads = attn_kv8_heads(a.kv, a.H, a.n_new);
-  a.chunk_keys = static_cast<int32_t>(attn_kv8_chunk(heads, keys, a.seq_pos != nullptr));
-  a.n_chunks = static_cast<int32_t>((keys + a.chunk_keys - 1) / a.chunk_keys);
+  const int64_t n = a.seq_pos ? chunks_ragged(heads, keys) : chunks_known(a, heads, keys);
+  a.chunk_keys = static_cast<int32_t>(div_up(div_up(keys, n), 64) * 64);
+  a.n_chunks = static_cast<int32_t>(div_up(keys, a.chunk_keys));
   if (a.kv.dh == 128)
     return a.kv.format == LD_KV8_E4M3 ? attn_t<128, LD_KV8_E4M3>(a, s) : attn_t<128, LD_KV8_INT8>(a, s);
   return a.kv.format == LD_KV8_E4M3 ? attn_t<64, LD_KV8_E4M3>(a, s) : attn_t<64, LD_KV8_INT8>(a, s);
