@@ -622,14 +622,14 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
 }
 
 // W waves per (sequence, query head, new row) merge the chunks its keys fill, where
-// they are several: each every W-th, 16 at once so that their partial rows are all
+// they are several: each every W-th, U at once so that their partial rows are all
 // in flight; then the waves' sums, in their order.  A launch of its own, about 4.5
 // us of a call: the last workgroup of a row doing it instead needs device-scope
 // release and acquire, which write back and empty the XCDs' L2s (a verify step over
 // 1506 keys 15.2 -> 44 us).
-template <int DH, int W>
+template <int DH, int W, int U>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void ld_attn_decode_kv8_combine(Kv8AttnArgs a) {
-  constexpr int CL = DH / 64, U = 16;
+  constexpr int CL = DH / 64;
   typedef float FRow __attribute__((ext_vector_type(CL)));
   __shared__ float ml[W][2];
   __shared__ __align__(16) FRow red[W][64];
@@ -639,15 +639,14 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void ld_attn_decode_kv8_comb
   const int w = W == 1 ? 0 : wave;
   const int64_t r = id, b = id / HN;
   const uint32_t h = id % HN / a.n_new, j = id % a.n_new;  // (HN is a multiple of n_new)
-  int p = a.pos;
+  int chunks = a.n_chunks;
   if (a.seq_pos) {
-    p = a.seq_pos[b];
-    if (p < 0 || p > a.pos) p = -a.n_new;
+    const int p = a.seq_pos[b];
+    chunks = p < 0 || p > a.pos ? 0 : (p + a.n_new + a.chunk_keys - 1) / a.chunk_keys;
   }
-  const int chunks = (p + a.n_new + a.chunk_keys - 1) / a.chunk_keys;
   if (chunks <= 1) return;  // written by the attention kernel
   const float* po = a.part_o + r * a.n_chunks * DH + lane * CL;
-  const float* pm = a.part_ml + r * a.n_chunks * 2;
+  const floatx2* pm = reinterpret_cast<const floatx2*>(a.part_ml) + r * a.n_chunks;
   float M = -INFINITY, L = 0.f;
   FRow acc = 0.f;
   for (int c0 = w; c0 < chunks; c0 += U * W) {
@@ -657,8 +656,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void ld_attn_decode_kv8_comb
     for (int u = 0; u < U; ++u) {  // past the last chunk: the last again, dropped below
       const int64_t c = min(c0 + u * W, chunks - 1);
       v[u] = *reinterpret_cast<const FRow*>(po + c * DH);
-      mc[u] = pm[c * 2];
-      lc[u] = pm[c * 2 + 1];
+      const floatx2 x = pm[c];
+      mc[u] = x[0];
+      lc[u] = x[1];
     }
     __builtin_amdgcn_sched_barrier(0);
     float m = M;
@@ -743,9 +743,11 @@ hipError_t attn_t(const Kv8AttnArgs& a, hipStream_t s) {
   if (e != hipSuccess || a.n_chunks == 1) return e;
   const int64_t rows = static_cast<int64_t>(a.kv.n_seq) * a.H * a.n_new;
   if (a.n_chunks > 8 && rows <= 8192)
-    hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 8>), dim3(rows), dim3(512), 0, s, a);
+    hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 8, 8>), dim3(rows), dim3(512), 0, s, a);
+  else if (a.n_chunks > 4)
+    hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 1, 16>), dim3((rows + 3) / 4), dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 1>), dim3((rows + 3) / 4), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 1, 4>), dim3((rows + 3) / 4), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
