@@ -132,6 +132,7 @@ struct Kv8Lanes {
 struct Kv8Unit {
   int b, piece, h, part;
 };
+__device__ __forceinline__ uint32_t kv8_workgroup() { return blockIdx.y * gridDim.x + blockIdx.x; }  // see kv8_grid
 __device__ __forceinline__ Kv8Unit kv8_unit(uint32_t id, uint32_t KV, uint32_t pieces) {
   const uint32_t head = id >> 1, at = head / KV;
   return Kv8Unit{static_cast<int>(at / pieces), static_cast<int>(at % pieces), static_cast<int>(head % KV),
@@ -148,7 +149,8 @@ __global__ __launch_bounds__(64 * W) void ld_kv8_store_k(Kv8StoreArgs a) {
   __shared__ uint32_t mu_s[W];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Kv8View& c = a.kv;
-  const Kv8Unit w = kv8_unit(blockIdx.x, c.KV, a.pieces);
+  const Kv8Unit w = kv8_unit(kv8_workgroup(), c.KV, a.pieces);
+  if (w.b >= c.n_seq) return;
   int p = a.pos;
   if (a.seq_pos) {
     p = a.seq_pos[w.b];
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(256) void ld_kv8_load_k(Kv8LoadArgs a) {
   __shared__ __align__(16) uint8_t lds[4][LN::TILES * LN::TILE_LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Kv8View& c = a.kv;
-  const Kv8Unit w = kv8_unit(blockIdx.x * 4 + wave, c.KV, a.pieces);
+  const Kv8Unit w = kv8_unit(kv8_workgroup() * 4 + wave, c.KV, a.pieces);
   if (w.b >= c.n_seq) return;
   const int f = (a.pos / U + w.piece) * U;
   int hi = a.pos + a.n;
@@ -531,9 +533,10 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
     for (int t = 0; t < TT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) l += x[t][r];
-    // Times the value scale, which e4m3 takes with the values' conversion.  NaN, which
-    // masked positions must not see, goes with the weights alone.
-    const bool bad = sv != sv;
+    // Times the value scale, which e4m3 takes with the values' conversion.  Masked
+    // positions must not see NaN, nor values that become infinite by it: such a
+    // scale goes with the weights.
+    const bool bad = !(sv < 0x1p119f);
     const float sv1 = bad ? 1.f : sv;
     if constexpr (FMT == LD_KV8_INT8) {
 #pragma unroll
@@ -544,7 +547,7 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
       for (int t = 0; t < TT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (bad && f + 4 * t + r <= qpos) x[t][r] = sv;
+          if (bad && f + 4 * t + r <= qpos) x[t][r] *= sv;
     }
     bf16x8 ph[TT / 2], pl[TT / 2];
 #pragma unroll
@@ -703,6 +706,12 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void ld_attn_decode_kv8_comb
   for (int cc = 0; cc < CL; ++cc) out[cc] = static_cast<bf16>(acc[cc]);
 }
 
+// Workgroups in two dimensions: one takes 2^32 threads at most.
+dim3 kv8_grid(int64_t wgs) {
+  constexpr int64_t kX = 1 << 20;
+  return wgs <= kX ? dim3(wgs) : dim3(kX, (wgs + kX - 1) / kX);
+}
+
 template <int DH, int FMT>
 hipError_t store_t(Kv8StoreArgs a, hipStream_t s) {
   constexpr int U = Kv8Lanes<DH>::U;
@@ -712,9 +721,9 @@ hipError_t store_t(Kv8StoreArgs a, hipStream_t s) {
                                             : (static_cast<int64_t>(a.pos) + a.n - 1) / pp - a.pos / pp + 1);
   const int64_t wgs = 2ll * a.kv.KV * a.kv.n_seq * a.pieces;
   if (waves == 4)
-    hipLaunchKernelGGL((ld_kv8_store_k<DH, FMT, 4>), dim3(wgs), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((ld_kv8_store_k<DH, FMT, 4>), kv8_grid(wgs), dim3(256), 0, s, a);
   else if constexpr (DH == 128)
-    hipLaunchKernelGGL((ld_kv8_store_k<DH, FMT, 8>), dim3(wgs), dim3(512), 0, s, a);
+    hipLaunchKernelGGL((ld_kv8_store_k<DH, FMT, 8>), kv8_grid(wgs), dim3(512), 0, s, a);
   return hipGetLastError();
 }
 
@@ -723,7 +732,7 @@ hipError_t load_t(Kv8LoadArgs a, hipStream_t s) {
   constexpr int U = Kv8Lanes<DH>::U;
   a.pieces = static_cast<int32_t>((static_cast<int64_t>(a.pos) + a.n - 1) / U - a.pos / U + 1);
   const int64_t units = 2ll * a.kv.KV * a.kv.n_seq * a.pieces;
-  hipLaunchKernelGGL((ld_kv8_load_k<DH, FMT>), dim3((units + 3) / 4), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((ld_kv8_load_k<DH, FMT>), kv8_grid((units + 3) / 4), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -393,6 +393,22 @@ def test_attn_nan_and_infinite(fmt):
     np.testing.assert_array_equal(got, want)
 
 
+@FMTS
+def test_attn_masked_largest_values(fmt):
+    """The largest bf16 in a row that earlier rows must not see: in 8 bits it
+    stands for 2^128, an infinity that would make NaN of a weight of zero."""
+    rng = np.random.default_rng(8)
+    dev = Dev(fmt, 16, 1, 1, 64, 40)
+    x = rows(rng, 1, 22, 2, 1, 64)
+    x[0, 21, 1, 0, 5] = torch.finfo(torch.bfloat16).max
+    dev.ref.store(x.double().numpy(), [0])
+    dev.upload()
+    q = rows(rng, 1, 2, 1, 64)
+    got = attend(dev, q, [20])[:, 0]
+    o, a, mag = kv8.attention(np.nan_to_num(dev.ref.read(), nan=0.0), q.double().numpy(), [20], 0)
+    assert np.all(np.abs(got - o[:, 0]) <= bound(o, a, mag, 64, 22)[:, 0])
+
+
 # ------------------------------------------------------------------ together
 
 @FMTS
@@ -474,6 +490,29 @@ def test_another_stream():
     with torch.cuda.stream(s):
         got = attend(dev, q, [699] * 2)
     np.testing.assert_array_equal(got, want)
+
+
+def test_many_heads():
+    """More tiles than a launch dimension has workgroups: the last sequence's rows
+    against the oracle."""
+    B, kvh, dh, s_max = 4200, 250, 64, 16
+    probe = ld.kv8(None, None, ld.LD_KV8_INT8, 16, B, kvh, dh, s_max)
+    codes = torch.zeros(ld.ld_kv8_code_bytes(probe), dtype=torch.uint8, device=DEV)
+    scales = torch.zeros(ld.ld_kv8_scale_bytes(probe) // 4, device=DEV)
+    kv = ld.kv8(codes, scales, ld.LD_KV8_INT8, 16, B, kvh, dh, s_max)
+    rng = np.random.default_rng(3)
+    x = rows(rng, 2, 1, 2, kvh, dh)
+    qkv = torch.zeros(B, 3 * kvh * dh, dtype=torch.bfloat16, device=DEV)
+    qkv[0, kvh * dh:], qkv[-1, kvh * dh:] = x[0].reshape(-1).to(DEV), x[1].reshape(-1).to(DEV)
+    ld.ld_kv8_store(kv, kvh, 1, 0, qkv)
+    out = torch.full((B, 1, 2 * kvh * dh), 7.0, dtype=torch.bfloat16, device=DEV)
+    ld.ld_kv8_load(kv, 0, 1, out)
+    ref = kv8.Cache(kv8.INT8, 16, 2, kvh, dh, s_max)
+    ref.store(x.double().numpy(), [0, 0])
+    want = ref.read()[..., :1, :].transpose(0, 3, 2, 1, 4).reshape(2, -1)
+    np.testing.assert_array_equal(f64(out[0]), want[:1])
+    np.testing.assert_array_equal(f64(out[-1]), want[1:])
+    assert not bool(out[1:-1].any())
 
 
 def test_offsets_past_32_bits():
