@@ -301,7 +301,8 @@ int ld_stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w,
  *           no infinities; largest Q = 448), or LD_KV8_INT8, integers
  *           -127..127 (Q = 127).
  *   block:  positions that share a scale: 16, 32, 64 or 128.
- *   d_head: 64 or 128.  s_max >= 1 positions.  n_seq, 2 n_kv_heads <= 65535.
+ *   d_head: 64 or 128.  1 <= s_max <= 2^30 positions.  n_seq, 2 n_kv_heads,
+ *           n_heads <= 65535.
  *   codes:  device, ld_kv8_code_bytes, 16-byte aligned.  With S16 = s_max
  *           rounded up to 16, sequence b's head h has at
  *           ((b n_kv_heads + h) 2) S16 d_head its keys [S16][d_head], then its

@@ -1291,8 +1291,8 @@ int check_kv8(const ld_kv8* kv, Kv8View* out) {
   if (kv->n_seq < 1 || kv->n_kv_heads < 1 || kv->s_max < 1) return fail(LD_E_SHAPE, "n_seq, n_kv_heads, s_max must be >= 1");
   if (kv->n_seq > kMaxGridYZ || kv->n_kv_heads > kMaxGridYZ / 2)
     return fail(LD_E_SHAPE, "n_seq or 2 n_kv_heads above %d", kMaxGridYZ);
-  // the tiles of 16 positions of all heads are numbered in 32 bits
-  if (kv->s_max > INT32_MAX - 512 || 2ll * kv->n_seq * kv->n_kv_heads > INT32_MAX / (kv->s_max / 16 + 3))
+  // sums of two positions and the tiles of 16 positions of all heads stay in 32 bits
+  if (kv->s_max > 1 << 30 || 2ll * kv->n_seq * kv->n_kv_heads > INT32_MAX / (kv->s_max / 16 + 3))
     return fail(LD_E_SHAPE, "n_seq n_kv_heads s_max too large");
   Kv8View v{};
   v.codes = static_cast<uint8_t*>(kv->codes);

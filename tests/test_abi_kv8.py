@@ -53,6 +53,7 @@ BAD_DESC = [(dict(format=2), INVALID), (dict(format=-1), INVALID), (dict(block=8
             (dict(d_head=96), UNSUPPORTED), (dict(d_head=256), UNSUPPORTED), (dict(n_seq=0), SHAPE),
             (dict(n_kv_heads=0), SHAPE), (dict(s_max=0), SHAPE), (dict(n_seq=65536), SHAPE),
             (dict(n_kv_heads=32768), SHAPE), (dict(s_max=2 ** 31 - 1), SHAPE),
+            (dict(n_seq=1, n_kv_heads=1, s_max=2 ** 30 + 1), SHAPE),
             (dict(n_seq=60000, n_kv_heads=30000), SHAPE)]
 
 
