@@ -23,7 +23,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kKv8Waves = 8;  // of an attention workgroup
 constexpr int kCus = 256;
 
-
 // ------------------------------------------------------------- conversions
 
 // 8 codes (two dwords) to bf16, exact: e4m3 has 4 significant bits, int8 seven.
@@ -115,11 +114,13 @@ __device__ __forceinline__ void transpose4(const uint32_t (&in)[4], uint32_t (&o
 // four lanes and meet in LDS (rows of 16 bytes, 16 more after each 8: the lanes'
 // dwords fall on different banks).
 //
-// Bound by memory.  Prompts of 8 x 2048 rows, 16 heads of 128: store 36.9 us for 201
-// MB (5.4 TB/s; units of 64 positions a wave, four times fewer waves, 44.9, and
-// loads that stay in the caches 41.2), load 30.2 us (6.7 TB/s, the codes still in the
-// memory-side cache; stores that push them out 39.9).  A new row of 32 sequences:
-// 5.9 us, its value bytes alone (16 lines a head); whole tiles read and written 6.9.
+// Bound by memory.  Prompts of 8 x 2048 rows, 16 heads of 128: store 34 to 37 us for
+// 201 MB (5.4 to 5.9 TB/s, a large copy's rate being 4.9; units of 64 positions a wave,
+// four times fewer waves, 44.9, and loads that stay in the caches 41.2), load 30 us
+// (6.7 TB/s, the codes still in the memory-side cache; stores that push them out 39.9).
+// Load of 4 x 4096 rows of 32 heads: 78 us for 403 MB (5.1 TB/s).  A new row of 32
+// sequences: 5.9 us, its value bytes alone (16 lines a head); whole tiles read and
+// written 6.9.  One row of one sequence: 3.8 us, a launch and four dependent accesses.
 template <int DH>
 struct Kv8Lanes {
   static constexpr int PT = DH / 8, U = 4 * 64 / PT, TILES = U / 16;  // a unit: U rows, TILES tiles
@@ -365,7 +366,14 @@ __global__ __launch_bounds__(256) void ld_kv8_load_k(Kv8LoadArgs a) {
 // two bf16 parts, which leave 2^-16 of it.
 //
 // Bound by the cache stream.  A wave asks for its keys and values at once (8 KB)
-// and waits; 16 waves a CU at 128 registers hold 128 KB in flight.
+// and waits; 16 waves a CU at 128 registers hold 128 KB in flight.  131072 keys of 8
+// heads of 128, 2 sequences: 537 MB in 89 us (6.0 TB/s; reading alone reaches 6.2);
+// 4096 keys of 32 heads of 8: 268 MB in 46.5 us (5.8); 16 sequences of up to 8192, 276
+// MB in 53 us (5.2: launch, tail).  A workgroup by itself takes in 36 bytes a ns, and no
+// more with 16 waves (1506 keys of 16 heads of 8 in two chunks 14.9 us against 14.5).
+// The next turn's keys asked for before this one's products (the queries then in
+// LDS): 2 to 9% faster where every chunk is long, the ragged batch 57.9 -> 72.8 us.
+// Two row tiles a workgroup: 8 rows of 8 query heads a head, 17.1 -> 21.4 us.
 template <int DH, int FMT, int NQ>
 __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8AttnArgs a) {
   constexpr int NS = DH / 64, MT = DH / 16, NW = kKv8Waves, TT = DH == 64 ? 4 : 2, LK = 4 * TT, WK = 16 * TT;
@@ -626,7 +634,7 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
 
 // W waves per (sequence, query head, new row) merge the chunks its keys fill, where
 // they are several: each every W-th, U at once so that their partial rows are all
-// in flight; then the waves' sums, in their order.  A launch of its own, about 4.5
+// in flight; then the waves' sums, in their order.  A launch of its own, 3 to 4.7
 // us of a call: the last workgroup of a row doing it instead needs device-scope
 // release and acquire, which write back and empty the XCDs' L2s (a verify step over
 // 1506 keys 15.2 -> 44 us).
