@@ -632,15 +632,16 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
   }
 }
 
-// W waves per (sequence, query head, new row) merge the chunks its keys fill, where
-// they are several: each every W-th, U at once so that their partial rows are all
-// in flight; then the waves' sums, in their order.  A launch of its own, 3 to 4.7
-// us of a call: the last workgroup of a row doing it instead needs device-scope
-// release and acquire, which write back and empty the XCDs' L2s (a verify step over
-// 1506 keys 15.2 -> 44 us).
-template <int DH, int W, int U>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void ld_attn_decode_kv8_combine(Kv8AttnArgs a) {
-  constexpr int CL = DH / 64;
+// W (four or one) waves per (sequence, query head, new row) merge the chunks its keys
+// fill, where they are several: each every W-th, U at once so that their partial
+// rows are all in flight; then the waves' sums, in their order.  Bound by two
+// dependent loads and, with many rows, by reading the partial rows.  A launch of its
+// own, 3 to 4.7 us of a call: the last workgroup of a row doing it instead needs
+// device-scope release and acquire, which write back and empty the XCDs' L2s (a
+// verify step over 1506 keys 15.2 -> 44 us).
+template <int DH, int W>
+__global__ __launch_bounds__(256) void ld_attn_decode_kv8_combine(Kv8AttnArgs a) {
+  constexpr int CL = DH / 64, U = 4;
   typedef float FRow __attribute__((ext_vector_type(CL)));
   __shared__ float ml[W][2];
   __shared__ __align__(16) FRow red[W][64];
@@ -750,6 +751,8 @@ hipError_t attn_t(const Kv8AttnArgs& a, hipStream_t s) {
   const dim3 block(64 * kKv8Waves);
   const dim3 grid = a.tiles == 1 ? dim3(a.n_chunks, a.kv.KV, a.kv.n_seq)
                                  : dim3(a.kv.KV * a.n_chunks * a.tiles, 1, a.kv.n_seq);
+  // rows kept for the merge: less LDS and, where workgroups are few, less time at the
+  // end (16 heads over 8000 keys: 11.4 us with 1, 11.7 with 8, 12.1 with 16)
   if (R == 1)
     hipLaunchKernelGGL((ld_attn_decode_kv8_k<DH, FMT, 1>), grid, block, 0, s, a);
   else if (R <= 8)
@@ -759,12 +762,13 @@ hipError_t attn_t(const Kv8AttnArgs& a, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_chunks == 1) return e;
   const int64_t rows = static_cast<int64_t>(a.kv.n_seq) * a.H * a.n_new;
-  if (a.n_chunks > 8 && rows <= 8192)
-    hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 8, 8>), dim3(rows), dim3(512), 0, s, a);
-  else if (a.n_chunks > 4)
-    hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 1, 16>), dim3((rows + 3) / 4), dim3(256), 0, s, a);
+  // four waves a row, or one where the rows fill the chip by themselves (us with one,
+  // four: 512 rows of up to 15 chunks 16.7, 14.9; 2048 20.2, 18.9; 4096 29.9, 30.0; 10240
+  // 67.0, 70.1; eight waves of eight chunks at once 15.5, 20.5, 32.7, 75.4)
+  if (rows <= 4096)
+    hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 4>), dim3(rows), dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 1, 4>), dim3((rows + 3) / 4), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 1>), dim3((rows + 3) / 4), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

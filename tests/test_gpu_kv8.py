@@ -343,6 +343,16 @@ def test_attn_long(fmt, dh, n_seq, kvh, keys):
 
 
 @FMTS
+@DHS
+def test_attn_many_rows_in_chunks(fmt, dh):
+    """More rows than the merge gives four waves each, of lengths from one chunk to
+    three and of none."""
+    dev, rng = filled(fmt, 32, 11, 4, dh, 1300, dh)
+    pos = [1300 - 8 if b % 4 == 0 else None if b % 4 == 1 else 97 * b for b in range(11)]
+    check(dev, rows(rng, 11, 8, 48, dh), pos, seq_pos=True)
+
+
+@FMTS
 def test_attn_far_scales(fmt):
     """Value blocks 2^60 apart, the largest under weights that vanish: nothing of the
     others may be lost; zero blocks with the smallest scale hold the weight."""
