@@ -793,7 +793,7 @@ int64_t attn_kv8_heads(const Kv8View& kv, int64_t H, int64_t n_new) {
 
 namespace {
 
-constexpr int64_t kKv8MinChunk = 256, kKv8OneChunk = 1024, kKv8RaggedChunk = 576, kKv8FewChunk = 320, kKv8MaxWgs = 8192;
+constexpr int64_t kKv8MinChunk = 256, kKv8ShortKeys = 1024, kKv8RaggedChunk = 576, kKv8FewChunk = 320, kKv8MaxWgs = 8192;
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -802,19 +802,23 @@ int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // over.  In a full round a CU gets its share of 6 TB/s (of twice and two and a half
 // times that where two or more row tiles read a chunk through one L2); in the last,
 // more the fewer there are, up to the 36 (int8: 28) bytes a ns that one workgroup
-// takes in on its own.  Several chunks are a second launch, 3.5 us more.  (us at n
-// chunks: 24 heads of 128 over 43825 keys 49.4 at 8, 51 to 52.5 at 10 to 96; 140 heads
-// over 3682 30.2 at 1, 32 to 34 at 3 to 14; 120 over 4321, int8, 29.2 at 2, 30 to 31 at 4
-// to 16; 24 over 1217, six rows, int8, 13.8 at 1, 12.1 at 2, 9.9 at 4; 16 of 64 of 3
-// sequences over 13181 with 40 rows 43 at 1, 34 at 4, 30.4 at 5.)
+// takes in on its own.  Several chunks are a second launch, 3.5 us more, and under 6
+// us the host is not ready sooner (16 heads over 777 keys 7.8 us at 1 chunk, 7.15 at 4
+// in a graph, but 7.7 and 8.7 called one by one).  us at n chunks: 24 heads of 128 over
+// 43825 keys 49.4 at 8, 51 to 52.5 at 10 to 96; 140 heads over 3682 30.2 at 1, 32 to 34
+// at 3 to 14; 120 over 4321, int8, 29.2 at 2, 30 to 31 at 4 to 16; 24 over 1217, six
+// rows, int8, 13.8 at 1, 12.1 at 2, 9.9 at 4; 16 over 1000, int8, 10.7 at 1, 7.5 at 4; 32
+// over 600 6.8 at 1, 7.3 at 3; 16 of 64 of 3 sequences over 13181 with 40 rows 43 at 1,
+// 34 at 4, 30.4 at 5.
 int64_t chunks_known(const Kv8AttnArgs& a, int64_t heads, int64_t keys) {
-  const int64_t most = keys <= kKv8OneChunk ? 1 : keys / kKv8MinChunk, lone = a.kv.format == LD_KV8_INT8 ? 28 : 36;
-  const int64_t twice = a.tiles > 2 ? 5 : 2 * a.tiles;  // 2 x tiles that share a reading
+  const int64_t most = div_up(keys, kKv8MinChunk), lone = a.kv.format == LD_KV8_INT8 ? 28 : 36;
+  const int64_t host = 6000, twice = a.tiles > 2 ? 5 : 2 * a.tiles;  // 2 x tiles that share a reading
   int64_t best = 1, best_cost = INT64_MAX;
   for (int64_t n = 1; n <= most && (n == 1 || heads * (n - 1) < 4 * kCus); ++n) {
     const int64_t bytes = div_up(keys, n) * 2 * a.kv.dh, wgs = heads * n, rest = wgs % kCus;
-    int64_t cost = wgs / kCus * (2 * bytes * kCus / (6000 * twice)) + (div_up(wgs, kCus) - 1) * 3000 + (n > 1 ? 3500 : 0);
+    int64_t cost = wgs / kCus * (2 * bytes * kCus / (6000 * twice)) + (div_up(wgs, kCus) - 1) * 3000;
     if (rest) cost += bytes / (lone * rest < 3000 * twice ? lone : 3000 * twice / rest);
+    if (n > 1) cost = cost + 3500 > host ? cost + 3500 : host;
     if (cost < best_cost) {
       best = n;
       best_cost = cost;
@@ -823,12 +827,13 @@ int64_t chunks_known(const Kv8AttnArgs& a, int64_t heads, int64_t keys) {
   return best;
 }
 
-// Where it does not (keys being the most a sequence can have): chunks of about 576
-// keys, so that whatever the lengths are spreads evenly; shorter ones where those
-// would be few.  (32 heads of 16 sequences of 8 to 8192 keys: 57 us, in chunks of 1024
-// 61; 8 heads of 5, up to 8235, int8: 13.4 us with 384 keys, 16.0 with 1030.)
-int64_t chunks_ragged(int64_t heads, int64_t keys) {
-  if (keys <= kKv8OneChunk) return 1;
+// Where it does not (keys being the most a sequence can have): up to 1024 as if all
+// had that many; more, chunks of about 576 keys, so that whatever the lengths are
+// spreads evenly; shorter ones where those would be few.  (32 heads of 16 sequences of
+// 8 to 8192 keys: 57 us, in chunks of 1024 61; 8 heads of 5, up to 8235, int8: 13.4 us
+// with 384 keys, 16.0 with 1030.)
+int64_t chunks_ragged(const Kv8AttnArgs& a, int64_t heads, int64_t keys) {
+  if (keys <= kKv8ShortKeys) return chunks_known(a, heads, keys);
   int64_t n = div_up(keys, kKv8RaggedChunk), few = 4 * kCus / heads;
   if (few > keys / kKv8FewChunk) few = keys / kKv8FewChunk;
   if (n < few) n = few;
@@ -848,7 +853,7 @@ hipError_t launch_attn_decode_kv8(Kv8AttnArgs a, hipStream_t s) {
   a.group = a.H / a.kv.KV;
   a.tiles = (a.group * a.n_new + 15) / 16;
   const int64_t heads = attn_kv8_heads(a.kv, a.H, a.n_new);
-  const int64_t n = a.seq_pos ? chunks_ragged(heads, keys) : chunks_known(a, heads, keys);
+  const int64_t n = a.seq_pos ? chunks_ragged(a, heads, keys) : chunks_known(a, heads, keys);
   a.chunk_keys = static_cast<int32_t>(div_up(div_up(keys, n), 64) * 64);
   a.n_chunks = static_cast<int32_t>(div_up(keys, a.chunk_keys));
   if (a.kv.dh == 128)
