@@ -351,6 +351,14 @@ __global__ __launch_bounds__(256) void ld_kv8_load_k(Kv8LoadArgs a) {
 
 // --------------------------------------------------------------- attention
 
+// Keys of a chunk of a sequence of nk: a.chunk_keys, and where lengths are the device's
+// more in a sequence that would make more than a.n_chunks of them.
+__device__ __forceinline__ int kv8_chunk_keys(const Kv8AttnArgs& a, int nk) {
+  if (!a.seq_pos) return a.chunk_keys;
+  const uint32_t n = a.n_chunks, even = ((static_cast<uint32_t>(max(nk, 0)) + n - 1) / n + 63) & ~63u;
+  return max(static_cast<int>(even), a.chunk_keys);
+}
+
 // A workgroup of eight waves takes a chunk of keys of one key/value head for 16
 // rows (of its query heads' new rows); a wave 32 keys at a time (64 for heads of
 // 64), with its own running maximum and sum; they meet once, to add up.
@@ -403,7 +411,7 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
     p = a.seq_pos[b];
     if (p < 0 || p > a.pos) p = -a.n_new;  // left out: no keys
   }
-  const int nk = p + a.n_new, k_first = chunk * a.chunk_keys;
+  const int nk = p + a.n_new, ck = kv8_chunk_keys(a, nk), k_first = chunk * ck;
   const int rows = min(R - r0, 16);
   const int64_t d = static_cast<int64_t>(a.H) * DH;
   // where row r of the head goes in the output
@@ -416,7 +424,7 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
       for (int e = tid; e < rows * DH; e += 64 * NW) out_at(r0 + e / DH)[e % DH] = static_cast<bf16>(0.f);
     return;
   }
-  const int k_end = min(k_first + a.chunk_keys, nk);
+  const int k_end = min(k_first + ck, nk);
   const int64_t head = static_cast<int64_t>(b) * c.KV + h;
   const uint8_t* kc = c.codes + head * 2 * c.s16 * DH;
   const uint8_t* vc = kc + static_cast<int64_t>(c.s16) * DH;
@@ -603,7 +611,7 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
   __syncthreads();
 
   // sum over the waves, in wave order, each scaled to the chunk's maximum
-  const bool only = nk <= a.chunk_keys;  // the sequence's one chunk: its rows are the result
+  const bool only = nk <= ck;  // the sequence's one chunk: its rows are the result
   for (int e = tid; e < rows * DH; e += 64 * NW) {
     const int i = e / DH, col = e % DH, r = r0 + i;
     float mw[NW], M = -INFINITY, L = 0.f, s = 0.f;
@@ -654,7 +662,8 @@ __global__ __launch_bounds__(256) void ld_attn_decode_kv8_combine(Kv8AttnArgs a)
   int chunks = a.n_chunks;
   if (a.seq_pos) {
     const int p = a.seq_pos[b];
-    chunks = p < 0 || p > a.pos ? 0 : (p + a.n_new + a.chunk_keys - 1) / a.chunk_keys;
+    const int nk = p + a.n_new, ck = kv8_chunk_keys(a, nk);
+    chunks = p < 0 || p > a.pos ? 0 : (nk + ck - 1) / ck;
   }
   if (chunks <= 1) return;  // written by the attention kernel
   const float* po = a.part_o + r * a.n_chunks * DH + lane * CL;
@@ -793,7 +802,8 @@ int64_t attn_kv8_heads(const Kv8View& kv, int64_t H, int64_t n_new) {
 
 namespace {
 
-constexpr int64_t kKv8MinChunk = 256, kKv8ShortKeys = 1024, kKv8RaggedChunk = 576, kKv8FewChunk = 320, kKv8MaxWgs = 8192;
+constexpr int64_t kKv8MinChunk = 256, kKv8ShortKeys = 1024, kKv8UnevenChunk = 576, kKv8FewChunk = 320,
+                  kKv8UnevenWgs = 2048;
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -827,24 +837,36 @@ int64_t chunks_known(const Kv8AttnArgs& a, int64_t heads, int64_t keys) {
   return best;
 }
 
-// Where it does not (keys being the most a sequence can have): up to 1024 as if all
-// had that many; more, chunks of about 576 keys, so that whatever the lengths are
-// spreads evenly; shorter ones where those would be few.  (32 heads of 16 sequences of
-// 8 to 8192 keys: 57 us, in chunks of 1024 61; 8 heads of 5, up to 8235, int8: 13.4 us
-// with 384 keys, 16.0 with 1030.)
-int64_t chunks_ragged(const Kv8AttnArgs& a, int64_t heads, int64_t keys) {
-  if (keys <= kKv8ShortKeys) return chunks_known(a, heads, keys);
-  int64_t n = div_up(keys, kKv8RaggedChunk), few = 4 * kCus / heads;
-  if (few > keys / kKv8FewChunk) few = keys / kKv8FewChunk;
-  if (n < few) n = few;
-  const int64_t most = div_up(kKv8MaxWgs, heads);
-  return n < most ? n : most;
+// Where it does not (keys being the most a sequence can have): for one sequence, or
+// up to 1024 keys, as many as if all had that many, of at least 256 keys.  Else chunks
+// of about 576 keys, so that
+// whatever the lengths are spreads evenly, shorter ones where those would be few (8
+// heads of 5 sequences up to 8235, int8: 13.4 us with 384 keys, 16.0 with 1030), and at
+// most 2048 workgroups, long sequences' chunks growing instead: most of a full grid
+// would find nothing to do, and each costs its start.  Us without that limit and
+// with it (1536 and 2560): 32 heads of 16 sequences of up to 8192 keys 59.3, 56.5 (60.8,
+// 57.6), all under 900 26.8, 21.4 (21.2, 21.8); 8 heads of 64 up to 4000 47.4, 44.8 (46.0,
+// 45.6); 32 of 16 with two row tiles up to 8000 69.3, 49.6 (60.8, 49.7), 16 of 64 up to
+// 2000 71.9, 38.2; 32 of 32 up to 3000, int8, 66.3, 70.
+void chunks_uneven(Kv8AttnArgs& a, int64_t heads, int64_t keys) {
+  int64_t n, least = kKv8MinChunk;
+  if (keys <= kKv8ShortKeys || a.kv.n_seq == 1) {
+    n = chunks_known(a, heads, keys);
+  } else {
+    const int64_t by_wgs = 4 * kCus / heads, by_keys = keys / kKv8FewChunk, few = by_wgs < by_keys ? by_wgs : by_keys;
+    n = div_up(keys, kKv8UnevenChunk);
+    if (n < few) n = few;
+    least = div_up(div_up(keys, n), 64) * 64;
+  }
+  const int64_t most = heads < kKv8UnevenWgs ? kKv8UnevenWgs / heads : 1;
+  a.n_chunks = static_cast<int32_t>(n < most ? n : most);
+  a.chunk_keys = static_cast<int32_t>(least);
 }
 
 }  // namespace
 
 int64_t attn_kv8_max_chunks(int64_t heads, int64_t keys) {
-  const int64_t by_keys = div_up(keys, kKv8MinChunk), by_wgs = div_up(kKv8MaxWgs, heads);
+  const int64_t by_keys = div_up(keys, kKv8MinChunk), by_wgs = div_up(kKv8UnevenWgs, heads);
   return by_keys < by_wgs ? by_keys : by_wgs;
 }
 
@@ -853,9 +875,12 @@ hipError_t launch_attn_decode_kv8(Kv8AttnArgs a, hipStream_t s) {
   a.group = a.H / a.kv.KV;
   a.tiles = (a.group * a.n_new + 15) / 16;
   const int64_t heads = attn_kv8_heads(a.kv, a.H, a.n_new);
-  const int64_t n = a.seq_pos ? chunks_ragged(a, heads, keys) : chunks_known(a, heads, keys);
-  a.chunk_keys = static_cast<int32_t>(div_up(div_up(keys, n), 64) * 64);
-  a.n_chunks = static_cast<int32_t>(div_up(keys, a.chunk_keys));
+  if (a.seq_pos) {
+    chunks_uneven(a, heads, keys);
+  } else {
+    a.chunk_keys = static_cast<int32_t>(div_up(div_up(keys, chunks_known(a, heads, keys)), 64) * 64);
+    a.n_chunks = static_cast<int32_t>(div_up(keys, a.chunk_keys));
+  }
   if (a.kv.dh == 128)
     return a.kv.format == LD_KV8_E4M3 ? attn_t<128, LD_KV8_E4M3>(a, s) : attn_t<128, LD_KV8_INT8>(a, s);
   return a.kv.format == LD_KV8_E4M3 ? attn_t<64, LD_KV8_E4M3>(a, s) : attn_t<64, LD_KV8_INT8>(a, s);

@@ -394,7 +394,7 @@ struct Kv8AttnArgs {
   void* out;       // [n_seq * n_new, H * dh]
   float* part_o;   // [n_seq][H * n_new rows of the heads in turn][n_chunks][dh]
   float* part_ml;  // [n_seq][H * n_new][n_chunks][2]: base-2 max, sum
-  int32_t H, n_new, pos, group, n_chunks, chunk_keys;  // group = H / KV
+  int32_t H, n_new, pos, group, n_chunks, chunk_keys;  // group = H / KV; chunk_keys: the least
   uint32_t tiles;  // of 16 rows a key/value head
   const int32_t* seq_pos;
   float scale;

@@ -248,8 +248,8 @@ def bound(o, a, mag, dh, keys):
     return 2.0 ** -8 * np.abs(o) + 1.01 * w[..., None] * a + 1e-38
 
 
-def attend(dev, q, pos, alibi=0, seq_pos=False, ws=None, extra=64):
-    """q bf16 [n_seq, n, H, dh]; the oracle's answer and the GPU's."""
+def attend(dev, q, pos, alibi=0, seq_pos=False, ws=None, extra=64, top=None):
+    """q bf16 [n_seq, n, H, dh]; top: the call's pos, where it is not the largest."""
     n_seq, n, H, dh = q.shape
     kvh = dev.shape[1]
     qkv = torch.full((n_seq * n, (H + 2 * kvh) * dh), 3.0, dtype=torch.bfloat16)
@@ -257,7 +257,7 @@ def attend(dev, q, pos, alibi=0, seq_pos=False, ws=None, extra=64):
     if ws is None:
         ws = torch.empty(ld.ld_attn_decode_kv8_ws_bytes(dev.kv, H, n), dtype=torch.uint8, device=DEV)
     o = torch.full((n_seq * n * H * dh + extra,), 7.0, dtype=torch.bfloat16, device=DEV)
-    top = max(p for p in pos if p is not None)
+    top = top or max(p for p in pos if p is not None)
     sp = torch.tensor([-1 if p is None else p for p in pos], dtype=torch.int32, device=DEV) if seq_pos else None
     for _ in range(2):
         before = o.clone()
@@ -268,8 +268,8 @@ def attend(dev, q, pos, alibi=0, seq_pos=False, ws=None, extra=64):
     return f64(o[:-extra]).reshape(n_seq, n, H, dh)
 
 
-def check(dev, q, pos, alibi=0, seq_pos=False):
-    got = attend(dev, q, pos, alibi, seq_pos)
+def check(dev, q, pos, alibi=0, seq_pos=False, top=None):
+    got = attend(dev, q, pos, alibi, seq_pos, top=top)
     values = np.nan_to_num(dev.ref.read(), nan=0.0)
     o, a, mag = kv8.attention(values, q.double().numpy(), pos, alibi)
     keys = max(p for p in pos if p is not None) + q.shape[1]
@@ -350,6 +350,29 @@ def test_attn_many_rows_in_chunks(fmt, dh):
     dev, rng = filled(fmt, 32, 11, 4, dh, 1300, dh)
     pos = [1300 - 8 if b % 4 == 0 else None if b % 4 == 1 else 97 * b for b in range(11)]
     check(dev, rows(rng, 11, 8, 48, dh), pos, seq_pos=True)
+
+
+@FMTS
+@pytest.mark.parametrize("n_seq,kvh,keys", [(8, 4, 3000), (16, 8, 1100)])
+def test_attn_uneven_in_a_full_grid(fmt, n_seq, kvh, keys):
+    """So many row tiles that long sequences' chunks grow (to one, in the second)
+    while short ones' stay."""
+    dev, rng = filled(fmt, 128, n_seq, kvh, 64, keys, kvh)
+    pos = [None if b == 2 else keys - 8 if b % 3 == 0 else min(100 + 97 * b, keys - 8) for b in range(n_seq)]
+    check(dev, rows(rng, n_seq, 8, 32 * kvh, 64), pos, seq_pos=True)
+
+
+@FMTS
+@DHS
+@pytest.mark.parametrize("p", [0, 255, 700, 2990])
+def test_attn_far_below_the_bound(fmt, dh, p):
+    """What a captured step does early on: pos is the most, seq_pos what there is."""
+    dev, rng = filled(fmt, 64, 1, 2, dh, 3000, p)
+    check(dev, rows(rng, 1, 1, 4, dh), [p], seq_pos=True, top=2999)
+    if p <= 1000:
+        check(dev, rows(rng, 1, 1, 4, dh), [p], seq_pos=True, top=1000)
+    dev, rng = filled(fmt, 64, 3, 2, dh, 3000, p + 1)
+    check(dev, rows(rng, 3, 2, 4, dh), [p, None, p // 2], seq_pos=True, top=2998)
 
 
 @FMTS
