@@ -377,7 +377,7 @@ __device__ __forceinline__ int kv8_chunk_keys(const Kv8AttnArgs& a, int nk) {
 // and waits; 16 waves a CU at 128 registers hold 128 KB in flight.  131072 keys of 8
 // heads of 128, 2 sequences: 537 MB in 89 us (6.0 TB/s; reading alone reaches 6.2);
 // 4096 keys of 32 heads of 8: 268 MB in 46.5 us (5.8); 16 sequences of up to 8192, 276
-// MB in 53 us (5.2: launch, tail).  A workgroup by itself takes in 36 bytes a ns, and no
+// MB in 51 us (5.4: launch, tail).  A workgroup by itself takes in 36 bytes a ns, and no
 // more with 16 waves (1506 keys of 16 heads of 8 in two chunks 14.9 us against 14.5).
 // The next turn's keys asked for before this one's products (the queries then in
 // LDS): 2 to 9% faster where every chunk is long, the ragged batch 57.9 -> 72.8 us.
@@ -771,10 +771,11 @@ hipError_t attn_t(const Kv8AttnArgs& a, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_chunks == 1) return e;
   const int64_t rows = static_cast<int64_t>(a.kv.n_seq) * a.H * a.n_new;
-  // four waves a row, or one where the rows fill the chip by themselves (us with one,
-  // four: 512 rows of up to 15 chunks 16.7, 14.9; 2048 20.2, 18.9; 4096 29.9, 30.0; 10240
-  // 67.0, 70.1; eight waves of eight chunks at once 15.5, 20.5, 32.7, 75.4)
-  if (rows <= 4096)
+  // Four waves a row, or one where there is little to share or the rows fill the chip
+  // by themselves.  Us with one, four: 16 rows of 12 chunks 11.3, 9.2; 512 of 8 17.2,
+  // 15.5; 2048 of 14 20.6, 19.6; 4096 of 8 24.0, 25.6; 512 of 4 20.5, 20.9; 2048 of 4 42.8,
+  // 43.7; 10240 of 2 53.7, 58.5.
+  if (a.n_chunks > 4 && rows <= 2048)
     hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 4>), dim3(rows), dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 1>), dim3((rows + 3) / 4), dim3(256), 0, s, a);
