@@ -355,7 +355,7 @@ __global__ __launch_bounds__(256) void ld_kv8_load_k(Kv8LoadArgs a) {
 // more in a sequence that would make more than a.n_chunks of them.
 __device__ __forceinline__ int kv8_chunk_keys(const Kv8AttnArgs& a, int nk) {
   if (!a.seq_pos) return a.chunk_keys;
-  const uint32_t n = a.n_chunks, even = ((static_cast<uint32_t>(max(nk, 0)) + n - 1) / n + 63) & ~63u;
+  const uint32_t n = a.n_chunks, even = ((static_cast<uint32_t>(nk) + n - 1) / n + 63) & ~63u;
   return max(static_cast<int>(even), a.chunk_keys);
 }
 
@@ -661,9 +661,8 @@ __global__ __launch_bounds__(256) void ld_attn_decode_kv8_combine(Kv8AttnArgs a)
   const uint32_t h = id % HN / a.n_new, j = id % a.n_new;  // (HN is a multiple of n_new)
   int chunks = a.n_chunks;
   if (a.seq_pos) {
-    const int p = a.seq_pos[b];
-    const int nk = p + a.n_new, ck = kv8_chunk_keys(a, nk);
-    chunks = p < 0 || p > a.pos ? 0 : (nk + ck - 1) / ck;
+    const int p = a.seq_pos[b], nk = p < 0 || p > a.pos ? 0 : p + a.n_new, ck = kv8_chunk_keys(a, nk);
+    chunks = (nk + ck - 1) / ck;
   }
   if (chunks <= 1) return;  // written by the attention kernel
   const float* po = a.part_o + r * a.n_chunks * DH + lane * CL;
