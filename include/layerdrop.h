@@ -489,9 +489,9 @@ int ld_kv8_load(const ld_kv8* kv, int32_t pos, int32_t n, const int32_t* seq_len
 /* ld_attn_decode over an 8-bit cache: the queries of qkv rows b n_new + j
  * (layout and seq_pos as in ld_kv8_store) at position pos + j over positions
  * 0 .. pos + j of the cache, which must already hold the new rows.  Causal,
- * with the ALiBi bias of n_heads heads when alibi = 1.  Scores, softmax and
- * sums in float32; a probability times its value scale is held to 2^-16.  The sums
- * are divided at the end: values of 2^127 / keys and more may overflow them.
+ * with the ALiBi bias of n_heads heads when alibi = 1.  Scores, softmax weights
+ * and sums in float32.  The sums are divided at the end: values of 2^127 / keys and
+ * more may overflow them.
  *   o: device bf16 [n_seq * n_new, n_heads d_head]; rows of sequences left
  *   out are zeros.  1 <= n_new <= 8.
  *   ws: device scratch of ld_attn_decode_kv8_ws_bytes(kv, n_heads, n_new)

@@ -21,6 +21,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kKv8Waves = 8;  // of an attention workgroup
+constexpr int kKv8Parts = 3;  // bf16 parts of a weight, 8 of its 24 bits each
 constexpr int kCus = 256;
 
 // ------------------------------------------------------------- conversions
@@ -370,8 +371,11 @@ __device__ __forceinline__ int kv8_chunk_keys(const Kv8AttnArgs& a, int nk) {
 // of one scale.  They are the B operand of O^T as they stand, and LK bytes of a
 // value tile's row the A operand.
 //
-// Codes are exact in bf16.  A probability, times its value scale, is split in
-// two bf16 parts, which leave 2^-16 of it.
+// Codes are exact in bf16.  A probability, times its value scale, goes in as three
+// bf16 parts, which are all of its 24 bits (parts below 2^-126, 2^-26 of the
+// smallest scale, may be lost).  Two parts leave up to 2^-17 of it: 0.5 to 0.9 us
+// less for verify steps and ragged batches of 14 and 48 us, but values that cancel
+// then lose as many bits more than the softmax does.
 //
 // Bound by the cache stream.  A wave asks for its keys and values at once (8 KB)
 // and waits; 16 waves a CU at 128 registers hold 128 KB in flight.  131072 keys of 8
@@ -565,20 +569,20 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
         for (int r = 0; r < 4; ++r)
           if (bad && f + 4 * t + r <= qpos) x[t][r] *= sv;
     }
-    bf16x8 ph[TT / 2], pl[TT / 2];
+    bf16x8 pw[kKv8Parts][TT / 2];
 #pragma unroll
     for (int t = 0; t < TT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; r += 2) {
-        const floatx2 w{x[t][r], x[t][r + 1]};
-        const bf16x2 hi = __builtin_convertvector(w, bf16x2);
-        const uint32_t hb = __builtin_bit_cast(uint32_t, hi);
-        const floatx2 rest{w[0] - __builtin_bit_cast(float, hb << 16), w[1] - __builtin_bit_cast(float, hb & 0xffff0000u)};
-        const bf16x2 lo = __builtin_convertvector(rest, bf16x2);
-        ph[t >> 1][4 * (t & 1) + r] = hi[0];
-        ph[t >> 1][4 * (t & 1) + r + 1] = hi[1];
-        pl[t >> 1][4 * (t & 1) + r] = lo[0];
-        pl[t >> 1][4 * (t & 1) + r + 1] = lo[1];
+        floatx2 w{x[t][r], x[t][r + 1]};
+#pragma unroll
+        for (int i = 0; i < kKv8Parts; ++i) {
+          const bf16x2 part = __builtin_convertvector(w, bf16x2);
+          const uint32_t pb = __builtin_bit_cast(uint32_t, part);
+          w -= floatx2{__builtin_bit_cast(float, pb << 16), __builtin_bit_cast(float, pb & 0xffff0000u)};
+          pw[i][t >> 1][4 * (t & 1) + r] = part[0];
+          pw[i][t >> 1][4 * (t & 1) + r + 1] = part[1];
+        }
       }
     if (k0 + WK > nk) {  // codes behind the last key may be anything, NaN too
 #pragma unroll
@@ -594,8 +598,9 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
 #pragma unroll
       for (int u = 0; u < TT / 2; ++u) {
         const bf16x8 v8 = codes_to_bf16<FMT>(vr[i][2 * u], vr[i][2 * u + 1], sv1);
-        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, ph[u], o[i], 0, 0, 0);
-        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, pl[u], o[i], 0, 0, 0);
+#pragma unroll
+        for (int part = 0; part < kKv8Parts; ++part)
+          o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, pw[part][u], o[i], 0, 0, 0);
       }
     }
   }
