@@ -495,7 +495,8 @@ int ld_kv8_load(const ld_kv8* kv, int32_t pos, int32_t n, const int32_t* seq_len
  *   o: device bf16 [n_seq * n_new, n_heads d_head]; rows of sequences left
  *   out are zeros.  1 <= n_new <= 8.
  *   ws: device scratch of ld_attn_decode_kv8_ws_bytes(kv, n_heads, n_new)
- *   bytes (enough for every pos; 0 on invalid arguments), 16-byte aligned. */
+ *   bytes (enough for every pos and for fewer new rows; 0 on invalid arguments),
+ *   16-byte aligned. */
 size_t ld_attn_decode_kv8_ws_bytes(const ld_kv8* kv, int32_t n_heads, int32_t n_new);
 int ld_attn_decode_kv8(const ld_kv8* kv, int32_t n_heads, int32_t alibi, int32_t pos, const int32_t* seq_pos,
                        int32_t n_new, const void* qkv, void* o, void* ws, size_t ws_bytes, void* stream);

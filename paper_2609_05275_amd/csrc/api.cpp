@@ -1341,6 +1341,11 @@ size_t kv8_part_rows(const Kv8View& v, int64_t n_heads, int64_t n_new) {
   return static_cast<size_t>(v.n_seq) * n_heads * n_new * attn_kv8_max_chunks(attn_kv8_heads(v, n_heads, n_new), v.s16);
 }
 
+size_t kv8_attn_bytes(const Kv8View& v, int64_t n_heads, int64_t n_new) {
+  const size_t rows = kv8_part_rows(v, n_heads, n_new);
+  return up(4 * rows * v.dh) + up(4 * rows * 2);
+}
+
 // Attention of qkv rows b n_new + j at positions pos + j (or seq_pos[b] + j) over an
 // 8-bit cache; part_o and part_ml hold kv8_part_rows.
 int run_kv8_attn(const Kv8View& kv, const void* qkv, void* o, float* part_o, float* part_ml, int32_t n_heads,
@@ -2310,8 +2315,10 @@ int ld_kv8_load(const ld_kv8* kv, int32_t pos, int32_t n, const int32_t* seq_len
 size_t ld_attn_decode_kv8_ws_bytes(const ld_kv8* kv, int32_t n_heads, int32_t n_new) {
   Kv8View v;
   if (check_kv8(kv, &v) || check_kv8_heads(kv, n_heads) || n_new < 1 || n_new > kDecMaxRows) return 0;
-  const size_t rows = kv8_part_rows(v, n_heads, n_new);
-  return up(4 * rows * v.dh) + up(4 * rows * 2);
+  // fewer rows may take more: in fewer row tiles there is room for more chunks
+  size_t most = 0;
+  for (int32_t n = 1; n <= n_new; ++n) most = std::max(most, kv8_attn_bytes(v, n_heads, n));
+  return most;
 }
 
 int ld_attn_decode_kv8(const ld_kv8* kv, int32_t n_heads, int32_t alibi, int32_t pos, const int32_t* seq_pos,
@@ -2324,7 +2331,7 @@ int ld_attn_decode_kv8(const ld_kv8* kv, int32_t n_heads, int32_t alibi, int32_t
   if (int rc = check_kv8_rows(kv, n_heads, n_new, pos, qkv, seq_pos)) return rc;
   if (!o || !ws) return fail(LD_E_INVALID, "NULL pointer");
   if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(LD_E_INVALID, "ws must be 16-byte aligned");
-  const size_t need = ld_attn_decode_kv8_ws_bytes(kv, n_heads, n_new);
+  const size_t need = kv8_attn_bytes(v, n_heads, n_new);
   if (ws_bytes < need) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
   float* part_o = static_cast<float*>(ws);
   float* part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + up(4 * kv8_part_rows(v, n_heads, n_new) * v.dh));
