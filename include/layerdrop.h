@@ -274,7 +274,7 @@ int ld_stack_eval(const ld_config* cfg, int32_t n_layers, const ld_weights* w, c
                   const float* r_eval, void* x, void* const* kv, int32_t s_max, void* ws,
                   size_t ws_bytes, void* stream);
 
-/* Bytes of scratch ld_stack_decode needs for n_new rows per sequence and
+/* Bytes of scratch ld_stack_decode needs for n_new rows per sequence or fewer and
  * caches of s_max positions (0 on invalid arguments). */
 size_t ld_decode_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max);
 
@@ -332,8 +332,8 @@ typedef struct {
 int ld_stack_eval_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
                       const float* r_eval, void* x, const ld_kv8* kv, void* ws, size_t ws_bytes, void* stream);
 
-/* Bytes of scratch ld_stack_decode_kv8 needs for n_new rows per sequence and
- * caches of at most s_max positions (0 on invalid arguments). */
+/* Bytes of scratch ld_stack_decode_kv8 needs for n_new rows per sequence or fewer
+ * and caches of at most s_max positions (0 on invalid arguments). */
 size_t ld_decode_kv8_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max);
 
 /* ld_stack_decode over 8-bit caches: each active layer writes the new rows'

@@ -1275,6 +1275,16 @@ DecLayout dec_layout(const Dims& D, int64_t n_new, size_t pc) {
   return L;
 }
 
+// Scratch that holds a step of n_new rows and every one of fewer: those of at most
+// kSkinnyMaxM rows in all may need the split-K sums that more do not, and the
+// attention more partial rows.  part_rows: of a number of new rows.
+template <class PartRows>
+size_t dec_bytes(const Dims& D, int32_t n_new, PartRows part_rows) {
+  size_t most = 0;
+  for (int32_t n = 1; n <= n_new; ++n) most = std::max(most, dec_layout(D, n, part_rows(n)).total);
+  return most;
+}
+
 // Where a qkv projection's keys/values also go (see SkinnyArgs).
 struct KvOut {
   void* kv;
@@ -1802,7 +1812,7 @@ int ld_stack_eval_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights* 
 size_t ld_decode_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max) {
   Dims D;
   if (check_cfg(cfg, &D) || n_new < 1 || n_new > kDecMaxRows || s_max < 1) return 0;
-  return dec_layout(D, n_new, dec_part_rows(D, s_max)).total;
+  return dec_bytes(D, n_new, [&](int32_t) { return dec_part_rows(D, s_max); });
 }
 
 size_t ld_decode_kv8_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max) {
@@ -1812,7 +1822,7 @@ size_t ld_decode_kv8_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max
                   s_max, nullptr, nullptr};
   Kv8View v;
   if (check_kv8(&kv, &v)) return 0;
-  return dec_layout(D, n_new, kv8_part_rows(v, D.H, n_new)).total;
+  return dec_bytes(D, n_new, [&](int32_t n) { return kv8_part_rows(v, D.H, n); });
 }
 
 }  // extern "C"

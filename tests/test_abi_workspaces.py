@@ -17,3 +17,12 @@ def grows(sizes):
 def test_attention_of_fewer_rows(n_seq, kv_heads, heads, s_max):
     kv = desc(n_seq=n_seq, n_kv_heads=kv_heads, s_max=s_max)
     grows([ld.ld_attn_decode_kv8_ws_bytes(kv, heads, n) for n in range(1, 9)])
+
+
+@pytest.mark.parametrize("batch", [1, 2, 9, 17, 33, 64])        # 64 rows are passed at different n_new
+@pytest.mark.parametrize("d,heads,f", [(512, 8, 1408), (1024, 16, 2816), (2560, 20, 6912), (4096, 32, 11008)])
+def test_decoding_steps_of_fewer_rows(batch, d, heads, f):
+    cfg = ld.config(batch, 128, d, heads, f)
+    for s_max in (64, 2048, 100000):
+        grows([ld.ld_decode_ws_bytes(cfg, n, s_max) for n in range(1, 9)])
+        grows([ld.ld_decode_kv8_ws_bytes(cfg, n, s_max) for n in range(1, 9)])
