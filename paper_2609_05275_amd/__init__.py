@@ -521,13 +521,16 @@ def ld_attn_decode_kv8(kv, n_heads, pos, n_new, qkv, o, ws, seq_pos=None, alibi=
 
 
 def _kv8_array(kv, n):
-    """Descriptors of n layers; None (an inactive layer's) as an empty one."""
+    """Descriptors of n layers; None (an inactive layer's) as an empty one.  And
+    the device that the other arguments have to be on (_kv8_device)."""
     if len(kv) != n:
         raise ValueError(f"{n} layers of weights, {len(kv)} of caches")
+    device = None
     for k in kv:
         if k is not None:
-            _kv8_device(k)
-    return (ld_kv8 * n)(*[k if k is not None else ld_kv8() for k in kv])
+            d = _kv8_device(k)
+            device = d if device is None else device
+    return (ld_kv8 * n)(*[k if k is not None else ld_kv8() for k in kv]), device
 
 
 def ld_stack_eval_kv8(cfg, ws_list, x, ws, kv, active=None, r_eval=None, stream=None):
@@ -535,9 +538,10 @@ def ld_stack_eval_kv8(cfg, ws_list, x, ws, kv, active=None, r_eval=None, stream=
     allowed for inactive layers)."""
     L = len(ws_list)
     wa = (ld_weights * L)(*[weights(w) for w in ws_list])
-    act, rr, kk = _u8_array(active, L), _f32_array(r_eval, L), _kv8_array(kv, L)
-    _check(_lib.ld_stack_eval_kv8(C.byref(cfg), L, wa, act, rr, _ptr(x), kk, _ptr(ws),
-                                  ws.numel() * ws.element_size(), _stream(stream)))
+    act, rr, (kk, dev) = _u8_array(active, L), _f32_array(r_eval, L), _kv8_array(kv, L)
+    px = _kv8_ptr(x, "x", dev, torch.bfloat16, cfg.batch * cfg.seq * cfg.d_model)
+    _check(_lib.ld_stack_eval_kv8(C.byref(cfg), L, wa, act, rr, px, kk, _kv8_ptr(ws, "ws", dev),
+                                  ws.numel() * ws.element_size(), _stream(stream, dev)))
 
 
 def ld_decode_kv8_ws_bytes(cfg, n_new, s_max):
@@ -549,12 +553,12 @@ def ld_stack_decode_kv8(cfg, ws_list, x, kv, pos, n_new, ws, seq_pos=None, activ
     """ld_stack_decode over 8-bit caches; seq_pos: int32 [batch] positions on
     the device (at most pos), where they differ or the call is captured."""
     L = len(ws_list)
-    _need(x, "x", torch.bfloat16, cfg.batch * n_new * cfg.d_model)
-    _need(seq_pos, "seq_pos", torch.int32, cfg.batch)
     wa = (ld_weights * L)(*[weights(w) for w in ws_list])
-    act, rr, kk = _u8_array(active, L), _f32_array(r_eval, L), _kv8_array(kv, L)
-    _check(_lib.ld_stack_decode_kv8(C.byref(cfg), L, wa, act, rr, _ptr(x), kk, pos, _ptr(seq_pos, "seq_pos"),
-                                    n_new, _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+    act, rr, (kk, dev) = _u8_array(active, L), _f32_array(r_eval, L), _kv8_array(kv, L)
+    px = _kv8_ptr(x, "x", dev, torch.bfloat16, cfg.batch * n_new * cfg.d_model)
+    _check(_lib.ld_stack_decode_kv8(C.byref(cfg), L, wa, act, rr, px, kk, pos,
+                                    _kv8_ptr(seq_pos, "seq_pos", dev, torch.int32, cfg.batch), n_new,
+                                    _kv8_ptr(ws, "ws", dev), ws.numel() * ws.element_size(), _stream(stream, dev)))
 
 
 def ld_rmsnorm_fwd(x, g, y, rstd, eps=1e-5, stream=None):
