@@ -1373,11 +1373,17 @@ int run_kv8_attn(const Kv8View& kv, const void* qkv, void* o, float* part_o, flo
   a.seq_pos = seq_pos;
   a.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(kv.dh)));
   a.alibi = alibi;
-  ProfScope ps("ld_attn_decode_kv8_k", s);
-  const hipError_t e = launch_attn_decode_kv8(a, s);
-  if (e != hipSuccess) return fail(LD_E_HIP, "attn decode kv8: %s", hipGetErrorString(e));
+  plan_attn_decode_kv8(a);
   const double keys = static_cast<double>(pos) + n_new, rows = static_cast<double>(kv.n_seq) * n_new * n_heads * kv.dh;
+  ProfScope ps("ld_attn_decode_kv8_k", s);
+  hipError_t e = launch_attn_decode_kv8(a, s);
+  if (e != hipSuccess) return fail(LD_E_HIP, "attn decode kv8: %s", hipGetErrorString(e));
   ps.end(4.0 * rows * keys, 2.0 * kv.n_seq * keys * kv.KV * kv.dh + 4.0 * rows);
+  if (a.n_chunks == 1) return LD_OK;
+  ProfScope pc("ld_attn_decode_kv8_combine", s);
+  if ((e = launch_attn_decode_kv8_combine(a, s)) != hipSuccess)
+    return fail(LD_E_HIP, "attn decode kv8 combine: %s", hipGetErrorString(e));
+  pc.end(0, 4.0 * rows / kv.dh * (kv.dh + 2) * a.n_chunks + 2.0 * rows);
   return LD_OK;
 }
 

@@ -772,8 +772,11 @@ hipError_t attn_t(const Kv8AttnArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((ld_attn_decode_kv8_k<DH, FMT, 8>), grid, block, 0, s, a);
   else
     hipLaunchKernelGGL((ld_attn_decode_kv8_k<DH, FMT, 16>), grid, block, 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.n_chunks == 1) return e;
+  return hipGetLastError();
+}
+
+template <int DH>
+hipError_t combine_t(const Kv8AttnArgs& a, hipStream_t s) {
   const int64_t rows = static_cast<int64_t>(a.kv.n_seq) * a.H * a.n_new;
   // Four waves a row, or one where there is little to share or the rows fill the chip
   // by themselves.  Us with one, four: 16 rows of 12 chunks 11.3, 9.2; 512 of 8 17.2,
@@ -875,7 +878,7 @@ int64_t attn_kv8_max_chunks(int64_t heads, int64_t keys) {
   return by_keys < by_wgs ? by_keys : by_wgs;
 }
 
-hipError_t launch_attn_decode_kv8(Kv8AttnArgs a, hipStream_t s) {
+void plan_attn_decode_kv8(Kv8AttnArgs& a) {
   const int64_t keys = static_cast<int64_t>(a.pos) + a.n_new;
   a.group = a.H / a.kv.KV;
   a.tiles = (a.group * a.n_new + 15) / 16;
@@ -886,9 +889,16 @@ hipError_t launch_attn_decode_kv8(Kv8AttnArgs a, hipStream_t s) {
     a.chunk_keys = static_cast<int32_t>(div_up(div_up(keys, chunks_known(a, heads, keys)), 64) * 64);
     a.n_chunks = static_cast<int32_t>(div_up(keys, a.chunk_keys));
   }
+}
+
+hipError_t launch_attn_decode_kv8(const Kv8AttnArgs& a, hipStream_t s) {
   if (a.kv.dh == 128)
     return a.kv.format == LD_KV8_E4M3 ? attn_t<128, LD_KV8_E4M3>(a, s) : attn_t<128, LD_KV8_INT8>(a, s);
   return a.kv.format == LD_KV8_E4M3 ? attn_t<64, LD_KV8_E4M3>(a, s) : attn_t<64, LD_KV8_INT8>(a, s);
+}
+
+hipError_t launch_attn_decode_kv8_combine(const Kv8AttnArgs& a, hipStream_t s) {
+  return a.kv.dh == 128 ? combine_t<128>(a, s) : combine_t<64>(a, s);
 }
 
 }  // namespace ld

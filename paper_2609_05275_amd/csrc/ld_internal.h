@@ -386,7 +386,7 @@ struct Kv8LoadArgs {
 };
 
 // Queries of rows b n_new + j of qkv over positions 0 .. p + j, p = pos or
-// seq_pos[b].  n_chunks and chunk_keys are the launch's choice.
+// seq_pos[b].  n_chunks and chunk_keys are plan_attn_decode_kv8's choice.
 struct Kv8AttnArgs {
   Kv8View kv;
   const void* qkv;
@@ -436,7 +436,10 @@ hipError_t launch_kv8_load(const Kv8LoadArgs& a, hipStream_t s);
 // grows with keys).
 int64_t attn_kv8_heads(const Kv8View& kv, int64_t H, int64_t n_new);
 int64_t attn_kv8_max_chunks(int64_t heads, int64_t keys);
-hipError_t launch_attn_decode_kv8(Kv8AttnArgs a, hipStream_t s);
+// Fills in group, tiles and the chunks; the second launch is for several chunks.
+void plan_attn_decode_kv8(Kv8AttnArgs& a);
+hipError_t launch_attn_decode_kv8(const Kv8AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_decode_kv8_combine(const Kv8AttnArgs& a, hipStream_t s);
 hipError_t launch_gather(int dtype, const RowsArgs& a, hipStream_t s);
 // n elements between bf16 and float32 (to_f32: bf16 -> float32, else
 // float32 -> bf16 with round to nearest even); n % 8 == 0.
