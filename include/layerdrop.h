@@ -536,7 +536,8 @@ int ld_attn_bwd_noalloc(int32_t dtype, int32_t n_seq, int32_t seq, int32_t n_hea
  * Per-kernel timing with HIP events recorded on the launch stream around
  * every launch of the named kernel (its __global__ name, e.g.
  * "ld_gemm_bf16_nt"), with the launch's algorithmic FLOPs and HBM bytes
- * computed from the kept counts.  Process-wide, not thread-safe; meant for
+ * computed from the kept counts (0 where they depend on positions or lengths in
+ * device memory, seq_pos and seq_len).  Process-wide, not thread-safe; meant for
  * benchmarks.  At most 1 << 16 launches are recorded. */
 int ld_prof_start(const char* kernel_name);
 int ld_prof_stop(void);

@@ -475,7 +475,7 @@ int run_kv8_store(const Kv8View& kv, const void* qkv, int32_t n_heads, int32_t n
   ProfScope ps("ld_kv8_store_k", s);
   const hipError_t e = launch_kv8_store(a, s);
   if (e != hipSuccess) return fail(LD_E_HIP, "kv8 store: %s", hipGetErrorString(e));
-  ps.end(0, 6.0 * kv.n_seq * n * kv.KV * kv.dh);
+  ps.end(0, seq_pos ? 0.0 : 6.0 * kv.n_seq * n * kv.KV * kv.dh);  // 0: only the device knows
   return LD_OK;
 }
 
@@ -1375,15 +1375,16 @@ int run_kv8_attn(const Kv8View& kv, const void* qkv, void* o, float* part_o, flo
   a.alibi = alibi;
   plan_attn_decode_kv8(a);
   const double keys = static_cast<double>(pos) + n_new, rows = static_cast<double>(kv.n_seq) * n_new * n_heads * kv.dh;
+  const double known = seq_pos ? 0.0 : 1.0;
   ProfScope ps("ld_attn_decode_kv8_k", s);
   hipError_t e = launch_attn_decode_kv8(a, s);
   if (e != hipSuccess) return fail(LD_E_HIP, "attn decode kv8: %s", hipGetErrorString(e));
-  ps.end(4.0 * rows * keys, 2.0 * kv.n_seq * keys * kv.KV * kv.dh + 4.0 * rows);
+  ps.end(known * 4.0 * rows * keys, known * (2.0 * kv.n_seq * keys * kv.KV * kv.dh + 4.0 * rows));
   if (a.n_chunks == 1) return LD_OK;
   ProfScope pc("ld_attn_decode_kv8_combine", s);
   if ((e = launch_attn_decode_kv8_combine(a, s)) != hipSuccess)
     return fail(LD_E_HIP, "attn decode kv8 combine: %s", hipGetErrorString(e));
-  pc.end(0, 4.0 * rows / kv.dh * (kv.dh + 2) * a.n_chunks + 2.0 * rows);
+  pc.end(0, known * (4.0 * rows / kv.dh * (kv.dh + 2) * a.n_chunks + 2.0 * rows));
   return LD_OK;
 }
 
@@ -2324,7 +2325,7 @@ int ld_kv8_load(const ld_kv8* kv, int32_t pos, int32_t n, const int32_t* seq_len
   ProfScope ps("ld_kv8_load_k", as_stream(stream));
   hipError_t e = launch_kv8_load(a, as_stream(stream));
   if (e != hipSuccess) return fail(LD_E_HIP, "kv8 load: %s", hipGetErrorString(e));
-  ps.end(0, 6.0 * kv->n_seq * n * kv->n_kv_heads * kv->d_head);
+  ps.end(0, seq_len ? 0.0 : 6.0 * kv->n_seq * n * kv->n_kv_heads * kv->d_head);
   return LD_OK;
 }
 
