@@ -343,7 +343,8 @@ size_t ld_decode_kv8_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max
  * (see ld_kv8_store); the launches do not depend on its values, so a captured
  * graph of this call decodes on as the caller advances them.  A sequence left out
  * (seq_pos outside [0, pos]) writes no cache, and its rows of x are what the
- * layers make of them without attention. */
+ * layers make of them without attention.  Drafts and rejected rows leave their mark
+ * on the caches (see ld_kv8_store). */
 int ld_stack_decode_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
                         const float* r_eval, void* x, const ld_kv8* kv, int32_t pos, const int32_t* seq_pos,
                         int32_t n_new, void* ws, size_t ws_bytes, void* stream);
@@ -472,7 +473,13 @@ size_t ld_kv8_scale_bytes(const ld_kv8* kv);
  * A new code is x / scale rounded to nearest, ties to even.  Earlier positions
  * of the first block must have been written (or be zeros, scale and codes);
  * later positions of the last block are no longer valid.  n_new >= 1,
- * pos + n_new <= s_max. */
+ * pos + n_new <= s_max.
+ * Rows that are taken back by storing others at their positions (a draft's, a
+ * verify step's rejected ones) leave what they did to the block they went into: a
+ * scale they raised stays raised, earlier codes stay rounded to it, and a NaN
+ * stays, until the block's first position is written again.  Speculative decoding
+ * over this cache is therefore not bit for bit decoding without drafts, as it is
+ * over the bf16 one.  Putting back the block's codes and scale undoes it. */
 int ld_kv8_store(const ld_kv8* kv, int32_t n_heads, int32_t n_new, int32_t pos, const int32_t* seq_pos,
                  const void* qkv, void* stream);
 
