@@ -373,19 +373,22 @@ __device__ __forceinline__ int kv8_chunk_keys(const Kv8AttnArgs& a, int nk) {
 //
 // Codes are exact in bf16.  A probability, times its value scale, goes in as three
 // bf16 parts, which are all of its 24 bits (parts below 2^-126, 2^-26 of the
-// smallest scale, may be lost).  Two parts leave up to 2^-17 of it: 0.5 to 0.9 us
-// less for verify steps and ragged batches of 14 and 48 us, but values that cancel
-// then lose as many bits more than the softmax does.
+// smallest scale, may be lost).  Two parts take 0.1 to 1.0 us less (a verify step
+// 14.6 us against 15.2, the ragged batch below 47.1 against 48.0, 131072 keys 94.4
+// against 94.9), but leave up to 2^-17 of it: seven bits of values that cancel.
 //
 // Bound by the cache stream.  A wave asks for its keys and values at once (8 KB)
 // and waits; 16 waves a CU at 128 registers hold 128 KB in flight.  131072 keys of 8
-// heads of 128, 2 sequences: 537 MB in 89 us (6.0 TB/s; reading alone reaches 6.2);
-// 4096 keys of 32 heads of 8: 268 MB in 46.5 us (5.8); 16 sequences of up to 8192, 276
-// MB in 51 us (5.4: launch, tail).  A workgroup by itself takes in 36 bytes a ns, and no
-// more with 16 waves (1506 keys of 16 heads of 8 in two chunks 14.9 us against 14.5).
-// The next turn's keys asked for before this one's products (the queries then in
-// LDS): 2 to 9% faster where every chunk is long, the ragged batch 57.9 -> 72.8 us.
-// Two row tiles a workgroup: 8 rows of 8 query heads a head, 17.1 -> 21.4 us.
+// heads of 128, 2 sequences: 537 MB in 91 us (5.9 TB/s; reading alone reaches 6.2);
+// 4096 keys of 32 heads of 8: 268 MB in 46.9 us (5.7); 16 sequences of up to 8192, 276
+// MB in 51.6 us (5.3: launch, tail).  Short chunks are start and end: 256 workgroups of
+// 64, 256, 512 and 753 keys (six rows, int8) 5.3, 7.8, 10.0 and 12.8 us in a graph, so
+// that each 256 keys more cost 2.3 to 2.8 us (7.3 to 6.0 TB/s, the cache partly in the
+// memory-side cache) after 5.3 for the first.  Tried, with weights in two parts: 16
+// waves a workgroup, 1506 keys of 16 heads of 8 in two chunks 14.5 -> 14.9 us; the next
+// turn's keys asked for before this one's products (the queries then in LDS), 2 to 9%
+// faster where every chunk is long, the ragged batch 57.9 -> 72.8; two row tiles a
+// workgroup, 8 rows of 8 query heads a head 17.1 -> 21.4.
 template <int DH, int FMT, int NQ>
 __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8AttnArgs a) {
   constexpr int NS = DH / 64, MT = DH / 16, NW = kKv8Waves, TT = DH == 64 ? 4 : 2, LK = 4 * TT, WK = 16 * TT;
@@ -649,7 +652,8 @@ __global__ __launch_bounds__(64 * kKv8Waves, 4) void ld_attn_decode_kv8_k(Kv8Att
 // fill, where they are several: each every W-th, U at once so that their partial
 // rows are all in flight; then the waves' sums, in their order.  Bound by two
 // dependent loads and, with many rows, by reading the partial rows.  A launch of its
-// own, 3 to 4.7 us of a call: the last workgroup of a row doing it instead needs
+// own, 2.5 to 3.1 us of a call in a graph (with and without it: 15.2 and 12.8, 93.5 and
+// 91.0, 57.0 and 54.0); the last workgroup of a row doing it instead needs
 // device-scope release and acquire, which write back and empty the XCDs' L2s (a
 // verify step over 1506 keys 15.2 -> 44 us).
 template <int DH, int W>
@@ -765,7 +769,7 @@ hipError_t attn_t(const Kv8AttnArgs& a, hipStream_t s) {
   const dim3 grid = a.tiles == 1 ? dim3(a.n_chunks, a.kv.KV, a.kv.n_seq)
                                  : dim3(a.kv.KV * a.n_chunks * a.tiles, 1, a.kv.n_seq);
   // rows kept for the merge: less LDS and, where workgroups are few, less time at the
-  // end (16 heads over 8000 keys: 11.4 us with 1, 11.7 with 8, 12.1 with 16)
+  // end (16 heads over 8000 keys: 11.3 us with 1, 11.5 with 8, 12.1 with 16)
   if (R == 1)
     hipLaunchKernelGGL((ld_attn_decode_kv8_k<DH, FMT, 1>), grid, block, 0, s, a);
   else if (R <= 8)
@@ -779,9 +783,9 @@ template <int DH>
 hipError_t combine_t(const Kv8AttnArgs& a, hipStream_t s) {
   const int64_t rows = static_cast<int64_t>(a.kv.n_seq) * a.H * a.n_new;
   // Four waves a row, or one where there is little to share or the rows fill the chip
-  // by themselves.  Us with one, four: 16 rows of 12 chunks 11.3, 9.2; 512 of 8 17.2,
-  // 15.5; 2048 of 14 20.6, 19.6; 4096 of 8 24.0, 25.6; 512 of 4 20.5, 20.9; 2048 of 4 42.8,
-  // 43.7; 10240 of 2 53.7, 58.5.
+  // by themselves.  Us of a call with one, four: 16 rows of 12 chunks 9.6, 8.4; 512 of 8
+  // 14.9, 14.2; 2048 of 14 34.4, 33.6; 4096 of 8 39.8, 39.8; 512 of 4 17.3, 17.4; 2048 of 4
+  // 16.2, 16.6; 10240 of 2 56.5, 58.9.
   if (a.n_chunks > 4 && rows <= 2048)
     hipLaunchKernelGGL((ld_attn_decode_kv8_combine<DH, 4>), dim3(rows), dim3(256), 0, s, a);
   else
@@ -820,14 +824,15 @@ int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // over.  In a full round a CU gets its share of 6 TB/s (of twice and two and a half
 // times that where two or more row tiles read a chunk through one L2); in the last,
 // more the fewer there are, up to the 36 (int8: 28) bytes a ns that one workgroup
-// takes in on its own.  Several chunks are a second launch, 3.5 us more, and under 6
-// us the host is not ready sooner (16 heads over 777 keys 7.8 us at 1 chunk, 7.15 at 4
-// in a graph, but 7.7 and 8.7 called one by one).  us at n chunks: 24 heads of 128 over
-// 43825 keys 49.4 at 8, 51 to 52.5 at 10 to 96; 140 heads over 3682 30.2 at 1, 32 to 34
-// at 3 to 14; 120 over 4321, int8, 29.2 at 2, 30 to 31 at 4 to 16; 24 over 1217, six
-// rows, int8, 13.8 at 1, 12.1 at 2, 9.9 at 4; 16 over 1000, int8, 10.7 at 1, 7.5 at 4; 32
-// over 600 6.8 at 1, 7.3 at 3; 16 of 64 of 3 sequences over 13181 with 40 rows 43 at 1,
-// 34 at 4, 30.4 at 5.
+// takes in on its own.  Several chunks are a second launch, counted as 3.5 us, and as
+// no less than 6 us together with the first, the host's time for two.  That floor
+// keeps one chunk where a call's own time is all there is to gain (16 heads over
+// 777 keys 8.1 us at 1 and at 4 chunks called one by one, but 8.3 and 7.6 in a graph).
+// us at n chunks, in a graph: 24 heads of 128 over 43825 keys 48.8 at 8, 50 to 56 at 10
+// to 96; 140 heads over 3682 30.3 at 1, 32 at 3 to 14; 120 over 4321, int8, 28.6 at 2, 30
+// to 31 at 4 to 16; 24 over 1217, six rows, int8, 14.3 at 1, 11.5 at 2, 9.5 at 4; 16 over
+// 1000, int8, 11.3 at 1, 8.0 at 4; 32 over 600 7.25 at 1, 7.7 at 3; 16 of 64 of 3
+// sequences over 13181 with 40 rows 48 at 1, 36.5 at 4, 32.3 at 5.
 int64_t chunks_known(const Kv8AttnArgs& a, int64_t heads, int64_t keys) {
   const int64_t most = div_up(keys, kKv8MinChunk), lone = a.kv.format == LD_KV8_INT8 ? 28 : 36;
   const int64_t host = 6000, twice = a.tiles > 2 ? 5 : 2 * a.tiles;  // 2 x tiles that share a reading
@@ -849,13 +854,14 @@ int64_t chunks_known(const Kv8AttnArgs& a, int64_t heads, int64_t keys) {
 // up to 1024 keys, as many as if all had that many, of at least 256 keys.  Else chunks
 // of about 576 keys, so that
 // whatever the lengths are spreads evenly, shorter ones where those would be few (8
-// heads of 5 sequences up to 8235, int8: 13.4 us with 384 keys, 16.0 with 1030), and at
+// heads of 5 sequences up to 8235, int8: 13.2 us with 384 keys, 15.7 with 1088), and at
 // most 2048 workgroups, long sequences' chunks growing instead: most of a full grid
 // would find nothing to do, and each costs its start.  Us without that limit and
-// with it (1536 and 2560): 32 heads of 16 sequences of up to 8192 keys 59.3, 56.5 (60.8,
-// 57.6), all under 900 26.8, 21.4 (21.2, 21.8); 8 heads of 64 up to 4000 47.4, 44.8 (46.0,
-// 45.6); 32 of 16 with two row tiles up to 8000 69.3, 49.6 (60.8, 49.7), 16 of 64 up to
-// 2000 71.9, 38.2; 32 of 32 up to 3000, int8, 66.3, 70.
+// with it (1536 and 2560): 32 heads of 16 sequences of up to 8192 keys 58.9, 55.6 (60.9,
+// 57.6), all under 900 22.8, 19.2 (15.4, 17.9); 8 heads of 64 up to 4000 47.0, 43.9 (44.3,
+// 44.3); with 32 rows a head (two tiles) 32 of 16 up to 8000 82.6, 55.2 (62.4, 54.6), 16
+// of 64 up to 2000 105, 71.1 (71.1, 71.1); 32 of 32 up to 3000, int8, 67.9, 70.6, the one
+// that loses.
 void chunks_uneven(Kv8AttnArgs& a, int64_t heads, int64_t keys) {
   int64_t n, least = kKv8MinChunk;
   if (keys <= kKv8ShortKeys || a.kv.n_seq == 1) {
