@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "ld_internal.h"
+#include "ld_kv8.h"
 
 using namespace ld;
 

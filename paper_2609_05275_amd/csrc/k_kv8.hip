@@ -1,12 +1,12 @@
 // Kernels of the 8-bit key/value cache: quantising writer, reader, and the
 // attention of a few new rows per sequence over it.  Layout and the meaning of
-// codes and scales: Kv8View in ld_internal.h, ld_kv8 in layerdrop.h.
+// codes and scales: Kv8View in ld_kv8.h, ld_kv8 in layerdrop.h.
 //
 // Scales are powers of two, so dividing by one and multiplying with it are
 // exact: a code is one rounding of its value, a value read back is the code's
 // in bf16 without another, and raising a block's scale rounds old codes by a
 // whole number of bits.
-#include "ld_internal.h"
+#include "ld_kv8.h"
 
 namespace ld {
 namespace {
