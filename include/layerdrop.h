@@ -349,6 +349,90 @@ int ld_stack_decode_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights
                         const float* r_eval, void* x, const ld_kv8* kv, int32_t pos, const int32_t* seq_pos,
                         int32_t n_new, void* ws, size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------- decoding in 4 bits
+ * Weights and key/value caches in 4 bits: what a decoding step reads, a quarter
+ * of bf16's.
+ *
+ * A code of LD_W4_E2M1 (and of the caches) is a 4-bit float: a sign (bit 3) and
+ * one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  32 neighbours share a scale 2^e, held as the byte
+ * e + 127: the smallest with e >= -100 and max|x| <= 6 2^e, but 2^125 at most (larger
+ * magnitudes are held as 6 2^125); 255 stands for NaN, where an element is not finite,
+ * and such a group reads as NaN as a whole.  A code of LD_W4_INT4 is a sign and 0 .. 7;
+ * `group` neighbours share a bf16 scale, max|w| / 7 rounded to nearest, at least 2^-100,
+ * or NaN.  A code is x / scale rounded to nearest, ties to even, and at most 6 (7).
+ *
+ * ld_w4: weights [n, k] in 4 bits, groups along k.
+ *   format: LD_W4_E2M1 (group 32) or LD_W4_INT4 (group 32, 64 or 128).
+ *   n >= 1; k >= 8, k % 8 == 0 (the last group may be a part of one).
+ *   codes:  device, ld_w4_code_bytes, 16-byte aligned: [ceil(n / 8)][ceil(k / 256)][64][4]
+ *           dwords.  Lane 16 g + 8 h + r, dword s holds row 8 t + r at k = 256 c + 128 h +
+ *           32 s + 8 g + e, e < 8: e2m1 in bits 4 e .. 4 e + 3; int4 with e < 4 in bits 8 e ..
+ *           8 e + 2 and the sign in 8 e + 7, with e = 4 + i in bits 8 i + 4 .. 8 i + 6 and the sign
+ *           in (8 i + 11) mod 32.  Rows and k past the last are zeros.
+ *   scales: device, ld_w4_scale_bytes, 16-byte aligned: [ceil(n / 8)][ceil(k / 256)][2 (h)]
+ *           [8 (r)][128 / group] bytes (e2m1) or bf16 (int4).
+ *
+ * ld_kv4: a key/value cache in 4 bits, a scale for each 32 dimensions of each
+ * position.  n_kv_heads may divide the call's n_heads, as in ld_kv8.  Nothing a position
+ * holds depends on another, so rows that are taken back (a draft's) leave nothing behind.
+ *   d_head: 64 or 128.  1 <= s_max <= 2^30 positions.  n_seq, 2 n_kv_heads, n_heads <= 65535.
+ *   codes:  device, ld_kv4_code_bytes, 16-byte aligned.  With S8 = s_max rounded up to 8,
+ *           sequence b's head h has at (b n_kv_heads + h) S8 d_head bytes its keys [S8]
+ *           [d_head / 2] (dimension 2 i in the low half of byte i), then its values [S8 / 8]
+ *           [16 (i)][d_head / 32 (j)][8 (position)], a byte with dimension 32 j + i in its low
+ *           half and 32 j + 16 + i in its high one.
+ *   scales: device, ld_kv4_scale_bytes, 16-byte aligned: bytes [n_seq][n_kv_heads][2]
+ *           [S8][d_head / 32], keys' then values'.
+ *   sums:   NULL, or device float32 [n_seq][n_kv_heads][s_max]: the attention weight each
+ *           position has drawn.  A store sets its rows' to 0; every ld_attn_decode_kv4 adds
+ *           to each position it sees its softmax weights, of the head's queries and the
+ *           call's new rows in that order (a draft's too).
+ * The memory need not be initialised: nothing is read behind the last position. */
+typedef enum { LD_W4_E2M1 = 0, LD_W4_INT4 = 1 } ld_w4_format;
+
+typedef struct {
+  int32_t format, group, n, k;
+  void* codes;
+  void* scales;
+} ld_w4;
+
+typedef struct {
+  int32_t n_seq, n_kv_heads, d_head, s_max;
+  void* codes;
+  void* scales;
+  float* sums;
+} ld_kv4;
+
+/* One layer's parameters with its matrices in 4 bits: those of ld_weights, the gains
+ * bf16. */
+typedef struct {
+  const void *g_attn, *g_mlp;
+  ld_w4 w_qkv, w_o, w_gate_up, w_down;
+} ld_weights_w4;
+
+/* ld_stack_eval with the keys and values of positions 0..S-1 written to 4-bit caches
+ * (bf16 only), as ld_stack_eval_kv8 writes 8-bit ones. */
+int ld_stack_eval_kv4(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
+                      const float* r_eval, void* x, const ld_kv4* kv, void* ws, size_t ws_bytes, void* stream);
+
+/* Bytes of scratch ld_stack_decode_kv4 and ld_stack_decode_w4 need for n_new rows per
+ * sequence or fewer and caches of at most s_max positions, with = 1 (or without = 0)
+ * sums (0 on invalid arguments). */
+size_t ld_decode_kv4_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max, int32_t sums);
+
+/* ld_stack_decode over 4-bit caches: each active layer writes the new rows' keys and
+ * values as ld_kv4_store does and attends as ld_attn_decode_kv4 does, which adds to
+ * the sums of the caches that have them.  kv, pos and seq_pos as in
+ * ld_stack_decode_kv8. */
+int ld_stack_decode_kv4(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
+                        const float* r_eval, void* x, const ld_kv4* kv, int32_t pos, const int32_t* seq_pos,
+                        int32_t n_new, void* ws, size_t ws_bytes, void* stream);
+
+/* The same with the layers' matrices in 4 bits too: every projection is ld_gemm_w4's. */
+int ld_stack_decode_w4(const ld_config* cfg, int32_t n_layers, const ld_weights_w4* w, const uint8_t* active,
+                       const float* r_eval, void* x, const ld_kv4* kv, int32_t pos, const int32_t* seq_pos,
+                       int32_t n_new, void* ws, size_t ws_bytes, void* stream);
+
 /* ------------------------------------------- kernel-level entry points
  * The single kernels the layer is built from, exposed for isolated parity
  * tests and roofline measurements.  dtype is an ld_dtype; all row counts are
@@ -507,6 +591,76 @@ int ld_kv8_load(const ld_kv8* kv, int32_t pos, int32_t n, const int32_t* seq_len
 size_t ld_attn_decode_kv8_ws_bytes(const ld_kv8* kv, int32_t n_heads, int32_t n_new);
 int ld_attn_decode_kv8(const ld_kv8* kv, int32_t n_heads, int32_t alibi, int32_t pos, const int32_t* seq_pos,
                        int32_t n_new, const void* qkv, void* o, void* ws, size_t ws_bytes, void* stream);
+
+/* Bytes of codes and of scales (the pointers are not used; 0 on an invalid
+ * descriptor). */
+size_t ld_w4_code_bytes(const ld_w4* w);
+size_t ld_w4_scale_bytes(const ld_w4* w);
+
+/* Weights to 4 bits and back.  src, dst: device bf16 [n, k], rows ld elements apart (a
+ * multiple of 8, >= k), 16-byte aligned.  A value read back is code x scale rounded to bf16
+ * (exact for e2m1). */
+int ld_w4_pack(const ld_w4* w, const void* src, int32_t ld, void* stream);
+int ld_w4_load(const ld_w4* w, void* dst, int32_t ld, void* stream);
+
+/* Projection of 1 <= M <= 64 rows by weights in 4 bits:
+ *   C[m, n] = act(R[m, n] + alpha * sum_k A'[m, k] W[n, k]),
+ * A' = A when g is NULL, else the RMSNorm of A's rows with gain g [k],
+ * A'[m, k] = A[m, k] * rstd_m * g[k], rstd_m = 1/sqrt(mean_k A[m, k]^2 + eps), unrounded
+ * (M <= 16 and k <= 8192; LD_E_UNSUPPORTED beyond).
+ *   act 0: none (R optional, [M, N], rows ldr apart); N = w->n
+ *   act 1: SwiGLU; W holds the gate rows 0..N-1, then the up rows: N = w->n / 2, a
+ *          multiple of 8; C = silu(u) v (R must be NULL)
+ *   act 2: squared ReLU (R must be NULL).
+ * A: device bf16 [M, k], rows lda apart (a multiple of 8), 16-byte aligned, as g; C: device
+ * bf16 [M, N], rows ldc apart.  C may be R.  Weights are exact, sums float32, and the
+ * activation takes the sums unrounded.  ws: device scratch of ld_gemm_w4_ws_bytes(w, M, act)
+ * bytes (may be 0, then ws may be NULL; enough for fewer rows), 16-byte aligned. */
+size_t ld_gemm_w4_ws_bytes(const ld_w4* w, int32_t M, int32_t act);
+int ld_gemm_w4(int32_t M, const void* A, int32_t lda, const void* g, float eps, const ld_w4* w, void* C, int32_t ldc,
+               float alpha, const void* R, int32_t ldr, int32_t act, void* ws, size_t ws_bytes, void* stream);
+
+size_t ld_kv4_code_bytes(const ld_kv4* kv);
+size_t ld_kv4_scale_bytes(const ld_kv4* kv);
+
+/* Quantises the keys and values of qkv rows into the cache, sets their sums to 0, and
+ * touches nothing else.  Arguments as in ld_kv8_store. */
+int ld_kv4_store(const ld_kv4* kv, int32_t n_heads, int32_t n_new, int32_t pos, const int32_t* seq_pos,
+                 const void* qkv, void* stream);
+
+/* Positions pos .. pos + n - 1 of every sequence back to bf16, exactly.  Arguments as in
+ * ld_kv8_load. */
+int ld_kv4_load(const ld_kv4* kv, int32_t pos, int32_t n, const int32_t* seq_len, void* out, void* stream);
+
+/* ld_attn_decode over a 4-bit cache; arguments as in ld_attn_decode_kv8.  Where the cache
+ * has sums, every position's weights are added to them.  Scores, softmax weights and sums
+ * in float32.
+ *   ws: device scratch of ld_attn_decode_kv4_ws_bytes(kv, n_heads, n_new) bytes (more for a
+ *   cache with sums; enough for every pos and for fewer new rows; 0 on invalid arguments),
+ *   16-byte aligned. */
+size_t ld_attn_decode_kv4_ws_bytes(const ld_kv4* kv, int32_t n_heads, int32_t n_new);
+int ld_attn_decode_kv4(const ld_kv4* kv, int32_t n_heads, int32_t alibi, int32_t pos, const int32_t* seq_pos,
+                       int32_t n_new, const void* qkv, void* o, void* ws, size_t ws_bytes, void* stream);
+
+/* Eviction: of the first `len` positions (seq_len[b], where given) of each sequence and
+ * key/value head of `from`, those that stay go to the first places of `to`, in their
+ * order, with their sums (if `to` has some).  Of n > keep positions the last `recent` stay, and
+ * the keep - recent of the others with the largest sums (NaN above all; of equal ones the
+ * first); of n <= keep all do.  Places behind are left as they are.
+ *   from->sums must be given.  `to`: another cache of as many sequences and heads of as
+ *   many dimensions, s_max >= keep, that shares no memory with `from`.
+ *   seq_len: NULL, or device int32[n_seq], len being the most; a sequence outside [0, len]
+ *   has no positions.
+ *   idx: device int32 [n_seq][n_kv_heads][keep], the positions that stayed, then -1.
+ *   1 <= len <= from->s_max, 0 <= recent <= keep, keep >= 1.
+ *   ws: device scratch of ld_kv4_evict_ws_bytes(from, len, keep) bytes (may be 0), 16-byte
+ *   aligned.
+ * A position's number in `to` is its place there, and decoding goes on at place
+ * min(n, keep).  Attention without position encoding is over the rows that stayed;
+ * with the ALiBi bias distances are those of the places, smaller than they were. */
+size_t ld_kv4_evict_ws_bytes(const ld_kv4* from, int32_t len, int32_t keep);
+int ld_kv4_evict(const ld_kv4* from, const ld_kv4* to, int32_t len, const int32_t* seq_len, int32_t keep,
+                 int32_t recent, int32_t* idx, void* ws, size_t ws_bytes, void* stream);
 
 /* Causal multi-head attention over n_seq independent sequences.
  *   qkv: device [n_seq*S, 3*H*dh] as produced by x W_qkv^T;

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "liblayerdrop.so")
 
 LD_F32, LD_BF16 = 0, 1
 LD_KV8_E4M3, LD_KV8_INT8 = 0, 1
+LD_W4_E2M1, LD_W4_INT4 = 0, 1
 LD_GRAN_LAYER_SEQ, LD_GRAN_SUBLAYER_SEQ, LD_GRAN_LAYER_BATCH, LD_GRAN_SUBLAYER_BATCH = 0, 1, 2, 3
 UNIFORM, ILD, ALD = 0, 1, 2
 CONSTANT, ITS, DTS = 0, 1, 2
@@ -44,6 +45,24 @@ class ld_kv8(C.Structure):
     tensors = ()
 
 
+class ld_w4(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("format", "group", "n", "k")] + [("codes", C.c_void_p), ("scales", C.c_void_p)]
+    device = None     # the tensors' GPU, where w4() was given tensors
+    tensors = ()
+
+
+class ld_kv4(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("n_seq", "n_kv_heads", "d_head", "s_max")] + \
+               [("codes", C.c_void_p), ("scales", C.c_void_p), ("sums", C.c_void_p)]
+    device = None     # the tensors' GPU, where kv4() was given tensors
+    tensors = ()
+
+
+class ld_weights_w4(C.Structure):
+    _fields_ = [("g_attn", C.c_void_p), ("g_mlp", C.c_void_p)] + \
+               [(k, ld_w4) for k in ("w_qkv", "w_o", "w_gate_up", "w_down")]
+
+
 class ld_weights(C.Structure):
     _fields_ = [(k, C.c_void_p) for k in WEIGHT_KEYS]
 
@@ -59,6 +78,8 @@ _lib = C.CDLL(LIB_PATH)
 _vp, _i32, _i64, _u64, _f32, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_float, C.c_size_t
 _PCFG = C.POINTER(ld_config)
 _PKV8 = C.POINTER(ld_kv8)
+_PKV4 = C.POINTER(ld_kv4)
+_PW4 = C.POINTER(ld_w4)
 _SIGS = {
     "ld_status_string": (C.c_char_p, [C.c_int]),
     "ld_last_error": (C.c_char_p, []),
@@ -120,6 +141,26 @@ _SIGS = {
     "ld_kv8_load": (C.c_int, [_PKV8, _i32, _i32, _vp, _vp, _vp]),
     "ld_attn_decode_kv8_ws_bytes": (_sz, [_PKV8, _i32, _i32]),
     "ld_attn_decode_kv8": (C.c_int, [_PKV8, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
+    "ld_stack_eval_kv4": (C.c_int, [_PCFG, _i32, C.POINTER(ld_weights), _vp, _vp, _vp, _PKV4, _vp, _sz, _vp]),
+    "ld_decode_kv4_ws_bytes": (_sz, [_PCFG, _i32, _i32, _i32]),
+    "ld_stack_decode_kv4": (C.c_int, [_PCFG, _i32, C.POINTER(ld_weights), _vp, _vp, _vp, _PKV4, _i32, _vp, _i32,
+                                      _vp, _sz, _vp]),
+    "ld_stack_decode_w4": (C.c_int, [_PCFG, _i32, C.POINTER(ld_weights_w4), _vp, _vp, _vp, _PKV4, _i32, _vp, _i32,
+                                     _vp, _sz, _vp]),
+    "ld_w4_code_bytes": (_sz, [_PW4]),
+    "ld_w4_scale_bytes": (_sz, [_PW4]),
+    "ld_w4_pack": (C.c_int, [_PW4, _vp, _i32, _vp]),
+    "ld_w4_load": (C.c_int, [_PW4, _vp, _i32, _vp]),
+    "ld_gemm_w4_ws_bytes": (_sz, [_PW4, _i32, _i32]),
+    "ld_gemm_w4": (C.c_int, [_i32, _vp, _i32, _vp, _f32, _PW4, _vp, _i32, _f32, _vp, _i32, _i32, _vp, _sz, _vp]),
+    "ld_kv4_code_bytes": (_sz, [_PKV4]),
+    "ld_kv4_scale_bytes": (_sz, [_PKV4]),
+    "ld_kv4_store": (C.c_int, [_PKV4, _i32, _i32, _i32, _vp, _vp, _vp]),
+    "ld_kv4_load": (C.c_int, [_PKV4, _i32, _i32, _vp, _vp, _vp]),
+    "ld_attn_decode_kv4_ws_bytes": (_sz, [_PKV4, _i32, _i32]),
+    "ld_attn_decode_kv4": (C.c_int, [_PKV4, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
+    "ld_kv4_evict_ws_bytes": (_sz, [_PKV4, _i32, _i32]),
+    "ld_kv4_evict": (C.c_int, [_PKV4, _PKV4, _i32, _vp, _i32, _i32, _vp, _vp, _sz, _vp]),
     "ld_prof_start": (C.c_int, [C.c_char_p]),
     "ld_prof_stop": (C.c_int, []),
     "ld_prof_result": (C.c_int, [C.POINTER(_i64), C.POINTER(C.c_double), C.POINTER(C.c_double),
@@ -461,8 +502,8 @@ def ld_kv8_scale_bytes(kv):
 
 
 def _kv8_device(kv):
-    """The current device, on which the cache and the stream have to be; None
-    for a cache given by addresses."""
+    """The current device, on which the cache (or 4-bit weights) and the stream
+    have to be; None for one given by addresses."""
     if kv.device is not None and kv.device != torch.cuda.current_device():
         raise ValueError(f"codes: on cuda:{kv.device}, which is not the current device")
     return kv.device
@@ -559,6 +600,244 @@ def ld_stack_decode_kv8(cfg, ws_list, x, kv, pos, n_new, ws, seq_pos=None, activ
     _check(_lib.ld_stack_decode_kv8(C.byref(cfg), L, wa, act, rr, px, kk, pos,
                                     _kv8_ptr(seq_pos, "seq_pos", dev, torch.int32, cfg.batch), n_new,
                                     _kv8_ptr(ws, "ws", dev), ws.numel() * ws.element_size(), _stream(stream, dev)))
+
+
+def _on_one_device(obj, tensors):
+    """Notes the device of a descriptor's tensors, which it keeps."""
+    devs = {t.device for t in tensors if isinstance(t, torch.Tensor)}
+    if len(devs) > 1:
+        raise ValueError("the descriptor's tensors are on " + " and ".join(sorted(map(str, devs))))
+    if devs:
+        obj.device = devs.pop().index
+    obj.tensors = tensors
+    return obj
+
+
+def w4(codes, scales, format, group, n, k):
+    """ld_w4 over device tensors: codes (uint8) and scales (uint8 for e2m1,
+    bfloat16 for int4), of ld_w4_code_bytes and ld_w4_scale_bytes bytes; None for
+    a descriptor that only those two are asked about.  It keeps the tensors."""
+    w = ld_w4(format, group, n, k)
+    if codes is None and scales is None:
+        return w
+    nb, sb = ld_w4_code_bytes(w), ld_w4_scale_bytes(w)
+    if nb:   # an invalid descriptor is refused by the call that takes it
+        _need(codes, "codes", torch.uint8, nb)
+        if format == LD_W4_E2M1:
+            _need(scales, "scales", torch.uint8, sb)
+        else:
+            _need(scales, "scales", torch.bfloat16, sb // 2)
+    w.codes, w.scales = _ptr(codes, "codes"), _ptr(scales, "scales")
+    return _on_one_device(w, (codes, scales))
+
+
+def ld_w4_code_bytes(w):
+    return _lib.ld_w4_code_bytes(C.byref(w))
+
+
+def ld_w4_scale_bytes(w):
+    return _lib.ld_w4_scale_bytes(C.byref(w))
+
+
+def _w4_rows(w, t, name, device):
+    """A matrix [n, k] in bfloat16 whose rows may be apart."""
+    if isinstance(t, torch.Tensor):
+        if t.dtype != torch.bfloat16 or tuple(t.shape) != (w.n, w.k):
+            raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, expected bfloat16 {(w.n, w.k)}")
+        if t.is_cuda and device is not None and t.device.index != device:
+            raise ValueError(f"{name}: on {t.device}, the descriptor's tensors on cuda:{device}")
+    return _ptr(t, name, inner=True), t.stride(0) if w.n > 1 else w.k
+
+
+def ld_w4_pack(w, src, stream=None):
+    """bfloat16 weights [n, k] to 4 bits."""
+    dev = _kv8_device(w)
+    p, ld = _w4_rows(w, src, "src", dev)
+    _check(_lib.ld_w4_pack(C.byref(w), p, ld, _stream(stream, dev)))
+
+
+def ld_w4_load(w, dst, stream=None):
+    """4-bit weights back to bfloat16 [n, k]."""
+    dev = _kv8_device(w)
+    p, ld = _w4_rows(w, dst, "dst", dev)
+    _check(_lib.ld_w4_load(C.byref(w), p, ld, _stream(stream, dev)))
+
+
+def ld_gemm_w4_ws_bytes(w, M, act=DEC_ACT_NONE):
+    return _lib.ld_gemm_w4_ws_bytes(C.byref(w), M, act)
+
+
+def _rows_2d(t, name, device, shape):
+    """Address and row distance of a bfloat16 matrix whose rows may be apart."""
+    if t is None:
+        return None, 0
+    if isinstance(t, torch.Tensor):
+        if t.dtype is not torch.bfloat16 or t.dim() != 2 or t.shape[0] != shape[0] or t.shape[1] != shape[1]:
+            raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, expected bfloat16 {tuple(shape)}")
+        if t.get_device() != (torch.cuda.current_device() if device is None else device):
+            raise ValueError(f"{name}: on {t.device}, which is not the current device")
+        if shape[1] > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name}: the last dimension must be contiguous")
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _ws(ws, device):
+    """Address and bytes of a workspace."""
+    if ws is None:
+        return None, 0
+    return _kv8_ptr(ws, "ws", device), ws.numel() * ws.element_size()
+
+
+def ld_gemm_w4(w, A, C_out, ws=None, g=None, eps=1e-5, alpha=1.0, R=None, act=DEC_ACT_NONE, stream=None):
+    """Projection of up to 64 rows by 4-bit weights, C = act(R + alpha A' W^T), A' the
+    RMSNorm of A's rows with gain g when g is given; with SwiGLU w holds the gate
+    rows then the up rows and C has half as many columns."""
+    dev = _kv8_device(w)
+    M, N = A.shape[0], w.n // 2 if act == DEC_ACT_SWIGLU else w.n
+    pa, lda = _rows_2d(A, "A", dev, (M, w.k))
+    pc, ldc = _rows_2d(C_out, "C_out", dev, (M, N))
+    pr, ldr = _rows_2d(R, "R", dev, (M, N))
+    pw, wsb = _ws(ws, dev)
+    _check(_lib.ld_gemm_w4(M, pa, lda, _kv8_ptr(g, "g", dev, torch.bfloat16, w.k),
+                           eps, C.byref(w), pc, ldc, alpha, pr, ldr, act, pw, wsb, _stream(stream, dev)))
+
+
+def kv4(codes, scales, n_seq, n_kv_heads, d_head, s_max, sums=None):
+    """ld_kv4 over device tensors: codes and scales (uint8) of ld_kv4_code_bytes and
+    ld_kv4_scale_bytes bytes, sums None or float32 [n_seq, n_kv_heads, s_max]; None for
+    a descriptor that only sizes are asked about.  It keeps the tensors."""
+    kv = ld_kv4(n_seq, n_kv_heads, d_head, s_max)
+    if codes is None and scales is None and sums is None:
+        return kv
+    n, m = ld_kv4_code_bytes(kv), ld_kv4_scale_bytes(kv)
+    if n:   # an invalid descriptor is refused by the call that takes it
+        _need(codes, "codes", torch.uint8, n)
+        _need(scales, "scales", torch.uint8, m)
+        _need(sums, "sums", torch.float32, n_seq * n_kv_heads * s_max)
+    kv.codes, kv.scales, kv.sums = _ptr(codes, "codes"), _ptr(scales, "scales"), _ptr(sums, "sums")
+    return _on_one_device(kv, (codes, scales, sums))
+
+
+def ld_kv4_code_bytes(kv):
+    return _lib.ld_kv4_code_bytes(C.byref(kv))
+
+
+def ld_kv4_scale_bytes(kv):
+    return _lib.ld_kv4_scale_bytes(C.byref(kv))
+
+
+def ld_kv4_store(kv, n_heads, n_new, pos, qkv, seq_pos=None, stream=None):
+    """Quantise the keys and values of qkv rows into the cache at positions
+    pos (or seq_pos[b] <= pos) onwards."""
+    dev = _kv8_device(kv)
+    _check(_lib.ld_kv4_store(C.byref(kv), n_heads, n_new, pos,
+                             _kv8_ptr(seq_pos, "seq_pos", dev, torch.int32, kv.n_seq),
+                             _kv8_rows(kv, n_heads, n_new, qkv, dev), _stream(stream, dev)))
+
+
+def ld_kv4_load(kv, pos, n, out, seq_len=None, stream=None):
+    """Positions pos .. pos + n - 1 back to bfloat16 rows [n_seq, n, 2 n_kv_heads d_head]."""
+    dev = _kv8_device(kv)
+    _check(_lib.ld_kv4_load(C.byref(kv), pos, n, _kv8_ptr(seq_len, "seq_len", dev, torch.int32, kv.n_seq),
+                            _kv8_ptr(out, "out", dev, torch.bfloat16, kv.n_seq * n * 2 * kv.n_kv_heads * kv.d_head),
+                            _stream(stream, dev)))
+
+
+def ld_attn_decode_kv4_ws_bytes(kv, n_heads, n_new):
+    return _lib.ld_attn_decode_kv4_ws_bytes(C.byref(kv), n_heads, n_new)
+
+
+def ld_attn_decode_kv4(kv, n_heads, pos, n_new, qkv, o, ws, seq_pos=None, alibi=0, stream=None):
+    """Attention of n_new rows per sequence at positions pos (or seq_pos[b])
+    onwards over the cache, which already holds them; its weights are added to
+    the cache's sums, if it has some."""
+    dev = _kv8_device(kv)
+    pw, wsb = _ws(ws, dev)
+    _check(_lib.ld_attn_decode_kv4(C.byref(kv), n_heads, int(alibi), pos,
+                                   _kv8_ptr(seq_pos, "seq_pos", dev, torch.int32, kv.n_seq), n_new,
+                                   _kv8_rows(kv, n_heads, n_new, qkv, dev),
+                                   _kv8_ptr(o, "o", dev, torch.bfloat16, kv.n_seq * n_new * n_heads * kv.d_head),
+                                   pw, wsb, _stream(stream, dev)))
+
+
+def ld_kv4_evict_ws_bytes(kv, length, keep):
+    return _lib.ld_kv4_evict_ws_bytes(C.byref(kv), length, keep)
+
+
+def ld_kv4_evict(src, dst, length, keep, recent, idx, ws=None, seq_len=None, stream=None):
+    """Of each head's first `length` (or seq_len[b] <= length) positions of src the last
+    `recent` and the keep - recent others with the largest sums, to dst; idx: int32
+    [n_seq, n_kv_heads, keep], their positions."""
+    dev = _kv8_device(src)
+    if dst.device is not None and dev is not None and dst.device != dev:
+        raise ValueError(f"dst: on cuda:{dst.device}, src on cuda:{dev}")
+    pw, wsb = _ws(ws, dev)
+    _check(_lib.ld_kv4_evict(C.byref(src), C.byref(dst), length,
+                             _kv8_ptr(seq_len, "seq_len", dev, torch.int32, src.n_seq), keep, recent,
+                             _kv8_ptr(idx, "idx", dev, torch.int32, src.n_seq * src.n_kv_heads * max(keep, 0)),
+                             pw, wsb, _stream(stream, dev)))
+
+
+def weights_w4(w):
+    """ld_weights_w4 from a dict keyed by WEIGHT_KEYS: gains as device tensors,
+    matrices as w4()s."""
+    return ld_weights_w4(_ptr(w["g_attn"], "g_attn"), _ptr(w["g_mlp"], "g_mlp"),
+                         *[w[k] for k in ("w_qkv", "w_o", "w_gate_up", "w_down")])
+
+
+def _kv4_array(kv, n):
+    """Descriptors of n layers and their device, as _kv8_array's."""
+    if len(kv) != n:
+        raise ValueError(f"{n} layers of weights, {len(kv)} of caches")
+    device = None
+    for k in kv:
+        if k is not None:
+            d = _kv8_device(k)
+            device = d if device is None else device
+    return (ld_kv4 * n)(*[k if k is not None else ld_kv4() for k in kv]), device
+
+
+def ld_stack_eval_kv4(cfg, ws_list, x, ws, kv, active=None, r_eval=None, stream=None):
+    """ld_stack_eval that writes 4-bit caches; kv: a kv4() per layer (None
+    allowed for inactive layers)."""
+    L = len(ws_list)
+    wa = (ld_weights * L)(*[weights(w) for w in ws_list])
+    act, rr, (kk, dev) = _u8_array(active, L), _f32_array(r_eval, L), _kv4_array(kv, L)
+    px = _kv8_ptr(x, "x", dev, torch.bfloat16, cfg.batch * cfg.seq * cfg.d_model)
+    pw, wsb = _ws(ws, dev)
+    _check(_lib.ld_stack_eval_kv4(C.byref(cfg), L, wa, act, rr, px, kk, pw, wsb, _stream(stream, dev)))
+
+
+def ld_decode_kv4_ws_bytes(cfg, n_new, s_max, sums=False):
+    return _lib.ld_decode_kv4_ws_bytes(C.byref(cfg), n_new, s_max, int(sums))
+
+
+def _stack_decode_4(call, cfg, wa, L, x, kv, pos, n_new, ws, seq_pos, active, r_eval, stream):
+    act, rr, (kk, dev) = _u8_array(active, L), _f32_array(r_eval, L), _kv4_array(kv, L)
+    px = _kv8_ptr(x, "x", dev, torch.bfloat16, cfg.batch * n_new * cfg.d_model)
+    pw, wsb = _ws(ws, dev)
+    _check(call(C.byref(cfg), L, wa, act, rr, px, kk, pos, _kv8_ptr(seq_pos, "seq_pos", dev, torch.int32, cfg.batch),
+                n_new, pw, wsb, _stream(stream, dev)))
+
+
+def ld_stack_decode_kv4(cfg, ws_list, x, kv, pos, n_new, ws, seq_pos=None, active=None, r_eval=None,
+                        stream=None):
+    """ld_stack_decode over 4-bit caches; seq_pos as in ld_stack_decode_kv8."""
+    L = len(ws_list)
+    _stack_decode_4(_lib.ld_stack_decode_kv4, cfg, (ld_weights * L)(*[weights(w) for w in ws_list]), L, x, kv, pos,
+                    n_new, ws, seq_pos, active, r_eval, stream)
+
+
+def ld_stack_decode_w4(cfg, ws_list, x, kv, pos, n_new, ws, seq_pos=None, active=None, r_eval=None,
+                       stream=None):
+    """ld_stack_decode_kv4 with the layers' matrices in 4 bits; ws_list: a dict
+    for weights_w4() per layer."""
+    L = len(ws_list)
+    for w in ws_list:
+        for k in ("w_qkv", "w_o", "w_gate_up", "w_down"):
+            _kv8_device(w[k])
+    _stack_decode_4(_lib.ld_stack_decode_w4, cfg, (ld_weights_w4 * L)(*[weights_w4(w) for w in ws_list]), L, x, kv, pos,
+                    n_new, ws, seq_pos, active, r_eval, stream)
 
 
 def ld_rmsnorm_fwd(x, g, y, rstd, eps=1e-5, stream=None):

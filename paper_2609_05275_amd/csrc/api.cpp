@@ -14,7 +14,9 @@
 #include <vector>
 
 #include "ld_internal.h"
+#include "ld_kv4.h"
 #include "ld_kv8.h"
+#include "ld_w4.h"
 
 using namespace ld;
 
@@ -480,17 +482,35 @@ int run_kv8_store(const Kv8View& kv, const void* qkv, int32_t n_heads, int32_t n
   return LD_OK;
 }
 
+int run_kv4_store(const Kv4View& kv, const void* qkv, int32_t n_heads, int32_t n, int32_t pos,
+                  const int32_t* seq_pos, hipStream_t s) {
+  Kv4StoreArgs a{};
+  a.kv = kv;
+  a.qkv = qkv;
+  a.ld_qkv = (static_cast<int64_t>(n_heads) + 2ll * kv.KV) * kv.dh;
+  a.H = n_heads;
+  a.n = n;
+  a.pos = pos;
+  a.seq_pos = seq_pos;
+  ProfScope ps("ld_kv4_store_k", s);
+  const hipError_t e = launch_kv4_store(a, s);
+  if (e != hipSuccess) return fail(LD_E_HIP, "kv4 store: %s", hipGetErrorString(e));
+  ps.end(0, seq_pos ? 0.0 : 2.0 * kv.n_seq * n * kv.KV * kv.dh * (2 + 17.0 / 32));  // 0: only the device knows
+  return LD_OK;
+}
+
 // Attention sub-block on the rows mv keeps.  hc: its kept count when
 // profiling (read back by the caller), else -1.  scatter = 0 leaves
 // Z = X + r f_attn(X) compacted in act (zk) for the FFN sub-block of the same
 // rows; scatter = 1 writes Z into the kept rows of x (sub-layer granularity,
 // where the FFN keeps its own rows).
 // kv: null, or a cache [B, s_max, 2d] that receives the keys and values of
-// positions 0..S-1 (evaluation form only: every sequence processed); kv8: likewise,
-// in 8 bits.
+// positions 0..S-1 (evaluation form only: every sequence processed); kv8, kv4:
+// likewise, in 8 or 4 bits.
 int attn_forward_part(const ld_config* cfg, const Dims& D, const ld_weights& w, const MaskView& mv,
                       const ActPtrs& act, Stream xs, int64_t hc, bool scatter, hipStream_t s,
-                      void* kv = nullptr, int32_t s_max = 0, const Kv8View* kv8 = nullptr) {
+                      void* kv = nullptr, int32_t s_max = 0, const Kv8View* kv8 = nullptr,
+                      const Kv4View* kv4 = nullptr) {
   const int dt = D.dtype;
   const int64_t T = D.T;
   const int64_t hm = hc * D.S;
@@ -559,6 +579,9 @@ int attn_forward_part(const ld_config* cfg, const Dims& D, const ld_weights& w, 
   }
   if (kv8)
     if (int rc = run_kv8_store(*kv8, act.at(act.L.qkv), static_cast<int32_t>(D.H), static_cast<int32_t>(D.S), 0, nullptr, s))
+      return rc;
+  if (kv4)
+    if (int rc = run_kv4_store(*kv4, act.at(act.L.qkv), static_cast<int32_t>(D.H), static_cast<int32_t>(D.S), 0, nullptr, s))
       return rc;
   // causal attention on the kept sequences
   {
@@ -1211,7 +1234,7 @@ int check_host_counts(const Dims& D, const LayerMasks& lm, const std::vector<int
 
 // Scratch of a decoding step.
 struct DecLayout {
-  size_t h, rstd, qkv, att, z, uv, s, part_o, part_ml, skp, skp_bytes, total;
+  size_t h, rstd, qkv, att, z, uv, s, part_o, part_ml, scores, row_ml, skp, skp_bytes, total;
 };
 
 size_t skinny_part_bytes(int64_t M, int64_t N, int64_t K) {
@@ -1248,8 +1271,9 @@ size_t dec_part_rows(const Dims& D, int64_t s_max) {
 }
 
 // Scratch of a decoding step of n_new rows per sequence.  pc: partial rows of the
-// attention (dec_part_rows, kv8_part_rows).
-DecLayout dec_layout(const Dims& D, int64_t n_new, size_t pc) {
+// attention (dec_part_rows, kv8_part_rows, kv4_part_rows).  score_keys: keys of a row's
+// scores, over caches with sums.  w4: the projections may be 4-bit weights' too.
+DecLayout dec_layout(const Dims& D, int64_t n_new, size_t pc, int64_t score_keys = 0, bool w4 = false) {
   DecLayout L{};
   size_t o = 0;
   auto take = [&](size_t bytes) {
@@ -1267,11 +1291,18 @@ DecLayout dec_layout(const Dims& D, int64_t n_new, size_t pc) {
   L.s = take(es * M * D.f);
   L.part_o = take(4 * pc * D.dh);
   L.part_ml = take(4 * pc * 2);
-  if (dec_split_k(M, D.d)) {
-    const int64_t shapes[4][2] = {{3 * D.d, D.d}, {D.d, D.d}, {D.fw, D.d}, {D.d, D.f}};
-    for (const auto& sh : shapes) L.skp_bytes = std::max(L.skp_bytes, skinny_fused_part_bytes(M, sh[0], sh[1]));
-    L.skp = take(L.skp_bytes);
+  if (score_keys) {
+    L.scores = take(4 * M * D.H * score_keys);
+    L.row_ml = take(8 * M * D.H);
   }
+  const int64_t shapes[4][2] = {{3 * D.d, D.d}, {D.d, D.d}, {D.fw, D.d}, {D.d, D.f}};
+  if (dec_split_k(M, D.d))
+    for (const auto& sh : shapes) L.skp_bytes = std::max(L.skp_bytes, skinny_fused_part_bytes(M, sh[0], sh[1]));
+  if (w4)
+    for (int i = 0; i < 4; ++i)
+      L.skp_bytes = std::max(L.skp_bytes, w4_gemm_ws_bytes(std::min<int64_t>(M, kW4MaxM), shapes[i][0], shapes[i][1],
+                                                          i == 2 && D.kind == LD_BLOCK_SWIGLU ? kDecActSwiglu : kDecActNone));
+  if (L.skp_bytes) L.skp = take(L.skp_bytes);
   L.total = o;
   return L;
 }
@@ -1280,9 +1311,9 @@ DecLayout dec_layout(const Dims& D, int64_t n_new, size_t pc) {
 // kSkinnyMaxM rows in all may need the split-K sums that more do not, and the
 // attention more partial rows.  part_rows: of a number of new rows.
 template <class PartRows>
-size_t dec_bytes(const Dims& D, int32_t n_new, PartRows part_rows) {
+size_t dec_bytes(const Dims& D, int32_t n_new, PartRows part_rows, int64_t score_keys = 0, bool w4 = false) {
   size_t most = 0;
-  for (int32_t n = 1; n <= n_new; ++n) most = std::max(most, dec_layout(D, n, part_rows(n)).total);
+  for (int32_t n = 1; n <= n_new; ++n) most = std::max(most, dec_layout(D, n, part_rows(n), score_keys, w4).total);
   return most;
 }
 
@@ -1397,6 +1428,201 @@ int check_kv8_layer(const Dims& D, const ld_kv8* kv, int32_t l, Kv8View* out) {
     return fail(LD_E_SHAPE, "kv[%d] is of %d sequences of %d heads of %d, the configuration of %lld, %lld, %lld", l,
                 kv->n_seq, kv->n_kv_heads, kv->d_head, static_cast<long long>(D.B), static_cast<long long>(D.H),
                 static_cast<long long>(D.dh));
+  return LD_OK;
+}
+
+// A 4-bit cache's descriptor, without its pointers.
+int check_kv4(const ld_kv4* kv, Kv4View* out) {
+  if (!kv) return fail(LD_E_INVALID, "NULL kv");
+  if (kv->d_head != 64 && kv->d_head != 128) return fail(LD_E_UNSUPPORTED, "d_head must be 64 or 128");
+  if (kv->n_seq < 1 || kv->n_kv_heads < 1 || kv->s_max < 1) return fail(LD_E_SHAPE, "n_seq, n_kv_heads, s_max must be >= 1");
+  if (kv->n_seq > kMaxGridYZ || kv->n_kv_heads > kMaxGridYZ / 2)
+    return fail(LD_E_SHAPE, "n_seq or 2 n_kv_heads above %d", kMaxGridYZ);
+  // sums of two positions and the tiles of 8 positions of all heads stay in 32 bits
+  if (kv->s_max > 1 << 30 || 2ll * kv->n_seq * kv->n_kv_heads > INT32_MAX / (kv->s_max / 8 + 3))
+    return fail(LD_E_SHAPE, "n_seq n_kv_heads s_max too large");
+  Kv4View v{};
+  v.codes = static_cast<uint8_t*>(kv->codes);
+  v.scales = static_cast<uint8_t*>(kv->scales);
+  v.sums = kv->sums;
+  v.n_seq = kv->n_seq;
+  v.KV = kv->n_kv_heads;
+  v.dh = kv->d_head;
+  v.s8 = (kv->s_max + 7) / 8 * 8;
+  v.s_max = kv->s_max;
+  *out = v;
+  return LD_OK;
+}
+
+size_t kv4_code_bytes(const Kv4View& v) { return static_cast<size_t>(v.n_seq) * v.KV * v.s8 * v.dh; }
+size_t kv4_scale_bytes(const Kv4View& v) { return static_cast<size_t>(v.n_seq) * v.KV * 2 * v.s8 * (v.dh / 32); }
+size_t kv4_sum_bytes(const Kv4View& v) { return 4ull * v.n_seq * v.KV * v.s_max; }
+
+int check_kv4_buffers(const ld_kv4* kv, Kv4View* out) {
+  if (int rc = check_kv4(kv, out)) return rc;
+  if (!kv->codes || !kv->scales) return fail(LD_E_INVALID, "NULL codes or scales");
+  if ((reinterpret_cast<uintptr_t>(kv->codes) | reinterpret_cast<uintptr_t>(kv->scales)) & 15)
+    return fail(LD_E_INVALID, "codes and scales must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(kv->sums) & 3) return fail(LD_E_INVALID, "sums must be 4-byte aligned");
+  return LD_OK;
+}
+
+int check_kv4_heads(const ld_kv4* kv, int32_t n_heads) {
+  if (n_heads < 1 || n_heads % kv->n_kv_heads) return fail(LD_E_SHAPE, "n_heads must be a multiple of n_kv_heads");
+  if (n_heads > kMaxGridYZ) return fail(LD_E_SHAPE, "n_heads above %d", kMaxGridYZ);
+  if (static_cast<int64_t>(kv->n_seq) * n_heads * kDecMaxRows > INT32_MAX) return fail(LD_E_SHAPE, "n_seq n_heads too large");
+  return LD_OK;
+}
+
+// The new rows of a call and where they stand.
+int check_kv4_rows(const ld_kv4* kv, int32_t n_heads, int32_t n_new, int32_t pos, const void* qkv,
+                   const int32_t* seq_pos) {
+  if (int rc = check_kv4_heads(kv, n_heads)) return rc;
+  if (n_new < 1) return fail(LD_E_SHAPE, "n_new must be >= 1");
+  if (pos < 0 || static_cast<int64_t>(pos) + n_new > kv->s_max) return fail(LD_E_SHAPE, "positions outside the cache");
+  if (!qkv) return fail(LD_E_INVALID, "NULL pointer");
+  if (reinterpret_cast<uintptr_t>(qkv) & 15) return fail(LD_E_INVALID, "qkv must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(seq_pos) & 3) return fail(LD_E_INVALID, "seq_pos must be 4-byte aligned");
+  return LD_OK;
+}
+
+// Partial rows of ld_attn_decode_kv4 over any number of keys up to s_max.
+size_t kv4_part_rows(const Kv4View& v, int64_t n_heads, int64_t n_new) {
+  return static_cast<size_t>(v.n_seq) * n_heads * n_new * attn_kv4_max_chunks(attn_kv4_heads(v, n_heads, n_new), v.s8);
+}
+
+// Scratch of ld_attn_decode_kv4: partial rows, and for sums the scores.
+struct Kv4Scratch {
+  size_t part_ml, scores, row_ml, total;
+};
+Kv4Scratch kv4_scratch(const Kv4View& v, int64_t n_heads, int64_t n_new) {
+  const size_t pc = kv4_part_rows(v, n_heads, n_new), rows = static_cast<size_t>(v.n_seq) * n_heads * n_new;
+  Kv4Scratch t{};
+  t.part_ml = up(4 * pc * v.dh);
+  t.scores = t.part_ml + up(4 * pc * 2);
+  t.row_ml = t.scores + (v.sums ? up(4 * rows * attn_kv4_score_keys(v.s8)) : 0);
+  t.total = t.row_ml + (v.sums ? up(8 * rows) : 0);
+  return t;
+}
+
+// Attention of qkv rows b n_new + j at positions pos + j (or seq_pos[b] + j) over a 4-bit
+// cache, and its weights into the sums; part_o and part_ml hold kv4_part_rows.
+int run_kv4_attn(const Kv4View& kv, const void* qkv, void* o, float* part_o, float* part_ml, float* scores, float* row_ml,
+                 int32_t n_heads, int32_t alibi, int32_t n_new, int32_t pos, const int32_t* seq_pos, hipStream_t s) {
+  Kv4AttnArgs a{};
+  a.kv = kv;
+  a.qkv = qkv;
+  a.ld_qkv = (static_cast<int64_t>(n_heads) + 2ll * kv.KV) * kv.dh;
+  a.out = o;
+  a.part_o = part_o;
+  a.part_ml = part_ml;
+  a.scores = kv.sums ? scores : nullptr;
+  a.row_ml = row_ml;
+  a.H = n_heads;
+  a.n_new = n_new;
+  a.pos = pos;
+  a.seq_pos = seq_pos;
+  a.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(kv.dh)));
+  a.alibi = alibi;
+  plan_attn_decode_kv4(a);
+  const double keys = static_cast<double>(pos) + n_new, rows = static_cast<double>(kv.n_seq) * n_new * n_heads;
+  const double known = seq_pos ? 0.0 : 1.0, scored = a.scores ? 4.0 * rows * keys : 0.0;
+  hipError_t e;
+  {
+    ProfScope ps("ld_attn_decode_kv4_k", s);
+    if ((e = launch_attn_decode_kv4(a, s)) != hipSuccess) return fail(LD_E_HIP, "attn decode kv4: %s", hipGetErrorString(e));
+    ps.end(known * 4.0 * rows * kv.dh * keys,
+           known * (kv.n_seq * keys * kv.KV * kv.dh * 17.0 / 16 + 4.0 * rows * kv.dh + scored));
+  }
+  if (a.n_chunks > 1) {
+    ProfScope pc("ld_attn_decode_kv4_combine", s);
+    if ((e = launch_attn_decode_kv4_combine(a, s)) != hipSuccess)
+      return fail(LD_E_HIP, "attn decode kv4 combine: %s", hipGetErrorString(e));
+    pc.end(0, known * (4.0 * rows * (kv.dh + 2) * a.n_chunks + 2.0 * rows * kv.dh));
+  }
+  if (a.scores) {
+    ProfScope pu("ld_kv4_sums_k", s);
+    if ((e = launch_kv4_sums(a, s)) != hipSuccess) return fail(LD_E_HIP, "kv4 sums: %s", hipGetErrorString(e));
+    pu.end(0, known * (scored + 8.0 * kv.n_seq * kv.KV * keys));
+  }
+  return LD_OK;
+}
+
+// The 4-bit cache of an active layer, with its pointers, against the configuration.
+int check_kv4_layer(const Dims& D, const ld_kv4* kv, int32_t l, Kv4View* out) {
+  if (int rc = check_kv4_buffers(kv, out)) return rc;
+  if (kv->n_seq != D.B || kv->n_kv_heads != D.H || kv->d_head != D.dh)
+    return fail(LD_E_SHAPE, "kv[%d] is of %d sequences of %d heads of %d, the configuration of %lld, %lld, %lld", l,
+                kv->n_seq, kv->n_kv_heads, kv->d_head, static_cast<long long>(D.B), static_cast<long long>(D.H),
+                static_cast<long long>(D.dh));
+  return LD_OK;
+}
+
+// 4-bit weights' descriptor, without its pointers.
+int check_w4(const ld_w4* w, W4View* out) {
+  if (!w) return fail(LD_E_INVALID, "NULL w");
+  if (w->format != LD_W4_E2M1 && w->format != LD_W4_INT4) return fail(LD_E_INVALID, "unknown w4 format");
+  if (w->format == LD_W4_E2M1 ? w->group != 32 : w->group != 32 && w->group != 64 && w->group != 128)
+    return fail(LD_E_UNSUPPORTED, "w4 group must be 32 (int4: or 64, 128)");
+  if (w->n < 1 || w->k < 8 || w->k % 8) return fail(LD_E_SHAPE, "need n >= 1, k >= 8, k %% 8 == 0");
+  if (w->n > 1 << 30 || w->k > 1 << 30) return fail(LD_E_SHAPE, "n or k above 2^30");
+  *out = W4View{static_cast<uint8_t*>(w->codes), w->scales, w->format, w->group, w->n, w->k};
+  return LD_OK;
+}
+
+int check_w4_buffers(const ld_w4* w, W4View* out) {
+  if (int rc = check_w4(w, out)) return rc;
+  if (!w->codes || !w->scales) return fail(LD_E_INVALID, "NULL codes or scales");
+  if ((reinterpret_cast<uintptr_t>(w->codes) | reinterpret_cast<uintptr_t>(w->scales)) & 15)
+    return fail(LD_E_INVALID, "codes and scales must be 16-byte aligned");
+  return LD_OK;
+}
+
+// 4-bit weights of a layer, of n rows of k.
+int check_w4_of(const ld_w4* w, const char* name, int32_t l, int64_t n, int64_t k) {
+  W4View v;
+  if (int rc = check_w4_buffers(w, &v)) return rc;
+  if (v.N != n || v.K != k)
+    return fail(LD_E_SHAPE, "%s[%d] is [%d, %d], the configuration's [%lld, %lld]", name, l, v.N, v.K,
+                static_cast<long long>(n), static_cast<long long>(k));
+  return LD_OK;
+}
+
+int check_weights_w4(const Dims& D, const ld_weights_w4& w, int32_t l) {
+  if (!w.g_attn || !w.g_mlp) return fail(LD_E_INVALID, "NULL weight pointer");
+  if ((reinterpret_cast<uintptr_t>(w.g_attn) | reinterpret_cast<uintptr_t>(w.g_mlp)) & 15)
+    return fail(LD_E_INVALID, "gains must be 16-byte aligned");
+  if (int rc = check_w4_of(&w.w_qkv, "w_qkv", l, 3 * D.d, D.d)) return rc;
+  if (int rc = check_w4_of(&w.w_o, "w_o", l, D.d, D.d)) return rc;
+  if (int rc = check_w4_of(&w.w_gate_up, "w_gate_up", l, D.fw, D.d)) return rc;
+  return check_w4_of(&w.w_down, "w_down", l, D.d, D.f);
+}
+
+// Projection by 4-bit weights (see launch_gemm_w4), kW4MaxM rows a launch.
+int run_gemm_w4(const W4View& w, const void* A, int64_t lda, const void* g, float eps, void* C, int64_t ldc, const void* R,
+                int64_t ldr, int64_t M, int64_t N, float alpha, int act, float* part, hipStream_t s) {
+  for (int64_t m = 0; m < M; m += kW4MaxM) {
+    W4GemmArgs a{};
+    a.w = w;
+    a.A = static_cast<const bf16*>(A) + m * lda;
+    a.lda = lda;
+    a.g = g;
+    a.eps = eps;
+    a.C = static_cast<bf16*>(C) + m * ldc;
+    a.ldc = ldc;
+    a.R = R ? static_cast<const bf16*>(R) + m * ldr : nullptr;
+    a.ldr = ldr;
+    a.M = static_cast<int32_t>(std::min<int64_t>(M - m, kW4MaxM));
+    a.N = static_cast<int32_t>(N);
+    a.alpha = alpha;
+    a.act = act;
+    a.part = part;
+    ProfScope ps("ld_gemm_w4_k", s);
+    const hipError_t e = launch_gemm_w4(a, s);
+    if (e != hipSuccess) return fail(LD_E_HIP, "w4 projection: %s", hipGetErrorString(e));
+    const double rows = w.N, K = w.K, scale = (w.format == LD_W4_E2M1 ? 1.0 : 2.0) / w.group;
+    ps.end(2.0 * a.M * rows * K, rows * K * (0.5 + scale) + 2.0 * a.M * (K + N * (R ? 2.0 : 1.0)));
+  }
   return LD_OK;
 }
 
@@ -1753,11 +1979,12 @@ size_t ld_eval_ws_bytes(const ld_config* cfg) {
 
 namespace {
 
-// The caches of a stack's layers: bf16 ones, 8-bit ones, or (evaluation) none.
+// The caches of a stack's layers: bf16 ones, 8-bit ones, 4-bit ones, or (evaluation) none.
 struct StackCaches {
   void* const* kv;     // with s_max positions each
   int32_t s_max;
   const ld_kv8* kv8;
+  const ld_kv4* kv4;
 };
 
 int stack_eval(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
@@ -1766,7 +1993,7 @@ int stack_eval(const ld_config* cfg, int32_t n_layers, const ld_weights* w, cons
   if (int rc = check_cfg(cfg, &D)) return rc;
   if (n_layers < 1 || n_layers > 1024) return fail(LD_E_INVALID, "n_layers outside [1, 1024]");
   if (!w || !x || !ws) return fail(LD_E_INVALID, "NULL pointer");
-  if ((c.kv || c.kv8) && D.dtype != LD_BF16) return fail(LD_E_UNSUPPORTED, "KV caches are bf16 only");
+  if ((c.kv || c.kv8 || c.kv4) && D.dtype != LD_BF16) return fail(LD_E_UNSUPPORTED, "KV caches are bf16 only");
   if (c.kv && c.s_max < D.S) return fail(LD_E_SHAPE, "s_max %d < seq %lld", c.s_max, static_cast<long long>(D.S));
   for (int32_t l = 0; l < n_layers; ++l) {
     if (active && !active[l]) continue;
@@ -1778,6 +2005,12 @@ int stack_eval(const ld_config* cfg, int32_t n_layers, const ld_weights* w, cons
       if (int rc = check_kv8_layer(D, &c.kv8[l], l, &v)) return rc;
       if (c.kv8[l].s_max < D.S)
         return fail(LD_E_SHAPE, "kv[%d]: s_max %d < seq %lld", l, c.kv8[l].s_max, static_cast<long long>(D.S));
+    }
+    if (c.kv4) {
+      Kv4View v;
+      if (int rc = check_kv4_layer(D, &c.kv4[l], l, &v)) return rc;
+      if (c.kv4[l].s_max < D.S)
+        return fail(LD_E_SHAPE, "kv[%d]: s_max %d < seq %lld", l, c.kv4[l].s_max, static_cast<long long>(D.S));
     }
   }
   const ActLayout al = act_layout(D);
@@ -1791,8 +2024,11 @@ int stack_eval(const ld_config* cfg, int32_t n_layers, const ld_weights* w, cons
     Kv8View v;
     if (c.kv8)
       if (int rc = check_kv8_layer(D, &c.kv8[l], l, &v)) return rc;
+    Kv4View v4;
+    if (c.kv4)
+      if (int rc = check_kv4_layer(D, &c.kv4[l], l, &v4)) return rc;
     if (int rc = attn_forward_part(cfg, D, w[l], mv, act, xs, D.B, false, s, c.kv ? c.kv[l] : nullptr, c.s_max,
-                                   c.kv8 ? &v : nullptr))
+                                   c.kv8 ? &v : nullptr, c.kv4 ? &v4 : nullptr))
       return rc;
     if (int rc = ffn_forward_part(cfg, D, w[l], mv, act, xs, D.B, false, s)) return rc;
   }
@@ -1807,14 +2043,21 @@ int ld_stack_eval(const ld_config* cfg, int32_t n_layers, const ld_weights* w, c
                   const float* r_eval, void* x, void* const* kv, int32_t s_max, void* ws,
                   size_t ws_bytes, void* stream) {
   t_err.clear();
-  return stack_eval(cfg, n_layers, w, active, r_eval, x, {kv, s_max, nullptr}, ws, ws_bytes, stream);
+  return stack_eval(cfg, n_layers, w, active, r_eval, x, {kv, s_max, nullptr, nullptr}, ws, ws_bytes, stream);
 }
 
 int ld_stack_eval_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
                       const float* r_eval, void* x, const ld_kv8* kv, void* ws, size_t ws_bytes, void* stream) {
   t_err.clear();
   if (!kv) return fail(LD_E_INVALID, "NULL kv");
-  return stack_eval(cfg, n_layers, w, active, r_eval, x, {nullptr, 0, kv}, ws, ws_bytes, stream);
+  return stack_eval(cfg, n_layers, w, active, r_eval, x, {nullptr, 0, kv, nullptr}, ws, ws_bytes, stream);
+}
+
+int ld_stack_eval_kv4(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
+                      const float* r_eval, void* x, const ld_kv4* kv, void* ws, size_t ws_bytes, void* stream) {
+  t_err.clear();
+  if (!kv) return fail(LD_E_INVALID, "NULL kv");
+  return stack_eval(cfg, n_layers, w, active, r_eval, x, {nullptr, 0, nullptr, kv}, ws, ws_bytes, stream);
 }
 
 size_t ld_decode_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max) {
@@ -1833,28 +2076,41 @@ size_t ld_decode_kv8_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max
   return dec_bytes(D, n_new, [&](int32_t n) { return kv8_part_rows(v, D.H, n); });
 }
 
+size_t ld_decode_kv4_ws_bytes(const ld_config* cfg, int32_t n_new, int32_t s_max, int32_t sums) {
+  Dims D;
+  if (check_cfg(cfg, &D) || n_new < 1 || n_new > kDecMaxRows || s_max < 1 || (sums != 0 && sums != 1)) return 0;
+  const ld_kv4 kv{static_cast<int32_t>(D.B), static_cast<int32_t>(D.H), static_cast<int32_t>(D.dh), s_max,
+                  nullptr, nullptr, nullptr};
+  Kv4View v;
+  if (check_kv4(&kv, &v)) return 0;
+  return dec_bytes(D, n_new, [&](int32_t n) { return kv4_part_rows(v, D.H, n); },
+                   sums ? attn_kv4_score_keys(v.s8) : 0, true);
+}
+
 }  // extern "C"
 
 namespace {
 
+// w4: the layers' weights in 4 bits, w being null.
 int stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
                  const float* r_eval, void* x, const StackCaches& c, int32_t pos, const int32_t* seq_pos,
-                 int32_t n_new, void* ws, size_t ws_bytes, void* stream) {
+                 int32_t n_new, void* ws, size_t ws_bytes, void* stream, const ld_weights_w4* w4 = nullptr) {
   Dims D;
   if (int rc = check_cfg(cfg, &D)) return rc;
   if (D.dtype != LD_BF16) return fail(LD_E_UNSUPPORTED, "decoding is bf16 only");
   if (n_layers < 1 || n_layers > 1024) return fail(LD_E_INVALID, "n_layers outside [1, 1024]");
-  if (!w || !x || (!c.kv && !c.kv8) || !ws) return fail(LD_E_INVALID, "NULL pointer");
+  if ((!w && !w4) || !x || (!c.kv && !c.kv8 && !c.kv4) || !ws) return fail(LD_E_INVALID, "NULL pointer");
   if (n_new < 1 || n_new > kDecMaxRows) return fail(LD_E_INVALID, "n_new outside [1, %d]", kDecMaxRows);
   if (pos < 0) return fail(LD_E_SHAPE, "pos %d < 0", pos);
   if (reinterpret_cast<uintptr_t>(seq_pos) & 3) return fail(LD_E_INVALID, "seq_pos must be 4-byte aligned");
   size_t part_rows = c.kv ? dec_part_rows(D, std::max(c.s_max, 1)) : 0;
+  int64_t score_keys = 0;
   auto inside = [&](int32_t s_max) { return s_max >= 1 && static_cast<int64_t>(pos) + n_new <= s_max; };
   if (c.kv && !inside(c.s_max))
     return fail(LD_E_SHAPE, "positions %d..%d outside the cache of %d", pos, pos + n_new - 1, c.s_max);
   for (int32_t l = 0; l < n_layers; ++l) {
     if (active && !active[l]) continue;
-    if (int rc = check_weights(&w[l])) return rc;
+    if (int rc = w4 ? check_weights_w4(D, w4[l], l) : check_weights(&w[l])) return rc;
     if (r_eval && !std::isfinite(r_eval[l])) return fail(LD_E_INVALID, "r_eval[%d] not finite", l);
     if (c.kv && !c.kv[l]) return fail(LD_E_INVALID, "kv[%d] is NULL for an active layer", l);
     if (c.kv8) {
@@ -1865,8 +2121,17 @@ int stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w, co
                     c.kv8[l].s_max);
       part_rows = std::max(part_rows, kv8_part_rows(v, D.H, n_new));
     }
+    if (c.kv4) {
+      Kv4View v;
+      if (int rc = check_kv4_layer(D, &c.kv4[l], l, &v)) return rc;
+      if (!inside(c.kv4[l].s_max))
+        return fail(LD_E_SHAPE, "positions %d..%lld outside kv[%d] of %d", pos, static_cast<long long>(pos) + n_new - 1, l,
+                    c.kv4[l].s_max);
+      part_rows = std::max(part_rows, kv4_part_rows(v, D.H, n_new));
+      if (v.sums) score_keys = std::max(score_keys, attn_kv4_score_keys(v.s8));
+    }
   }
-  const DecLayout L = dec_layout(D, n_new, part_rows);
+  const DecLayout L = dec_layout(D, n_new, part_rows, score_keys, w4 != nullptr);
   if (ws_bytes < L.total) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, L.total);
   hipStream_t s = as_stream(stream);
   char* base = static_cast<char*>(ws);
@@ -1893,20 +2158,36 @@ int stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w, co
   // GEMMs whose partial sums are reduced together with what follows them, the
   // residual and the next RMSNorm (output and down projections) or the FFN
   // activation.  Else (more than 64 rows) the general GEMM.
-  const bool part_fused = dec_split_k(M, d), fused = !part_fused && dec_gemm_fuses_norm(M, d);
+  // 4-bit weights: a launch per projection, with the norm of its rows where they are few.
+  const bool part_fused = !w4 && dec_split_k(M, d), fused = !w4 && !part_fused && dec_gemm_fuses_norm(M, d);
+  const bool norm_w4 = w4 && w4_gemm_fuses_norm(M, d);
   float* skp = reinterpret_cast<float*>(base + L.skp);
   bool h_ready = false;  // L.h holds RMSNorm(x) with this layer's gain
   const int act = D.kind == LD_BLOCK_SWIGLU ? kDecActSwiglu : kDecActRelu2;
   for (int32_t l = 0; l < n_layers; ++l) {
     if (active && !active[l]) continue;
     const float r = r_eval ? r_eval[l] : 1.f;
-    const ld_weights& wl = w[l];
+    const ld_weights wl = w ? w[l] : ld_weights{w4[l].g_attn, nullptr, nullptr, w4[l].g_mlp, nullptr, nullptr};
+    // rows A (their norm with gain g) by 4-bit weights
+    auto proj_w4 = [&](const ld_w4& of, const void* A, int64_t K, const void* g, void* C, const void* R, int64_t N, float alpha,
+                       int act_of) {
+      W4View v;
+      if (int rc = check_w4_buffers(&of, &v)) return rc;
+      if (g && !norm_w4) {
+        if (int rc = norm(A, g)) return rc;
+        A = P(L.h);
+        g = nullptr;
+      }
+      return run_gemm_w4(v, A, K, g, cfg->rms_eps, C, N, R, N, M, N, alpha, act_of, skp, s);
+    };
     // h = RMSNorm(x); qkv = h W_qkv^T; new keys/values into the cache
     const KvOut ko{c.kv ? c.kv[l] : nullptr, static_cast<int32_t>(d), n_new, c.s_max, pos};
-    if (!fused && !h_ready)
+    if (!w4 && !fused && !h_ready)
       if (int rc = norm(x, wl.g_attn)) return rc;
     h_ready = false;
-    if (fused) {
+    if (w4) {
+      if (int rc = proj_w4(w4[l].w_qkv, x, d, wl.g_attn, P(L.qkv), nullptr, 3 * d, 1.f, kDecActNone)) return rc;
+    } else if (fused) {
       if (int rc = dec_proj(x, d, wl.g_attn, cfg->rms_eps, wl.w_qkv, d, P(L.qkv), 3 * d, nullptr, 0, M, 3 * d, d, 1.f,
                             kDecActNone, s, c.kv ? &ko : nullptr))
         return rc;
@@ -1948,6 +2229,14 @@ int stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w, co
       if (int rc = check_kv8_layer(D, &c.kv8[l], l, &v)) return rc;
       if (int rc = run_kv8_store(v, P(L.qkv), H, n_new, pos, seq_pos, s)) return rc;
       if (int rc = run_kv8_attn(v, P(L.qkv), P(L.att), part_o, part_ml, H, alibi, n_new, pos, seq_pos, s)) return rc;
+    } else if (c.kv4) {
+      Kv4View v;
+      const int32_t H = static_cast<int32_t>(D.H);
+      if (int rc = check_kv4_layer(D, &c.kv4[l], l, &v)) return rc;
+      if (int rc = run_kv4_store(v, P(L.qkv), H, n_new, pos, seq_pos, s)) return rc;
+      if (int rc = run_kv4_attn(v, P(L.qkv), P(L.att), part_o, part_ml, reinterpret_cast<float*>(base + L.scores),
+                                reinterpret_cast<float*>(base + L.row_ml), H, alibi, n_new, pos, seq_pos, s))
+        return rc;
     } else {
       DecAttnArgs at{};
       at.qkv = P(L.qkv);
@@ -1972,6 +2261,13 @@ int stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w, co
       }
     }
     // z = x + r (att W_o^T); h = RMSNorm(z); uv = h W_gate_up^T; s = act(uv)
+    if (w4) {
+      if (int rc = proj_w4(w4[l].w_o, P(L.att), d, nullptr, P(L.z), x, d, r, kDecActNone)) return rc;
+      if (int rc = proj_w4(w4[l].w_gate_up, P(L.z), d, wl.g_mlp, P(L.s), nullptr, D.f, 1.f, act)) return rc;
+      // x = z + r (s W_down^T)
+      if (int rc = proj_w4(w4[l].w_down, P(L.s), D.f, nullptr, x, P(L.z), d, r, kDecActNone)) return rc;
+      continue;
+    }
     if (fused) {
       if (int rc = dec_proj(P(L.att), d, nullptr, 0.f, wl.w_o, d, P(L.z), d, x, d, M, d, d, r, kDecActNone, s))
         return rc;
@@ -2042,7 +2338,7 @@ int ld_stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w,
                     const float* r_eval, void* x, void* const* kv, int32_t s_max, int32_t pos,
                     int32_t n_new, void* ws, size_t ws_bytes, void* stream) {
   t_err.clear();
-  return stack_decode(cfg, n_layers, w, active, r_eval, x, {kv, s_max, nullptr}, pos, nullptr, n_new, ws, ws_bytes,
+  return stack_decode(cfg, n_layers, w, active, r_eval, x, {kv, s_max, nullptr, nullptr}, pos, nullptr, n_new, ws, ws_bytes,
                       stream);
 }
 
@@ -2050,7 +2346,26 @@ int ld_stack_decode_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights
                         const float* r_eval, void* x, const ld_kv8* kv, int32_t pos, const int32_t* seq_pos,
                         int32_t n_new, void* ws, size_t ws_bytes, void* stream) {
   t_err.clear();
-  return stack_decode(cfg, n_layers, w, active, r_eval, x, {nullptr, 0, kv}, pos, seq_pos, n_new, ws, ws_bytes, stream);
+  return stack_decode(cfg, n_layers, w, active, r_eval, x, {nullptr, 0, kv, nullptr}, pos, seq_pos, n_new, ws, ws_bytes,
+                      stream);
+}
+
+int ld_stack_decode_kv4(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
+                        const float* r_eval, void* x, const ld_kv4* kv, int32_t pos, const int32_t* seq_pos,
+                        int32_t n_new, void* ws, size_t ws_bytes, void* stream) {
+  t_err.clear();
+  if (!w) return fail(LD_E_INVALID, "NULL pointer");
+  return stack_decode(cfg, n_layers, w, active, r_eval, x, {nullptr, 0, nullptr, kv}, pos, seq_pos, n_new, ws, ws_bytes,
+                      stream);
+}
+
+int ld_stack_decode_w4(const ld_config* cfg, int32_t n_layers, const ld_weights_w4* w, const uint8_t* active,
+                       const float* r_eval, void* x, const ld_kv4* kv, int32_t pos, const int32_t* seq_pos,
+                       int32_t n_new, void* ws, size_t ws_bytes, void* stream) {
+  t_err.clear();
+  if (!w) return fail(LD_E_INVALID, "NULL pointer");
+  return stack_decode(cfg, n_layers, nullptr, active, r_eval, x, {nullptr, 0, nullptr, kv}, pos, seq_pos, n_new, ws, ws_bytes,
+                      stream, w);
 }
 
 // ------------------------------------------------------ kernel-level calls
@@ -2354,6 +2669,213 @@ int ld_attn_decode_kv8(const ld_kv8* kv, int32_t n_heads, int32_t alibi, int32_t
   float* part_o = static_cast<float*>(ws);
   float* part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + up(4 * kv8_part_rows(v, n_heads, n_new) * v.dh));
   return run_kv8_attn(v, qkv, o, part_o, part_ml, n_heads, alibi, n_new, pos, seq_pos, as_stream(stream));
+}
+
+size_t ld_w4_code_bytes(const ld_w4* w) {
+  W4View v;
+  if (check_w4(w, &v)) return 0;
+  return static_cast<size_t>((v.N + 7ll) / 8) * ((v.K + 255ll) / 256) * 1024;
+}
+
+size_t ld_w4_scale_bytes(const ld_w4* w) {
+  W4View v;
+  if (check_w4(w, &v)) return 0;
+  return static_cast<size_t>((v.N + 7ll) / 8) * ((v.K + 255ll) / 256) * 16 * (128 / v.group) * (v.format == LD_W4_E2M1 ? 1 : 2);
+}
+
+}  // extern "C"
+
+namespace {
+
+int w4_convert(const ld_w4* w, const void* src, void* dst, int32_t ld, void* stream) {
+  W4PackArgs a{};
+  if (int rc = check_w4_buffers(w, &a.w)) return rc;
+  const void* rows = src ? src : dst;
+  if (!rows) return fail(LD_E_INVALID, "NULL pointer");
+  if (reinterpret_cast<uintptr_t>(rows) & 15) return fail(LD_E_INVALID, "rows must be 16-byte aligned");
+  if (ld < a.w.K || ld % 8) return fail(LD_E_SHAPE, "ld must be a multiple of 8, at least k");
+  a.src = src;
+  a.dst = dst;
+  a.ld = ld;
+  const char* name = src ? "ld_w4_pack_k" : "ld_w4_load_k";
+  ProfScope ps(name, as_stream(stream));
+  const hipError_t e = src ? launch_w4_pack(a, as_stream(stream)) : launch_w4_load(a, as_stream(stream));
+  if (e != hipSuccess) return fail(LD_E_HIP, "%s: %s", name, hipGetErrorString(e));
+  ps.end(0, 2.5 * a.w.N * a.w.K);
+  return LD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ld_w4_pack(const ld_w4* w, const void* src, int32_t ld, void* stream) {
+  t_err.clear();
+  return w4_convert(w, src, nullptr, ld, stream);
+}
+
+int ld_w4_load(const ld_w4* w, void* dst, int32_t ld, void* stream) {
+  t_err.clear();
+  return w4_convert(w, nullptr, dst, ld, stream);
+}
+
+size_t ld_gemm_w4_ws_bytes(const ld_w4* w, int32_t M, int32_t act) {
+  W4View v;
+  if (check_w4(w, &v) || M < 1 || M > kW4MaxM || act < kDecActNone || act > kDecActRelu2) return 0;
+  size_t most = 0;
+  for (int32_t m = 1; m <= M; ++m) most = std::max(most, w4_gemm_ws_bytes(m, v.N, v.K, act));
+  return most;
+}
+
+int ld_gemm_w4(int32_t M, const void* A, int32_t lda, const void* g, float eps, const ld_w4* w, void* C, int32_t ldc,
+               float alpha, const void* R, int32_t ldr, int32_t act, void* ws, size_t ws_bytes, void* stream) {
+  t_err.clear();
+  W4View v;
+  if (int rc = check_w4_buffers(w, &v)) return rc;
+  if (M < 1 || M > kW4MaxM) return fail(LD_E_SHAPE, "M outside [1, %d]", kW4MaxM);
+  if (act != kDecActNone && act != kDecActSwiglu && act != kDecActRelu2) return fail(LD_E_INVALID, "unknown act");
+  if (act != kDecActNone && R) return fail(LD_E_INVALID, "a residual only without activation");
+  if (act == kDecActSwiglu && v.N % 16) return fail(LD_E_SHAPE, "SwiGLU needs n / 2 to be a multiple of 8");
+  const int32_t N = act == kDecActSwiglu ? v.N / 2 : v.N;
+  if (g && !w4_gemm_fuses_norm(M, v.K)) return fail(LD_E_UNSUPPORTED, "no norm of M = %d rows of %d", M, v.K);
+  if (lda < v.K || ldc < N || (R && ldr < N)) return fail(LD_E_SHAPE, "leading dimension too small");
+  if (lda % 8) return fail(LD_E_SHAPE, "lda must be a multiple of 8");
+  if (!A || !C) return fail(LD_E_INVALID, "NULL pointer");
+  if ((reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(g)) & 15)
+    return fail(LD_E_INVALID, "A and g must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(C) | reinterpret_cast<uintptr_t>(R)) & 1)
+    return fail(LD_E_INVALID, "C and R must be 2-byte aligned");
+  if (!std::isfinite(alpha)) return fail(LD_E_INVALID, "alpha not finite");
+  if (g && !(eps > 0.f)) return fail(LD_E_INVALID, "eps must be > 0");
+  const size_t need = w4_gemm_ws_bytes(M, v.N, v.K, act);
+  if (need && (!ws || ws_bytes < need)) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+  if (need && (reinterpret_cast<uintptr_t>(ws) & 15)) return fail(LD_E_INVALID, "ws must be 16-byte aligned");
+  return run_gemm_w4(v, A, lda, g, eps, C, ldc, R, ldr, M, N, alpha, act, static_cast<float*>(ws), as_stream(stream));
+}
+
+size_t ld_kv4_code_bytes(const ld_kv4* kv) {
+  Kv4View v;
+  return check_kv4(kv, &v) ? 0 : kv4_code_bytes(v);
+}
+
+size_t ld_kv4_scale_bytes(const ld_kv4* kv) {
+  Kv4View v;
+  return check_kv4(kv, &v) ? 0 : kv4_scale_bytes(v);
+}
+
+int ld_kv4_store(const ld_kv4* kv, int32_t n_heads, int32_t n_new, int32_t pos, const int32_t* seq_pos,
+                 const void* qkv, void* stream) {
+  t_err.clear();
+  Kv4View v;
+  if (int rc = check_kv4_buffers(kv, &v)) return rc;
+  if (int rc = check_kv4_rows(kv, n_heads, n_new, pos, qkv, seq_pos)) return rc;
+  return run_kv4_store(v, qkv, n_heads, n_new, pos, seq_pos, as_stream(stream));
+}
+
+int ld_kv4_load(const ld_kv4* kv, int32_t pos, int32_t n, const int32_t* seq_len, void* out, void* stream) {
+  t_err.clear();
+  Kv4LoadArgs a{};
+  if (int rc = check_kv4_buffers(kv, &a.kv)) return rc;
+  if (n < 1) return fail(LD_E_SHAPE, "n must be >= 1");
+  if (pos < 0 || static_cast<int64_t>(pos) + n > kv->s_max) return fail(LD_E_SHAPE, "positions outside the cache");
+  if (!out) return fail(LD_E_INVALID, "NULL pointer");
+  if (reinterpret_cast<uintptr_t>(out) & 15) return fail(LD_E_INVALID, "out must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(seq_len) & 3) return fail(LD_E_INVALID, "seq_len must be 4-byte aligned");
+  a.out = out;
+  a.pos = pos;
+  a.n = n;
+  a.seq_len = seq_len;
+  ProfScope ps("ld_kv4_load_k", as_stream(stream));
+  hipError_t e = launch_kv4_load(a, as_stream(stream));
+  if (e != hipSuccess) return fail(LD_E_HIP, "kv4 load: %s", hipGetErrorString(e));
+  ps.end(0, seq_len ? 0.0 : 2.0 * kv->n_seq * n * kv->n_kv_heads * kv->d_head * (2 + 17.0 / 32));
+  return LD_OK;
+}
+
+size_t ld_attn_decode_kv4_ws_bytes(const ld_kv4* kv, int32_t n_heads, int32_t n_new) {
+  Kv4View v;
+  if (check_kv4(kv, &v) || check_kv4_heads(kv, n_heads) || n_new < 1 || n_new > kDecMaxRows) return 0;
+  // fewer rows may take more: in fewer row tiles there is room for more chunks
+  size_t most = 0;
+  for (int32_t n = 1; n <= n_new; ++n) most = std::max(most, kv4_scratch(v, n_heads, n).total);
+  return most;
+}
+
+int ld_attn_decode_kv4(const ld_kv4* kv, int32_t n_heads, int32_t alibi, int32_t pos, const int32_t* seq_pos,
+                       int32_t n_new, const void* qkv, void* o, void* ws, size_t ws_bytes, void* stream) {
+  t_err.clear();
+  Kv4View v;
+  if (int rc = check_kv4_buffers(kv, &v)) return rc;
+  if (n_new < 1 || n_new > kDecMaxRows) return fail(LD_E_INVALID, "n_new outside [1, %d]", kDecMaxRows);
+  if (alibi != 0 && alibi != 1) return fail(LD_E_INVALID, "alibi must be 0 or 1");
+  if (int rc = check_kv4_rows(kv, n_heads, n_new, pos, qkv, seq_pos)) return rc;
+  if (!o || !ws) return fail(LD_E_INVALID, "NULL pointer");
+  if (reinterpret_cast<uintptr_t>(o) & 1) return fail(LD_E_INVALID, "o must be 2-byte aligned");
+  if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(LD_E_INVALID, "ws must be 16-byte aligned");
+  const Kv4Scratch t = kv4_scratch(v, n_heads, n_new);
+  if (ws_bytes < t.total) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, t.total);
+  char* base = static_cast<char*>(ws);
+  auto at = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
+  return run_kv4_attn(v, qkv, o, at(0), at(t.part_ml), at(t.scores), at(t.row_ml), n_heads, alibi, n_new, pos, seq_pos,
+                      as_stream(stream));
+}
+
+size_t ld_kv4_evict_ws_bytes(const ld_kv4* from, int32_t len, int32_t keep) {
+  Kv4View v;
+  if (check_kv4(from, &v) || len < 1 || len > from->s_max || keep < 1) return 0;
+  return kv4_evict_ws_bytes(v, len, keep);
+}
+
+int ld_kv4_evict(const ld_kv4* from, const ld_kv4* to, int32_t len, const int32_t* seq_len, int32_t keep,
+                 int32_t recent, int32_t* idx, void* ws, size_t ws_bytes, void* stream) {
+  t_err.clear();
+  Kv4EvictArgs a{};
+  if (int rc = check_kv4_buffers(from, &a.from)) return rc;
+  if (int rc = check_kv4_buffers(to, &a.to)) return rc;
+  if (!from->sums) return fail(LD_E_INVALID, "from has no sums");
+  if (from->n_seq != to->n_seq || from->n_kv_heads != to->n_kv_heads || from->d_head != to->d_head)
+    return fail(LD_E_SHAPE, "from and to differ in n_seq, n_kv_heads or d_head");
+  if (len < 1 || len > from->s_max) return fail(LD_E_SHAPE, "len outside [1, %d]", from->s_max);
+  if (keep < 1 || keep > to->s_max) return fail(LD_E_SHAPE, "keep outside [1, %d]", to->s_max);
+  if (recent < 0 || recent > keep) return fail(LD_E_SHAPE, "recent outside [0, %d]", keep);
+  if (!idx) return fail(LD_E_INVALID, "NULL pointer");
+  if ((reinterpret_cast<uintptr_t>(idx) | reinterpret_cast<uintptr_t>(seq_len)) & 3)
+    return fail(LD_E_INVALID, "idx and seq_len must be 4-byte aligned");
+  struct Span {
+    const void* p;
+    size_t n;
+  };
+  const Span fs[3] = {{from->codes, kv4_code_bytes(a.from)}, {from->scales, kv4_scale_bytes(a.from)},
+                      {from->sums, kv4_sum_bytes(a.from)}};
+  const Span ts[3] = {{to->codes, kv4_code_bytes(a.to)}, {to->scales, kv4_scale_bytes(a.to)},
+                      {to->sums, to->sums ? kv4_sum_bytes(a.to) : 0}};
+  for (const Span& f : fs)
+    for (const Span& t : ts) {
+      const uintptr_t x = reinterpret_cast<uintptr_t>(f.p), y = reinterpret_cast<uintptr_t>(t.p);
+      if (t.n && x < y + t.n && y < x + f.n) return fail(LD_E_INVALID, "from and to share memory");
+    }
+  a.len = len;
+  a.keep = keep;
+  a.recent = recent;
+  a.seq_len = seq_len;
+  a.idx = idx;
+  const size_t need = kv4_evict_ws_bytes(a.from, len, keep);
+  if (need && (!ws || ws_bytes < need)) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+  if (need && (reinterpret_cast<uintptr_t>(ws) & 15)) return fail(LD_E_INVALID, "ws must be 16-byte aligned");
+  a.ws = static_cast<uint32_t*>(ws);
+  hipStream_t s = as_stream(stream);
+  const double heads = static_cast<double>(from->n_seq) * from->n_kv_heads, known = seq_len ? 0.0 : 1.0;
+  const double kept = heads * std::min(len, keep);
+  hipError_t e;
+  {
+    ProfScope ps("ld_kv4_select_k", s);
+    if ((e = launch_kv4_select(a, s)) != hipSuccess) return fail(LD_E_HIP, "kv4 select: %s", hipGetErrorString(e));
+    ps.end(0, known * (4.0 * heads * len + 4.0 * kept));
+  }
+  ProfScope pg("ld_kv4_gather_k", s);
+  if ((e = launch_kv4_gather(a, s)) != hipSuccess) return fail(LD_E_HIP, "kv4 gather: %s", hipGetErrorString(e));
+  pg.end(0, known * kept * (from->d_head * 17.0 / 8 + 12.0));
+  return LD_OK;
 }
 
 size_t ld_gemm_ws_bytes(int32_t dtype, int32_t a_kcontig, int32_t b_kcontig, int32_t M, int32_t N,

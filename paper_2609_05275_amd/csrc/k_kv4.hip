@@ -1,0 +1,917 @@
+// Kernels of the 4-bit key/value cache: quantising writer, reader, the attention
+// of a few new rows per sequence over it with the positions' summed weights, and
+// the eviction by those.  Layout and the meaning of codes and scales: Kv4View in
+// ld_kv4.h, ld_kv4 in layerdrop.h.
+//
+// A code is a 4-bit float (sign, two bits of exponent, one of mantissa), its scale a
+// power of two for 32 neighbouring dimensions of one position.  Both are what
+// v_cvt_scalef32_pk_bf16_fp4 takes: two codes to two bf16, exact, in one instruction.
+#include "ld_kv4.h"
+
+namespace ld {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kKv4Waves = 8;  // of an attention workgroup
+constexpr int kKv4Parts = 3;  // bf16 parts of a weight, 8 of its 24 bits each
+constexpr int kCus = 256;
+constexpr uint32_t kNanScale = 255;
+constexpr int kKv4MaxExp = 125;  // 6 2^125 is finite
+
+// ------------------------------------------------------------- conversions
+
+// The scale in byte b of w as the conversions take it: they look at a float's
+// exponent alone, so the neighbours' bits may stay where sign and mantissa are.
+template <int B>
+__device__ __forceinline__ float scale_byte(uint32_t w) {
+  return __builtin_bit_cast(float, B == 0 ? w << 23 : B == 1 ? w << 15 : B == 2 ? w << 7 : w >> 1);
+}
+
+// Two codes of byte B times a scale.
+template <int B>
+__device__ __forceinline__ bf16x2 pair_of(uint32_t w, float scale) {
+  return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B);
+}
+
+// Eight codes of one scale.
+__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t w, float scale) {
+  union {
+    bf16x8 v;
+    bf16x2 p[4];
+  } r;
+  r.p[0] = pair_of<0>(w, scale);
+  r.p[1] = pair_of<1>(w, scale);
+  r.p[2] = pair_of<2>(w, scale);
+  r.p[3] = pair_of<3>(w, scale);
+  return r.v;
+}
+
+// Eight values divided by a scale, to codes: nearest, ties to even, 6 at most.
+__device__ __forceinline__ uint32_t bf16_to_codes(bf16x8 v, float scale) {
+  union {
+    bf16x8 v;
+    bf16x2 p[4];
+  } x;
+  x.v = v;
+  uint32_t r = 0;
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, x.p[0], scale, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, x.p[1], scale, 1);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, x.p[2], scale, 2);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, x.p[3], scale, 3);
+  return r;
+}
+
+// The scale's byte that a largest absolute value (bf16 bits) needs.
+__device__ __forceinline__ uint32_t scale_needed(uint32_t amax) {
+  if (amax >= 0x7f80u) return kNanScale;
+  // 6 = 1.5 2^2
+  const int e = static_cast<int>(amax >> 7) - 127 - 2 + ((amax & 0x7fu) > 0x40u ? 1 : 0);
+  return static_cast<uint32_t>(min(max(e, kKv4MinExp), kKv4MaxExp) + 127);  // zeros and subnormals too
+}
+
+// The low 16 bits' nibbles to bytes.
+__device__ __forceinline__ uint32_t spread4(uint32_t x) {
+  x = (x | (x << 8)) & 0x00ff00ffu;
+  return (x | (x << 4)) & 0x0f0f0f0fu;
+}
+// Bytes' low nibbles to the low 16 bits.
+__device__ __forceinline__ uint32_t gather4(uint32_t x) {
+  x &= 0x0f0f0f0fu;
+  x = (x | (x >> 4)) & 0x00ff00ffu;
+  return (x | (x >> 8)) & 0xffffu;
+}
+
+// ---------------------------------------------------------- store and load
+
+// A wave takes a unit of U = 8 positions (16 for heads of 64) of one head's keys or
+// values.  Lane l has dimensions 16 (l % PT) .. + 15 of row l / PT, PT = DH / 16: half a
+// scale's dimensions, so that a neighbour holds the other nibbles of its values' bytes.
+template <int DH>
+struct Kv4Lanes {
+  static constexpr int PT = DH / 16, U = 64 / PT, TILES = U / 8, TB = DH * 4;  // TB: bytes of a tile of 8 values
+};
+
+struct Kv4Unit {
+  int b, piece, h, part;
+};
+__device__ __forceinline__ uint32_t kv4_workgroup() { return blockIdx.y * gridDim.x + blockIdx.x; }  // see kv4_grid
+// Piece number -> (sequence, piece of it, head, part), heads and parts first:
+// neighbours read neighbouring columns of the same rows.
+__device__ __forceinline__ Kv4Unit kv4_unit(uint32_t id, uint32_t KV, uint32_t pieces) {
+  const uint32_t head = id >> 1, at = head / KV;
+  return Kv4Unit{static_cast<int>(at / pieces), static_cast<int>(at % pieces), static_cast<int>(head % KV),
+                 static_cast<int>(id & 1)};
+}
+
+template <int DH>
+__global__ __launch_bounds__(256) void ld_kv4_store_k(Kv4StoreArgs a) {
+  using LN = Kv4Lanes<DH>;
+  constexpr int PT = LN::PT, U = LN::U, TB = LN::TB, JN = DH / 32;
+  __shared__ __align__(16) uint8_t lds[4][LN::TILES * TB];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Kv4View& c = a.kv;
+  const Kv4Unit w = kv4_unit(kv4_workgroup() * 4 + wave, c.KV, a.pieces);
+  if (w.b >= c.n_seq) return;
+  int lo = a.pos;
+  if (a.seq_pos) {
+    lo = a.seq_pos[w.b];
+    if (lo < 0 || lo > a.pos) return;
+  }
+  const int hi = lo + a.n, f = (lo / U + w.piece) * U;
+  if (f >= hi) return;
+  const int row = lane / PT, c16 = lane % PT, j = c16 >> 1, half = c16 & 1, t = f + row;
+  const bool in = t >= lo && t < hi;
+  const int64_t head = static_cast<int64_t>(w.b) * c.KV + w.h;
+  uint8_t* codes = c.codes + (head * 2 + w.part) * c.s8 * (DH / 2);
+  uint8_t* scales = c.scales + (head * 2 + w.part) * c.s8 * JN;
+
+  union Row {
+    bf16x8 v;
+    ushortx2 u[4];
+  } v[2];
+  v[0].v = v[1].v = static_cast<bf16>(0.f);
+  if (in) {
+    const bf16* src = static_cast<const bf16*>(a.qkv) + (static_cast<int64_t>(w.b) * a.n + t - lo) * a.ld_qkv +
+                      (a.H + w.part * c.KV + w.h) * static_cast<int64_t>(DH) + 16 * c16;
+    v[0].v = *reinterpret_cast<const bf16x8*>(src);
+    v[1].v = *reinterpret_cast<const bf16x8*>(src + 8);
+  }
+  ushortx2 m2{0, 0};
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m2 = __builtin_elementwise_max(m2, v[i].u[e] & static_cast<unsigned short>(0x7fff));
+  uint32_t mu = max(m2[0], m2[1]);
+  mu = max(mu, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mu), 1, 64)));
+  const uint32_t sb = scale_needed(mu);
+  const float s = __builtin_bit_cast(float, sb << 23);
+  // (a block of NaN scale: its codes are zeros)
+  uint32_t q0 = sb == kNanScale ? 0u : bf16_to_codes(v[0].v, s), q1 = sb == kNanScale ? 0u : bf16_to_codes(v[1].v, s);
+  if (in && half == 0) scales[static_cast<int64_t>(t) * JN + j] = static_cast<uint8_t>(sb);
+  if (w.part == 0) {
+    if (in) {
+      *reinterpret_cast<u32x2*>(codes + static_cast<int64_t>(t) * (DH / 2) + 8 * c16) = u32x2{q0, q1};
+      if (c.sums && c16 == 0) c.sums[head * c.s_max + t] = 0.f;
+    }
+    return;
+  }
+  // bytes n = 8 half + i: the even lane's dimension in the low nibble, the odd one's in the high
+  const uint32_t got = static_cast<uint32_t>(__shfl_xor(static_cast<int>(half ? q0 : q1), 1, 64));
+  const uint32_t ln = half ? got : q0, hn = half ? q1 : got;
+  const uint32_t b0 = spread4(ln & 0xffffu) | spread4(hn & 0xffffu) << 4, b1 = spread4(ln >> 16) | spread4(hn >> 16) << 4;
+  const int at = (row & 7) + 8 * j + 8 * half * 8 * JN;  // of byte 0 in its tile
+  const int tile = row >> 3, t0 = f + 8 * tile;
+  uint8_t* tb = codes + static_cast<int64_t>(t0 >> 3) * TB;
+  if (t0 < lo || t0 + 8 > hi) {  // no whole tile: the new bytes alone
+    if (in) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) tb[at + i * 8 * JN] = static_cast<uint8_t>((i < 4 ? b0 : b1) >> (8 * (i & 3)));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) lds[wave][tile * TB + at + i * 8 * JN] = static_cast<uint8_t>((i < 4 ? b0 : b1) >> (8 * (i & 3)));
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int tw = lane * 8 / TB, w0 = f + 8 * tw;  // the lane's tile of the way out
+  if (w0 >= lo && w0 + 8 <= hi)
+    *reinterpret_cast<u32x2*>(codes + static_cast<int64_t>(w0 >> 3) * TB + lane * 8 % TB) =
+        *reinterpret_cast<const u32x2*>(&lds[wave][lane * 8]);
+}
+
+// A wave takes a unit, lanes as in the store.
+template <int DH>
+__global__ __launch_bounds__(256) void ld_kv4_load_k(Kv4LoadArgs a) {
+  using LN = Kv4Lanes<DH>;
+  constexpr int PT = LN::PT, U = LN::U, TB = LN::TB, JN = DH / 32;
+  __shared__ __align__(16) uint8_t lds[4][LN::TILES * TB];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Kv4View& c = a.kv;
+  const Kv4Unit w = kv4_unit(kv4_workgroup() * 4 + wave, c.KV, a.pieces);
+  if (w.b >= c.n_seq) return;
+  const int f = (a.pos / U + w.piece) * U;
+  int hi = a.pos + a.n;
+  if (a.seq_len) hi = min(hi, a.seq_len[w.b]);
+  if (f >= hi) return;
+  const int row = lane / PT, c16 = lane % PT, j = c16 >> 1, half = c16 & 1, t = f + row;
+  const bool in = t >= a.pos && t < hi;
+  const int64_t head = static_cast<int64_t>(w.b) * c.KV + w.h;
+  const uint8_t* codes = c.codes + (head * 2 + w.part) * c.s8 * (DH / 2);
+  const uint8_t* scales = c.scales + (head * 2 + w.part) * c.s8 * JN;
+  const uint32_t sb = in ? scales[static_cast<int64_t>(t) * JN + j] : 0u;
+  uint32_t q0 = 0, q1 = 0;
+  if (w.part == 0) {
+    if (in) {
+      const u32x2 r = *reinterpret_cast<const u32x2*>(codes + static_cast<int64_t>(t) * (DH / 2) + 8 * c16);
+      q0 = r[0];
+      q1 = r[1];
+    }
+  } else {
+    u32x2 r{0, 0};
+    if (f + 8 * (lane * 8 / TB) < hi) r = *reinterpret_cast<const u32x2*>(codes + static_cast<int64_t>(f >> 3) * TB + lane * 8);
+    *reinterpret_cast<u32x2*>(&lds[wave][lane * 8]) = r;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const uint8_t* at = &lds[wave][(row >> 3) * TB + (row & 7) + 8 * j + 8 * half * 8 * JN];
+    uint32_t b0 = 0, b1 = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      b0 |= static_cast<uint32_t>(at[i * 8 * JN]) << (8 * i);
+      b1 |= static_cast<uint32_t>(at[(i + 4) * 8 * JN]) << (8 * i);
+    }
+    const uint32_t ln = gather4(b0) | gather4(b1) << 16, hn = gather4(b0 >> 4) | gather4(b1 >> 4) << 16;
+    const uint32_t got = static_cast<uint32_t>(__shfl_xor(static_cast<int>(half ? ln : hn), 1, 64));
+    q0 = half ? got : ln;
+    q1 = half ? hn : got;
+  }
+  if (!in) return;
+  const float s = __builtin_bit_cast(float, sb << 23);
+  const int64_t ld = 2ll * c.KV * DH;
+  bf16* out = static_cast<bf16*>(a.out) + (static_cast<int64_t>(w.b) * a.n + t - a.pos) * ld +
+              (static_cast<int64_t>(w.part) * c.KV + w.h) * DH + 16 * c16;
+  *reinterpret_cast<bf16x8*>(out) = codes_to_bf16(q0, s);
+  *reinterpret_cast<bf16x8*>(out + 8) = codes_to_bf16(q1, s);
+}
+
+// --------------------------------------------------------------- attention
+
+// Keys of a chunk of a sequence of nk: a.chunk_keys, and where lengths are the device's
+// more in a sequence that would make more than a.n_chunks of them.
+__device__ __forceinline__ int kv4_chunk_keys(const Kv4AttnArgs& a, int nk) {
+  if (!a.seq_pos) return a.chunk_keys;
+  const uint32_t n = a.n_chunks, even = ((static_cast<uint32_t>(nk) + n - 1) / n + 63) & ~63u;
+  return max(static_cast<int>(even), a.chunk_keys);
+}
+
+// A weight's bf16 parts, TT / 2 operands of 8 positions each.
+template <int TT>
+struct Kv4Parts {
+  bf16x8 p[kKv4Parts][TT / 2];
+  __device__ __forceinline__ void split(const floatx4 (&x)[TT]) {
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        floatx2 w{x[t][r], x[t][r + 1]};
+#pragma unroll
+        for (int i = 0; i < kKv4Parts; ++i) {
+          const bf16x2 part = __builtin_convertvector(w, bf16x2);
+          const uint32_t pb = __builtin_bit_cast(uint32_t, part);
+          w -= floatx2{__builtin_bit_cast(float, pb << 16), __builtin_bit_cast(float, pb & 0xffff0000u)};
+          p[i][t >> 1][4 * (t & 1) + r] = part[0];
+          p[i][t >> 1][4 * (t & 1) + r + 1] = part[1];
+        }
+      }
+  }
+};
+
+// A workgroup of eight waves takes a chunk of keys of one key/value head for 16
+// rows (of its query heads' new rows); a wave 16 TT keys at a time, with its own running
+// maximum and sum; they meet once, to add up.
+//
+// Scores S^T = K Q^T and output O^T = V^T P^T on the matrix cores (16x16x32
+// bf16).  The A rows of score product t are the keys LK g + 4 t + r (row 4 g + r), LK =
+// 4 TT, so lane group g = lane / 16 of the result holds keys LK g + 4 t + r, r < 4, of its
+// query row: LK neighbouring keys, whole tiles of the cache's values.  They are the B
+// operand of O^T as they stand.  A lane's k of the scores are DH / 4 neighbouring
+// dimensions, DH / 8 bytes of a key, of one scale.
+//
+// Values are converted in pairs of dimensions, which share position and scale, and put
+// together over positions by byte permutes.  A probability goes in as three bf16 parts,
+// which are all of its 24 bits.
+template <int DH, int NQ>
+__global__ __launch_bounds__(64 * kKv4Waves, 4) void ld_attn_decode_kv4_k(Kv4AttnArgs a) {
+  constexpr int NS = DH / 32, JN = DH / 32, MT = DH / 16, NW = kKv4Waves, TT = DH == 64 ? 4 : 2, LK = 4 * TT, WK = 16 * TT;
+  constexpr int VT = LK / 8, TB = DH * 4;  // value tiles a lane group; bytes of one
+  __shared__ float ml[NW][NQ][2];
+  __shared__ __align__(16) float red[NW][NQ][DH];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  const Kv4View& c = a.kv;
+  // Workgroups go round the 8 XCDs by their number.  Chunks are turned by the
+  // head, or a number of chunks that shares a factor with the XCDs' would leave
+  // those of the last chunks, which short sequences do not fill, with little to do.
+  // Several row tiles: a sequence's (head, chunk) go in sets of 8, a set's tiles one
+  // after the other, so that a chunk's tiles read it through one L2 at about one time.
+  const int b = blockIdx.z;
+  int h = blockIdx.y, chunk = blockIdx.x, r0 = 0;  // r0: the workgroup's first row
+  if (a.tiles > 1) {
+    const uint32_t nc = a.n_chunks, units = c.KV * nc, set = blockIdx.x / (8 * a.tiles), of = blockIdx.x % (8 * a.tiles);
+    const uint32_t n8 = min(units - 8 * set, 8u), unit = 8 * set + of % n8;
+    h = __builtin_amdgcn_readfirstlane(unit / nc);
+    chunk = __builtin_amdgcn_readfirstlane(unit % nc);
+    r0 = __builtin_amdgcn_readfirstlane(of / n8 * 16);
+  }
+  chunk = (chunk + h + b) % a.n_chunks;
+  const int G = a.group, R = G * a.n_new;
+  int p = a.pos;
+  if (a.seq_pos) {
+    p = a.seq_pos[b];
+    if (p < 0 || p > a.pos) p = -a.n_new;  // left out: no keys
+  }
+  const int nk = p + a.n_new, ck = kv4_chunk_keys(a, nk), k_first = chunk * ck;
+  const int rows = min(R - r0, 16);
+  const int64_t d = static_cast<int64_t>(a.H) * DH;
+  // where row r of the head goes in the output
+  auto out_at = [&](uint32_t r) {
+    return static_cast<bf16*>(a.out) + (static_cast<int64_t>(b) * a.n_new + r % static_cast<uint32_t>(a.n_new)) * d +
+           (h * G + r / static_cast<uint32_t>(a.n_new)) * static_cast<int64_t>(DH);
+  };
+  if (k_first >= nk) {
+    if (chunk == 0)  // left out: its rows are zeros
+      for (int e = tid; e < rows * DH; e += 64 * NW) out_at(r0 + e / DH)[e % DH] = static_cast<bf16>(0.f);
+    return;
+  }
+  const int k_end = min(k_first + ck, nk);
+  const int64_t head = static_cast<int64_t>(b) * c.KV + h;
+  const uint8_t* kc = c.codes + head * c.s8 * DH;
+  const uint8_t* vc = kc + static_cast<int64_t>(c.s8) * (DH / 2);
+  const uint8_t* ks = c.scales + head * 2 * c.s8 * JN;
+  const uint8_t* vs = ks + static_cast<int64_t>(c.s8) * JN;
+
+  // Keys k0 .. k0 + WK - 1 (past the last key: key 0, masked later): row n of
+  // product t, dimensions DH / 4 g + 0 .. DH / 4 - 1.
+  const int krow = LK * (n >> 2) + (n & 3);
+  typedef uint32_t KRaw __attribute__((ext_vector_type(NS)));
+  typedef uint32_t VRaw __attribute__((ext_vector_type(4)));
+  typedef uint32_t SRaw __attribute__((ext_vector_type(2 * JN)));
+  KRaw kr[TT];
+  uint32_t sk[TT];
+  union {
+    VRaw q[JN / 2];
+    uint32_t d[JN][2];  // [dimensions 32 j + n and 32 j + 16 + n][positions 0-3, 4-7]
+  } vr[VT];
+  union {
+    SRaw q;
+    uint32_t d[2 * JN];
+  } sv[VT];  // [position][j] bytes
+  auto load_keys = [&](int k0) {
+    const bool whole = k0 + WK <= nk;
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      int kk = k0 + krow + 4 * t;
+      if (!whole) kk = kk < nk ? kk : 0;
+      kr[t] = *reinterpret_cast<const KRaw*>(kc + static_cast<int64_t>(kk) * (DH / 2) + DH / 8 * g);
+      sk[t] = ks[static_cast<int64_t>(kk) * JN + (DH / 4 * g) / 32];
+    }
+  };
+  auto load_values = [&](int k0) {
+#pragma unroll
+    for (int v = 0; v < VT; ++v) {
+      const int f = k0 + LK * g + 8 * v, fc = f < nk ? f : 0;
+      const uint8_t* at = vc + static_cast<int64_t>(fc >> 3) * TB + n * (8 * JN);
+#pragma unroll
+      for (int i = 0; i < JN / 2; ++i) vr[v].q[i] = *reinterpret_cast<const VRaw*>(at + 16 * i);
+      sv[v].q = *reinterpret_cast<const SRaw*>(vs + static_cast<int64_t>(fc) * JN);
+    }
+  };
+
+  const uint32_t row = r0 + min(n, rows - 1), j = row % static_cast<uint32_t>(a.n_new);
+  const int qh = h * G + row / static_cast<uint32_t>(a.n_new), qpos = p + j;
+  bf16x8 qf[NS];
+  {
+    const bf16* q = static_cast<const bf16*>(a.qkv) + (static_cast<int64_t>(b) * a.n_new + j) * a.ld_qkv +
+                    static_cast<int64_t>(qh) * DH;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(q + DH / 4 * g + 8 * s);
+  }
+  const float al2 = a.alibi ? alibi_slope(qh, a.H) * kLog2e : 0.f, sl2 = a.scale * kLog2e;
+
+  float m = -INFINITY, l = 0.f;
+  floatx4 o[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  for (int k0 = k_first + wave * WK; k0 < k_end; k0 += WK * NW) {
+    load_keys(k0);
+    load_values(k0);
+    __builtin_amdgcn_sched_barrier(0);
+    const int f = k0 + LK * g;  // the lane's keys
+    float ss = sl2;             // of a product to a base-2 score
+    floatx4 x[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      x[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+      const float s = scale_byte<0>(sk[t]);
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+        x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(kr[t][i], s), qf[i], x[t], 0, 0, 0);
+    }
+    if (a.alibi) {
+      const float far = al2 * static_cast<float>(qpos - f);
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          x[t][r] = __builtin_fmaf(x[t][r], ss, __builtin_fmaf(al2, static_cast<float>(4 * t + r), -far));
+      ss = 1.f;
+    }
+    const bool cut = k0 + WK - 1 > p;  // some of the keys may be behind a row, or behind the last one
+    if (cut) {
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (f + 4 * t + r > qpos) x[t][r] = -INFINITY;
+    }
+    if (a.scores && n < rows) {
+      float* sc = a.scores + (head * R + r0 + n) * a.score_keys + f;
+#pragma unroll
+      for (int t = 0; t < TT; ++t) *reinterpret_cast<floatx4*>(sc + 4 * t) = x[t] * ss;
+    }
+    // the largest score: of the lane's products (their scale is positive), then of all
+    float mn = x[0][0];
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mn = fmaxf(mn, x[t][r]);
+    mn = fmaxf(m, mn * ss);
+    mn = fmaxf(mn, __shfl_xor(mn, 16, 64));
+    mn = fmaxf(mn, __shfl_xor(mn, 32, 64));
+    const float mz = mn == -INFINITY ? 0.f : mn;  // of nothing but -inf, whose weights are 0
+    if (__any(mn != m)) {
+      const float keep = __builtin_amdgcn_exp2f(m - mz);
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) o[i] *= keep;
+    }
+    m = mn;
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], ss, -mz));  // of a NaN score NaN
+        l += x[t][r];
+      }
+    bool bad = false;  // masked positions must not see NaN
+    if (cut) {
+#pragma unroll
+      for (int v = 0; v < VT; ++v) {
+        const int have = nk - f - 8 * v;  // positions of this tile; what is behind them may be anything
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int of = have - 4 * u;
+          const uint32_t mask = of <= 0 ? 0u : of >= 4 ? ~0u : (1u << (8 * of)) - 1u;
+#pragma unroll
+          for (int i = 0; i < JN; ++i) vr[v].d[i][u] &= mask;
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          constexpr uint32_t one = JN == 4 ? 0x7f7f7f7fu : 0x7f7fu;
+          const int at = q * JN / 4, sh = q * JN % 4 * 8;
+          constexpr uint32_t full = JN == 4 ? ~0u : 0xffffu;
+          if (q >= have) sv[v].d[at] = (sv[v].d[at] & ~(full << sh)) | (one << sh);
+          const uint32_t z = ~sv[v].d[at];  // a byte of 255 is one of zero here
+          bad |= ((z - 0x01010101u) & ~z & 0x80808080u) != 0;
+        }
+      }
+      bad = __any(bad);
+    }
+    Kv4Parts<TT> pw;
+    pw.split(x);
+#pragma unroll
+    for (int jj = 0; jj < JN; ++jj) {
+      if (bad) {  // NaN scales go with the weights of the rows that see them
+        floatx4 y[TT];
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int v = t >> 1, q = 4 * (t & 1) + r, at = q * JN / 4, sh = (q * JN % 4 + jj) * 8;
+            const bool nan = ((sv[v].d[at] >> sh) & 255u) == kNanScale;
+            y[t][r] = nan && f + 4 * t + r <= qpos ? __builtin_nanf("") : x[t][r];
+            if (nan) sv[v].d[at] ^= 0x80u << sh;  // 127: one
+          }
+        pw.split(y);
+      }
+#pragma unroll
+      for (int v = 0; v < VT; ++v) {
+        bf16x2 pr[8];
+#define LD_KV4_PAIR(q, B)                                                                          \
+  pr[q] = pair_of<B>(vr[v].d[jj][q / 4], __builtin_bit_cast(float, sv_shift(sv[v].d[q * JN / 4], q * JN % 4 + jj)))
+        auto sv_shift = [](uint32_t w, int byte) {
+          return byte == 0 ? w << 23 : byte == 1 ? w << 15 : byte == 2 ? w << 7 : w >> 1;
+        };
+        LD_KV4_PAIR(0, 0);
+        LD_KV4_PAIR(1, 1);
+        LD_KV4_PAIR(2, 2);
+        LD_KV4_PAIR(3, 3);
+        LD_KV4_PAIR(4, 0);
+        LD_KV4_PAIR(5, 1);
+        LD_KV4_PAIR(6, 2);
+        LD_KV4_PAIR(7, 3);
+#undef LD_KV4_PAIR
+        union {
+          bf16x8 v8;
+          uint32_t u[4];
+        } lo, hi;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t e = __builtin_bit_cast(uint32_t, pr[2 * i]), f2 = __builtin_bit_cast(uint32_t, pr[2 * i + 1]);
+          lo.u[i] = __builtin_amdgcn_perm(f2, e, 0x05040100u);
+          hi.u[i] = __builtin_amdgcn_perm(f2, e, 0x07060302u);
+        }
+#pragma unroll
+        for (int part = 0; part < kKv4Parts; ++part) {
+          o[2 * jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo.v8, pw.p[part][v], o[2 * jj], 0, 0, 0);
+          o[2 * jj + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi.v8, pw.p[part][v], o[2 * jj + 1], 0, 0, 0);
+        }
+      }
+    }
+  }
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (lane < NQ) {
+    ml[wave][lane][0] = m;
+    ml[wave][lane][1] = l;
+  }
+  if (n < NQ)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) *reinterpret_cast<floatx4*>(&red[wave][n][16 * i + 4 * g]) = o[i];
+  __syncthreads();
+
+  // sum over the waves, in wave order, each scaled to the chunk's maximum
+  const bool only = nk <= ck;  // the sequence's one chunk: its rows are the result
+  for (int e = tid; e < rows * DH; e += 64 * NW) {
+    const int i = e / DH, col = e % DH, r = r0 + i;
+    float mw[NW], M = -INFINITY, L = 0.f, s = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      mw[w] = ml[w][i][0];
+      M = fmaxf(M, mw[w]);
+    }
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      // (a wave whose every score was NaN has no maximum, but NaN sums: 0 times them is NaN)
+      const float wgt = mw[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[w] - M);
+      L = __builtin_fmaf(wgt, ml[w][i][1], L);
+      s = __builtin_fmaf(wgt, red[w][i][col], s);
+    }
+    if (only) {
+      out_at(r)[col] = static_cast<bf16>(s * (1.f / L));
+      if (a.scores && col == 0) {
+        a.row_ml[(head * R + r) * 2] = M;
+        a.row_ml[(head * R + r) * 2 + 1] = 1.f / L;
+      }
+    } else {
+      const int64_t pr = (head * R + r) * a.n_chunks + chunk;
+      a.part_o[pr * DH + col] = s;
+      if (col == 0) {
+        a.part_ml[pr * 2] = M;
+        a.part_ml[pr * 2 + 1] = L;
+      }
+    }
+  }
+}
+
+// W (four or one) waves per (sequence, query head, new row) merge the chunks its keys
+// fill, where they are several: each every W-th, U at once so that their partial
+// rows are all in flight; then the waves' sums, in their order.
+template <int DH, int W>
+__global__ __launch_bounds__(256) void ld_attn_decode_kv4_combine(Kv4AttnArgs a) {
+  constexpr int CL = DH / 64, U = 4;
+  typedef float FRow __attribute__((ext_vector_type(CL)));
+  __shared__ float ml[W][2];
+  __shared__ __align__(16) FRow red[W][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t id = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x, HN = a.H * a.n_new;
+  if (id >= a.kv.n_seq * HN) return;
+  const int w = W == 1 ? 0 : wave;
+  const int64_t r = id, b = id / HN;
+  const uint32_t h = id % HN / a.n_new, j = id % a.n_new;  // (HN is a multiple of n_new)
+  int chunks = a.n_chunks;
+  if (a.seq_pos) {
+    const int p = a.seq_pos[b], nk = p < 0 || p > a.pos ? 0 : p + a.n_new, ck = kv4_chunk_keys(a, nk);
+    chunks = (nk + ck - 1) / ck;
+  }
+  if (chunks <= 1) return;  // written by the attention kernel
+  const float* po = a.part_o + r * a.n_chunks * DH + lane * CL;
+  const floatx2* pm = reinterpret_cast<const floatx2*>(a.part_ml) + r * a.n_chunks;
+  float M = -INFINITY, L = 0.f;
+  FRow acc = 0.f;
+  for (int c0 = w; c0 < chunks; c0 += U * W) {
+    FRow v[U];
+    float mc[U], lc[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {  // past the last chunk: the last again, dropped below
+      const int64_t c = min(c0 + u * W, chunks - 1);
+      v[u] = *reinterpret_cast<const FRow*>(po + c * DH);
+      const floatx2 x = pm[c];
+      mc[u] = x[0];
+      lc[u] = x[1];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    float m = M;
+#pragma unroll
+    for (int u = 0; u < U; ++u) m = fmaxf(m, mc[u]);
+    const float keep = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - m);
+    L *= keep;
+    acc *= keep;
+    M = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool in = c0 + u * W < chunks;  // else selected out: 0 times an infinity in v would be NaN
+      const float wgt = !in || mc[u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc[u] - m);
+      L = __builtin_fmaf(wgt, in ? lc[u] : 0.f, L);
+      acc += wgt * (in ? v[u] : FRow(0.f));
+    }
+  }
+  if constexpr (W > 1) {
+    if (lane == 0) {
+      ml[w][0] = M;
+      ml[w][1] = L;
+    }
+    red[w][lane] = acc;
+    __syncthreads();
+    if (w) return;
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < W; ++u) m = fmaxf(m, ml[u][0]);
+    L = 0.f;
+    acc = 0.f;
+#pragma unroll
+    for (int u = 0; u < W; ++u) {
+      const float wgt = ml[u][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[u][0] - m);
+      L = __builtin_fmaf(wgt, ml[u][1], L);
+      acc += wgt * red[u][lane];
+    }
+    M = m;
+  }
+  acc *= 1.f / L;
+  if (a.scores && lane == 0) {
+    a.row_ml[r * 2] = M;
+    a.row_ml[r * 2 + 1] = 1.f / L;
+  }
+  bf16* out = static_cast<bf16*>(a.out) + (b * a.n_new + j) * (static_cast<int64_t>(a.H) * DH) +
+              static_cast<int64_t>(h) * DH + lane * CL;
+#pragma unroll
+  for (int cc = 0; cc < CL; ++cc) out[cc] = static_cast<bf16>(acc[cc]);
+}
+
+// sums += the weights of a head's rows, a thread a position, rows in their order.
+__global__ __launch_bounds__(256) void ld_kv4_sums_k(Kv4AttnArgs a) {
+  const int b = blockIdx.z, h = blockIdx.y, t = blockIdx.x * 256 + threadIdx.x, R = a.group * a.n_new;
+  int p = a.pos;
+  if (a.seq_pos) {
+    p = a.seq_pos[b];
+    if (p < 0 || p > a.pos) return;
+  }
+  if (t >= p + a.n_new) return;
+  const int64_t head = static_cast<int64_t>(b) * a.kv.KV + h;
+  const float* sc = a.scores + head * R * a.score_keys + t;
+  const float* rm = a.row_ml + head * R * 2;
+  float s = 0.f;
+  for (int r = 0; r < R; ++r) {
+    const float x = sc[r * a.score_keys];
+    // (a masked position counts nothing, whatever the row holds)
+    s += t > p + r % a.n_new ? 0.f : __builtin_amdgcn_exp2f(x - rm[2 * r]) * rm[2 * r + 1];
+  }
+  a.kv.sums[head * a.kv.s_max + t] += s;
+}
+
+// ---------------------------------------------------------------- eviction
+
+// Order of the sums: larger ones first, NaN before all.
+__device__ __forceinline__ uint32_t evict_rank(float x) {
+  if (x != x) return ~0u;
+  const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.f);  // (-0 is 0)
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__device__ __forceinline__ int evict_len(const Kv4EvictArgs& a, int b) {
+  if (!a.seq_len) return a.len;
+  const int n = a.seq_len[b];
+  return n < 0 || n > a.len ? 0 : n;
+}
+
+// A workgroup takes a head: the rank of the last one that stays by four passes of 8
+// bits over counts, then the places of all that stay, in order.
+__global__ __launch_bounds__(1024) void ld_kv4_select_k(Kv4EvictArgs a) {
+  __shared__ uint32_t hist[256];
+  __shared__ uint32_t s_prefix, s_left;
+  __shared__ uint32_t wsum[2][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int h = blockIdx.x, b = blockIdx.y, n = evict_len(a, b);
+  const int64_t head = static_cast<int64_t>(b) * a.from.KV + h;
+  int32_t* idx = a.idx + head * a.keep;
+  if (n <= a.keep) {
+    for (int i = tid; i < a.keep; i += 1024) idx[i] = i < n ? i : -1;
+    return;
+  }
+  const float* sums = a.from.sums + head * a.from.s_max;
+  const int old = n - a.recent;
+  uint32_t left = a.keep - a.recent, prefix = 0, mask = 0;  // of those with the prefix `left` stay
+  for (int shift = 24; shift >= 0 && left; shift -= 8) {
+    for (int i = tid; i < 256; i += 1024) hist[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < old; i += 1024) {
+      const uint32_t u = evict_rank(sums[i]);
+      if ((u & mask) == prefix) atomicAdd(&hist[(u >> shift) & 255], 1u);
+    }
+    __syncthreads();
+    if (tid == 0) {
+      uint32_t more = 0;
+      int d = 255;
+      while (d > 0 && more + hist[d] < left) more += hist[d--];
+      s_prefix = prefix | static_cast<uint32_t>(d) << shift;
+      s_left = left - more;
+    }
+    __syncthreads();
+    prefix = s_prefix;
+    left = s_left;
+    mask |= 255u << shift;
+    __syncthreads();
+  }
+  // those above the prefix stay, and the first `left` of those at it
+  const bool none = a.keep == a.recent;
+  uint32_t kept = 0, same = 0;
+  for (int i0 = 0; i0 < old; i0 += 1024) {
+    const int i = i0 + tid;
+    const uint32_t u = i < old ? evict_rank(sums[i]) : 0u;
+    const bool over = !none && i < old && u > prefix, eq = !none && i < old && u == prefix;
+    const uint64_t below = (1ull << lane) - 1, me = __ballot(eq);
+    if (lane == 0) wsum[0][wave] = __popcll(me);
+    __syncthreads();
+    uint32_t before = same, all_eq = 0;
+    for (int w = 0; w < 16; ++w) {
+      before += w < wave ? wsum[0][w] : 0;
+      all_eq += wsum[0][w];
+    }
+    const bool stay = over || (eq && before + __popcll(me & below) < left);
+    const uint64_t mo = __ballot(stay);
+    if (lane == 0) wsum[1][wave] = __popcll(mo);
+    __syncthreads();
+    uint32_t at = kept, all = 0;
+    for (int w = 0; w < 16; ++w) {
+      at += w < wave ? wsum[1][w] : 0;
+      all += wsum[1][w];
+    }
+    if (stay) idx[at + __popcll(mo & below)] = i;
+    kept += all;
+    same += all_eq;
+  }
+  for (int i = tid; i < a.recent; i += 1024) idx[a.keep - a.recent + i] = old + i;
+}
+
+// A wave takes a tile of 8 places of the smaller cache: their keys, values, scales
+// and sums.
+template <int DH>
+__global__ __launch_bounds__(256) void ld_kv4_gather_k(Kv4EvictArgs a) {
+  constexpr int JN = DH / 32, TB = DH * 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t tiles = (a.keep + 7) / 8, id = kv4_workgroup() * 4 + wave;
+  const int64_t head = id / tiles;
+  if (head >= static_cast<int64_t>(a.to.n_seq) * a.to.KV) return;
+  const int t0 = id % tiles * 8, n = min(evict_len(a, head / a.to.KV), a.keep);
+  if (t0 >= n) return;
+  const int32_t* idx = a.idx + head * a.keep + t0;
+  const uint8_t* kf = a.from.codes + head * a.from.s8 * DH;
+  const uint8_t* vf = kf + static_cast<int64_t>(a.from.s8) * (DH / 2);
+  uint8_t* kt = a.to.codes + head * a.to.s8 * DH;
+  uint8_t* vt = kt + static_cast<int64_t>(a.to.s8) * (DH / 2);
+  const uint8_t* sf = a.from.scales + head * 2 * a.from.s8 * JN;
+  uint8_t* st = a.to.scales + head * 2 * a.to.s8 * JN;
+  const int have = min(n - t0, 8);
+  // keys: DH / 16 lanes of 8 bytes a row
+  for (int e = lane; e < have * (DH / 16); e += 64) {
+    const int r = e / (DH / 16), o = e % (DH / 16) * 8;
+    *reinterpret_cast<u32x2*>(kt + static_cast<int64_t>(t0 + r) * (DH / 2) + o) =
+        *reinterpret_cast<const u32x2*>(kf + static_cast<int64_t>(idx[r]) * (DH / 2) + o);
+  }
+  // values: byte by byte
+  for (int e = lane; e < DH / 2; e += 64)
+    for (int r = 0; r < have; ++r) {
+      const int i = idx[r];
+      vt[static_cast<int64_t>(t0 >> 3) * TB + e * 8 + r] = vf[static_cast<int64_t>(i >> 3) * TB + e * 8 + (i & 7)];
+    }
+  for (int e = lane; e < have * 2 * JN; e += 64) {
+    const int r = e / (2 * JN), part = e / JN % 2, jj = e % JN;
+    st[(static_cast<int64_t>(part) * a.to.s8 + t0 + r) * JN + jj] =
+        sf[(static_cast<int64_t>(part) * a.from.s8 + idx[r]) * JN + jj];
+  }
+  if (a.to.sums && lane < have) a.to.sums[head * a.to.s_max + t0 + lane] = a.from.sums[head * a.from.s_max + idx[lane]];
+}
+
+// Workgroups in two dimensions: one takes 2^32 threads at most.
+dim3 kv4_grid(int64_t wgs) {
+  constexpr int64_t kX = 1 << 20;
+  return wgs <= kX ? dim3(wgs) : dim3(kX, (wgs + kX - 1) / kX);
+}
+
+template <int DH>
+hipError_t store_t(Kv4StoreArgs a, hipStream_t s) {
+  constexpr int U = Kv4Lanes<DH>::U;
+  // pieces of any sequence: from the one that holds its first row
+  a.pieces = static_cast<int32_t>(a.seq_pos ? (static_cast<int64_t>(a.n) + U - 2) / U + 1
+                                            : (static_cast<int64_t>(a.pos) + a.n - 1) / U - a.pos / U + 1);
+  const int64_t units = 2ll * a.kv.KV * a.kv.n_seq * a.pieces;
+  hipLaunchKernelGGL((ld_kv4_store_k<DH>), kv4_grid((units + 3) / 4), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int DH>
+hipError_t load_t(Kv4LoadArgs a, hipStream_t s) {
+  constexpr int U = Kv4Lanes<DH>::U;
+  a.pieces = static_cast<int32_t>((static_cast<int64_t>(a.pos) + a.n - 1) / U - a.pos / U + 1);
+  const int64_t units = 2ll * a.kv.KV * a.kv.n_seq * a.pieces;
+  hipLaunchKernelGGL((ld_kv4_load_k<DH>), kv4_grid((units + 3) / 4), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int DH>
+hipError_t attn_t(const Kv4AttnArgs& a, hipStream_t s) {
+  const int R = a.group * a.n_new;
+  const dim3 block(64 * kKv4Waves);
+  const dim3 grid = a.tiles == 1 ? dim3(a.n_chunks, a.kv.KV, a.kv.n_seq)
+                                 : dim3(a.kv.KV * a.n_chunks * a.tiles, 1, a.kv.n_seq);
+  // rows kept for the merge: less LDS
+  if (R == 1)
+    hipLaunchKernelGGL((ld_attn_decode_kv4_k<DH, 1>), grid, block, 0, s, a);
+  else if (R <= 8)
+    hipLaunchKernelGGL((ld_attn_decode_kv4_k<DH, 8>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((ld_attn_decode_kv4_k<DH, 16>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+template <int DH>
+hipError_t combine_t(const Kv4AttnArgs& a, hipStream_t s) {
+  const int64_t rows = static_cast<int64_t>(a.kv.n_seq) * a.H * a.n_new;
+  if (a.n_chunks > 4 && rows <= 2048)
+    hipLaunchKernelGGL((ld_attn_decode_kv4_combine<DH, 4>), dim3(rows), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((ld_attn_decode_kv4_combine<DH, 1>), dim3((rows + 3) / 4), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+constexpr int64_t kKv4MinChunk = 256, kKv4Wgs = 2048;
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+}  // namespace
+
+hipError_t launch_kv4_store(const Kv4StoreArgs& a, hipStream_t s) { return a.kv.dh == 128 ? store_t<128>(a, s) : store_t<64>(a, s); }
+hipError_t launch_kv4_load(const Kv4LoadArgs& a, hipStream_t s) { return a.kv.dh == 128 ? load_t<128>(a, s) : load_t<64>(a, s); }
+
+int64_t attn_kv4_heads(const Kv4View& kv, int64_t H, int64_t n_new) {
+  const int64_t R = H / kv.KV * n_new;
+  return static_cast<int64_t>(kv.n_seq) * kv.KV * ((R + 15) / 16);
+}
+
+int64_t attn_kv4_max_chunks(int64_t heads, int64_t keys) {
+  const int64_t by_keys = div_up(keys, kKv4MinChunk), by_wgs = div_up(kKv4Wgs, heads);
+  return by_keys < by_wgs ? by_keys : by_wgs;
+}
+
+// A turn writes whole products' scores, 64 keys at most.
+int64_t attn_kv4_score_keys(int64_t keys) { return div_up(keys, 64) * 64; }
+
+void plan_attn_decode_kv4(Kv4AttnArgs& a) {
+  const int64_t keys = static_cast<int64_t>(a.pos) + a.n_new;
+  a.group = a.H / a.kv.KV;
+  a.tiles = (a.group * a.n_new + 15) / 16;
+  const int64_t heads = attn_kv4_heads(a.kv, a.H, a.n_new);
+  int64_t n = attn_kv4_max_chunks(heads, keys);
+  a.chunk_keys = static_cast<int32_t>(div_up(div_up(keys, n), 64) * 64);
+  a.n_chunks = static_cast<int32_t>(div_up(keys, a.chunk_keys));
+  a.score_keys = attn_kv4_score_keys(keys);
+}
+
+hipError_t launch_attn_decode_kv4(const Kv4AttnArgs& a, hipStream_t s) {
+  return a.kv.dh == 128 ? attn_t<128>(a, s) : attn_t<64>(a, s);
+}
+
+hipError_t launch_attn_decode_kv4_combine(const Kv4AttnArgs& a, hipStream_t s) {
+  return a.kv.dh == 128 ? combine_t<128>(a, s) : combine_t<64>(a, s);
+}
+
+hipError_t launch_kv4_sums(const Kv4AttnArgs& a, hipStream_t s) {
+  const int64_t keys = static_cast<int64_t>(a.pos) + a.n_new;
+  hipLaunchKernelGGL(ld_kv4_sums_k, dim3(div_up(keys, 256), a.kv.KV, a.kv.n_seq), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+size_t kv4_evict_ws_bytes(const Kv4View&, int64_t, int64_t) { return 0; }
+
+hipError_t launch_kv4_select(const Kv4EvictArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(ld_kv4_select_k, dim3(a.from.KV, a.from.n_seq), dim3(1024), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv4_gather(const Kv4EvictArgs& a, hipStream_t s) {
+  const int64_t waves = static_cast<int64_t>(a.to.n_seq) * a.to.KV * div_up(a.keep, 8);
+  if (a.to.dh == 128)
+    hipLaunchKernelGGL((ld_kv4_gather_k<128>), kv4_grid(div_up(waves, 4)), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((ld_kv4_gather_k<64>), kv4_grid(div_up(waves, 4)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace ld
