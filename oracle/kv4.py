@@ -56,9 +56,12 @@ def quantise(x):
     """Values of codes and scale bytes of the last dimension's groups."""
     x = np.asarray(x, dtype=np.float64)
     g = x.reshape(-1, GROUP)
-    byte = np.array([need(r) for r in g], dtype=np.uint8)
-    with np.errstate(all="ignore"):
-        code = np.where((byte == NAN_BYTE)[:, None], 0.0, round_to(np.where(np.isfinite(g), g, 0.0) / np.ldexp(1.0, byte.astype(np.int64) - 127)[:, None]))
+    fine = np.isfinite(g).all(-1)
+    g = np.where(fine[:, None], g, 0.0)
+    m, e = np.frexp(np.abs(g).max(-1))      # m 2^e, m in [1/2, 1); 6 = 0.75 2^3
+    e = np.where(m == 0.0, -100, np.clip(e - 3 + (m > 0.75), -100, 125))
+    code = round_to(g / np.ldexp(1.0, e)[:, None])
+    byte = np.where(fine, e + 127, NAN_BYTE).astype(np.uint8)
     return code.reshape(x.shape), byte.reshape(*x.shape[:-1], -1)
 
 

@@ -1300,8 +1300,7 @@ DecLayout dec_layout(const Dims& D, int64_t n_new, size_t pc, int64_t score_keys
     for (const auto& sh : shapes) L.skp_bytes = std::max(L.skp_bytes, skinny_fused_part_bytes(M, sh[0], sh[1]));
   if (w4)
     for (int i = 0; i < 4; ++i)
-      L.skp_bytes = std::max(L.skp_bytes, w4_gemm_ws_bytes(std::min<int64_t>(M, kW4MaxM), shapes[i][0], shapes[i][1],
-                                                          i == 2 && D.kind == LD_BLOCK_SWIGLU ? kDecActSwiglu : kDecActNone));
+      L.skp_bytes = std::max(L.skp_bytes, w4_gemm_ws_bytes(std::min<int64_t>(M, kW4MaxM), shapes[i][1]));
   if (L.skp_bytes) L.skp = take(L.skp_bytes);
   L.total = o;
   return L;
@@ -1600,7 +1599,7 @@ int check_weights_w4(const Dims& D, const ld_weights_w4& w, int32_t l) {
 
 // Projection by 4-bit weights (see launch_gemm_w4), kW4MaxM rows a launch.
 int run_gemm_w4(const W4View& w, const void* A, int64_t lda, const void* g, float eps, void* C, int64_t ldc, const void* R,
-                int64_t ldr, int64_t M, int64_t N, float alpha, int act, float* part, hipStream_t s) {
+                int64_t ldr, int64_t M, int64_t N, float alpha, int act, void* ws, hipStream_t s) {
   for (int64_t m = 0; m < M; m += kW4MaxM) {
     W4GemmArgs a{};
     a.w = w;
@@ -1616,8 +1615,8 @@ int run_gemm_w4(const W4View& w, const void* A, int64_t lda, const void* g, floa
     a.N = static_cast<int32_t>(N);
     a.alpha = alpha;
     a.act = act;
-    a.part = part;
-    ProfScope ps("ld_gemm_w4_k", s);
+    a.ws = ws;
+    ProfScope ps(a.M > kW4FewRows ? "ld_gemm_w4_rows" : "ld_gemm_w4_k", s);
     const hipError_t e = launch_gemm_w4(a, s);
     if (e != hipSuccess) return fail(LD_E_HIP, "w4 projection: %s", hipGetErrorString(e));
     const double rows = w.N, K = w.K, scale = (w.format == LD_W4_E2M1 ? 1.0 : 2.0) / w.group;
@@ -2723,7 +2722,7 @@ size_t ld_gemm_w4_ws_bytes(const ld_w4* w, int32_t M, int32_t act) {
   W4View v;
   if (check_w4(w, &v) || M < 1 || M > kW4MaxM || act < kDecActNone || act > kDecActRelu2) return 0;
   size_t most = 0;
-  for (int32_t m = 1; m <= M; ++m) most = std::max(most, w4_gemm_ws_bytes(m, v.N, v.K, act));
+  for (int32_t m = 1; m <= M; ++m) most = std::max(most, w4_gemm_ws_bytes(m, v.K));
   return most;
 }
 
@@ -2747,10 +2746,10 @@ int ld_gemm_w4(int32_t M, const void* A, int32_t lda, const void* g, float eps, 
     return fail(LD_E_INVALID, "C and R must be 2-byte aligned");
   if (!std::isfinite(alpha)) return fail(LD_E_INVALID, "alpha not finite");
   if (g && !(eps > 0.f)) return fail(LD_E_INVALID, "eps must be > 0");
-  const size_t need = w4_gemm_ws_bytes(M, v.N, v.K, act);
+  const size_t need = w4_gemm_ws_bytes(M, v.K);
   if (need && (!ws || ws_bytes < need)) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
   if (need && (reinterpret_cast<uintptr_t>(ws) & 15)) return fail(LD_E_INVALID, "ws must be 16-byte aligned");
-  return run_gemm_w4(v, A, lda, g, eps, C, ldc, R, ldr, M, N, alpha, act, static_cast<float*>(ws), as_stream(stream));
+  return run_gemm_w4(v, A, lda, g, eps, C, ldc, R, ldr, M, N, alpha, act, ws, as_stream(stream));
 }
 
 size_t ld_kv4_code_bytes(const ld_kv4* kv) {

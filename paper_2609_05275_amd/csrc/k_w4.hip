@@ -5,58 +5,10 @@
 // power-of-two scale along, an integer of sign and three bits as an 8-bit float below
 // its smallest normal number (steps of 2^-9), times 2^9.  The integers' scales go on
 // the float32 sums of a group's products.
-#include "ld_w4.h"
+#include "w4_codes.h"
 
 namespace ld {
 namespace {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
-typedef unsigned short ushortx4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kWaves = 8;
-
-// ------------------------------------------------------------- conversions
-
-// The scale in byte B of w as the conversions take it: they look at a float's
-// exponent alone.
-__device__ __forceinline__ float scale_byte(uint32_t w, int b) {
-  return __builtin_bit_cast(float, b == 0 ? w << 23 : b == 1 ? w << 15 : b == 2 ? w << 7 : w >> 1);
-}
-
-union Oct {
-  bf16x8 v;
-  bf16x2 p[4];
-  ushortx2 u[4];
-};
-
-// Eight codes of a dword; scale: of 4-bit floats.
-template <int FMT>
-__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t w, float scale) {
-  Oct r;
-  if constexpr (FMT == LD_W4_E2M1) {
-    r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
-    r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
-    r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
-    r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
-  } else {
-    const uint32_t a = w & 0x87878787u, b = __builtin_amdgcn_alignbit(w, w, 4) & 0x87878787u;
-    r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 512.f, false);
-    r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 512.f, true);
-    r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 512.f, false);
-    r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 512.f, true);
-  }
-  return r.v;
-}
-
-template <int FMT, int GROUP>
-struct W4Scales {
-  static constexpr int kPer = 128 / GROUP;                           // of a lane's row in half a chunk
-  static constexpr int kBytes = kPer * (FMT == LD_W4_E2M1 ? 1 : 2);
-};
 
 // ---------------------------------------------------------- pack and load
 
@@ -168,74 +120,193 @@ __global__ __launch_bounds__(256) void ld_w4_load_k(W4PackArgs a) {
 
 // ------------------------------------------------------------- projections
 
-__device__ __forceinline__ bf16x8 load8(const bf16* p) { return *reinterpret_cast<const bf16x8*>(p); }
-
-// Element (m, n) from its sums (SwiGLU: of the gate and the up row).
-__device__ __forceinline__ void w4_finish(const W4GemmArgs& a, int m, int64_t n, float s0, float s1, float scale) {
-  float y;
-  if (a.act == kDecActSwiglu) {
-    y = swiglu_fwd_f(scale * s0, scale * s1);
-  } else if (a.act == kDecActRelu2) {
-    const float z = fmaxf(scale * s0, 0.f);
-    y = z * z;
-  } else {
-    y = scale * s0;
-    if (a.R) y += static_cast<float>(static_cast<const bf16*>(a.R)[m * a.ldr + n]);
-  }
-  static_cast<bf16*>(a.C)[m * a.ldc + n] = static_cast<bf16>(y);
+// The chunks' numbers go round the waves, and neighbouring workgroups of an XCD (every
+// 8th) count from different waves, so that they do not all ask for the same lines of A
+// first.  Sums go by this number: the results do not depend on it.
+__device__ __forceinline__ int w4_wave() {
+  return __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) + (blockIdx.x >> 3)) & (kWaves - 1);
 }
 
-// Scales of a lane's row in half a chunk.
-template <int FMT, int GROUP>
-struct W4ScaleRaw {
-  typedef uint32_t type;  // four bytes, or two bf16
-};
-template <>
-struct W4ScaleRaw<LD_W4_INT4, 32> {
-  typedef uint64_t type;
-};
-template <>
-struct W4ScaleRaw<LD_W4_INT4, 128> {
-  typedef uint16_t type;
-};
+// Up to 8 MB rows of up to 256 kWaves CPW: every wave holds its chunks of the rows in
+// registers, as operands, for all the tiles that its workgroup takes.  A tile is 8 columns of
+// C (of W 8 rows; SwiGLU: 8 gate and 8 up rows); T of them are asked for, multiplied and
+// summed over the waves together, with one barrier, the next T's codes on their way.
+// As operands of a 16x16x32 product the rows of A stand twice, with the first and the
+// last 128 k of a chunk, and so do the weights: the product's two diagonal 8x8 blocks
+// are added, the others, which mix the halves, dropped.
+template <int FMT, int GROUP, int MB, int NR, bool NORM, int CPW>
+__global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_k(W4GemmArgs a) {
+  typedef typename W4ScaleRaw<FMT, GROUP>::type SRaw;
+  constexpr int T = NR * CPW >= 8 ? 1 : 8 / (NR * CPW), kWave = T * NR * MB * 64;
+  constexpr int kOut = T * MB * 64, kMine = (kOut + 64 * kWaves - 1) / (64 * kWaves);  // outputs of T tiles, a thread's
+  __shared__ __align__(16) float red[2][kWaves * kWave];
+  __shared__ float ssq[NORM ? kWaves : 1][MB * 8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = w4_wave();
+  const int K = a.w.K, M = a.M, C = (K + kW4Chunk - 1) / kW4Chunk;
+  const int r = lane & 7, lk = 128 * ((lane >> 3) & 1) + 8 * (lane >> 4);
+  const int tiles = (a.N + kW4Rows - 1) / kW4Rows, up = a.N / kW4Rows, step = gridDim.x;
 
-// acc[mb] += x[mb] (+ xl[mb], where there are low parts) times step s of the codes.
-// INT4: sums of a group in `part`, which go to acc times their scale at its end.
-template <int FMT, int GROUP, int MB, bool LOW>
-__device__ __forceinline__ void w4_step(int s, uint32_t q, typename W4ScaleRaw<FMT, GROUP>::type sc, const bf16x8 (&x)[MB],
-                                        const bf16x8 (&xl)[MB], floatx4 (&acc)[MB], floatx4 (&part)[MB]) {
-  if constexpr (FMT == LD_W4_E2M1) {
-    const bf16x8 w = codes_to_bf16<FMT>(q, scale_byte(sc, s));
+  struct Codes {
+    u32x4 q[T][NR][CPW];
+    SRaw s[T][NR][CPW];
+    uint16_t resid[kMine];
+  };
+  // tiles past the last and chunks past K: the last ones again, not used
+  auto load_w = [&](Codes& w, int first) {
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-      acc[mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[mb], w, acc[mb], 0, 0, 0);
-      if constexpr (LOW) acc[mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xl[mb], w, acc[mb], 0, 0, 0);
-    }
-  } else {
-    constexpr int kSteps = GROUP / 32;
-    const bf16x8 w = codes_to_bf16<FMT>(q, 1.f);
-    const floatx4 zero{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < T; ++t) {
+      if (t && first + t * step >= tiles) break;
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-      part[mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[mb], w, s % kSteps ? part[mb] : zero, 0, 0, 0);
-      if constexpr (LOW) part[mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xl[mb], w, part[mb], 0, 0, 0);
+      for (int j = 0; j < NR; ++j)
+#pragma unroll
+        for (int u = 0; u < CPW; ++u) {
+          const int64_t block = static_cast<int64_t>(first + t * step + j * up) * C + min(wave + kWaves * u, C - 1);
+          w.q[t][j][u] = reinterpret_cast<const u32x4*>(a.w.codes)[block * 64 + lane];
+          w.s[t][j][u] = static_cast<const SRaw*>(a.w.scales)[block * 16 + (lane & 15)];
+        }
     }
-    if (s % kSteps == kSteps - 1) {
-      const float f = __builtin_bit_cast(float, static_cast<uint32_t>(static_cast<uint64_t>(sc) >> (s / kSteps * 16)) << 16);
+    if (a.R) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const int e = tid + 64 * kWaves * i, tile = first + e / (MB * 64) * step;
+        const int m = min(e / 8 % (MB * 8), M - 1), n = min(tile * kW4Rows + (e & 7), a.N - 1);
+        w.resid[i] = static_cast<const uint16_t*>(a.R)[static_cast<int64_t>(m) * a.ldr + n];
+      }
+    }
+  };
+  Codes w0, w1;
+  load_w(w0, blockIdx.x);
+
+  // the wave's rows (those past M repeat the last; with a gain in two parts)
+  bf16x8 x[CPW][4][MB], xl[CPW][4][MB];
+#pragma unroll
+  for (int u = 0; u < CPW; ++u)
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int k = (wave + kWaves * u) * kW4Chunk + 32 * s + lk;
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[mb][e] = __builtin_fmaf(part[mb][e], f, acc[mb][e]);
+        x[u][s][mb] = load8(static_cast<const bf16*>(a.A) + static_cast<int64_t>(min(mb * 8 + r, M - 1)) * a.lda + (k < K ? k : 0));
     }
+  bf16x8 gv[NORM ? CPW : 1][4];
+  if constexpr (NORM) {
+#pragma unroll
+    for (int u = 0; u < CPW; ++u)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int k = (wave + kWaves * u) * kW4Chunk + 32 * s + lk;
+        gv[u][s] = load8(static_cast<const bf16*>(a.g) + (k < K ? k : 0));
+      }
+  }
+#pragma unroll
+  for (int u = 0; u < CPW; ++u)
+    if ((wave + kWaves * u + 1) * kW4Chunk > K) {  // wave-uniform
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) keep_if(x[u][s][mb], (wave + kWaves * u) * kW4Chunk + 32 * s + lk < K);
+    }
+  if constexpr (NORM) {
+    // Sums of squares from the products of the rows with themselves (the diagonals of the
+    // two blocks).  A row times the gain has 16 bits: two bf16 parts.
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      floatx4 q{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < CPW; ++u)
+#pragma unroll
+        for (int s = 0; s < 4; ++s) q = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[u][s][mb], x[u][s][mb], q, 0, 0, 0);
+      // lane l: rows 4 (l / 16) + e of column l % 16
+      const int e = lane & 3;
+      float ss = e == 0 ? q[0] : e == 1 ? q[1] : e == 2 ? q[2] : q[3];
+      ss += __shfl_xor(ss, 40, 64);
+      if ((lane & 40) == 0 && (lane & 15) >> 2 == lane >> 4) ssq[wave][mb * 8 + r] = ss;
+    }
+#pragma unroll
+    for (int u = 0; u < CPW; ++u) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float y = static_cast<float>(x[u][s][mb][e]) * static_cast<float>(gv[u][s][e]);
+            x[u][s][mb][e] = static_cast<bf16>(y);
+            xl[u][s][mb][e] = static_cast<bf16>(y - static_cast<float>(x[u][s][mb][e]));
+          }
+      if ((wave + kWaves * u + 1) * kW4Chunk > K) {  // a gain past K may be anything
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb) {
+            const bool in = (wave + kWaves * u) * kW4Chunk + 32 * s + lk < K;
+            keep_if(x[u][s][mb], in);
+            keep_if(xl[u][s][mb], in);
+          }
+      }
+    }
+  }
+
+  auto do_tiles = [&](Codes& w, int first, int next, float* sums, Codes& wn) {
+    if (next < tiles) load_w(wn, next);
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      if (t && first + t * step >= tiles) break;
+#pragma unroll
+      for (int j = 0; j < NR; ++j) {
+        floatx4 acc[MB], part[MB];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) acc[mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < CPW; ++u) {
+          if (wave + kWaves * u >= C) break;  // wave-uniform
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+            w4_step<FMT, GROUP, MB, NORM>(s, w.q[t][j][u][s], w.s[t][j][u], x[u][s], xl[u][s], acc, part);
+        }
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+          floatx4 v = acc[mb];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], 40, 64);
+          if ((lane & 40) == 0)
+            *reinterpret_cast<floatx4*>(sums + wave * kWave + (((t * NR + j) * MB + mb) * 8 + r) * 8 + 4 * (lane >> 4)) = v;
+        }
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int e = tid + 64 * kWaves * i, t = e / (MB * 64), m = e / 8 % (MB * 8), tile = first + t * step;
+      const int64_t n = static_cast<int64_t>(tile) * kW4Rows + (e & 7);
+      if (e >= kOut || m >= M || tile >= tiles || n >= a.N) continue;
+      const float* at = sums + ((t * NR * MB + m / 8) * 8 + (e & 7)) * 8 + (m & 7);
+      float s0 = 0.f, s1 = 0.f, scale = a.alpha;
+#pragma unroll
+      for (int wv = 0; wv < kWaves; ++wv) {
+        s0 += at[wv * kWave];
+        if constexpr (NR == 2) s1 += at[wv * kWave + MB * 64];
+      }
+      if constexpr (NORM) {
+        float tot = 0.f;
+#pragma unroll
+        for (int wv = 0; wv < kWaves; ++wv) tot += ssq[wv][m];
+        scale *= rsqrtf(tot / static_cast<float>(K) + a.eps);
+      }
+      w4_finish(a, m, n, s0, s1, scale, w.resid[i]);
+    }
+  };
+  // (a buffer's readers are past the next barrier before it is written again)
+  for (int tile = blockIdx.x; tile < tiles; tile += 2 * T * step) {
+    do_tiles(w0, tile, tile + T * step, red[0], w1);
+    if (tile + T * step < tiles) do_tiles(w1, tile + T * step, tile + 2 * T * step, red[1], w0);
   }
 }
 
-// A workgroup takes 8 columns of C (of W 8 rows; SwiGLU: 8 gate and 8 up rows), its
-// waves every eighth chunk of 256 k.  As operands of a 16x16x32 product the rows of A
-// stand twice, with the first and the last 128 k of the chunk, and so do the weights: the
-// product's two diagonal 8x8 blocks are added, the others, which mix the halves, dropped.
+// Any rows and K: a workgroup takes 8 columns, its waves every eighth chunk, and reads
+// rows and codes beside each other.
 template <int FMT, int GROUP, int MB, int NR, bool NORM>
-__global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_k(W4GemmArgs a) {
+__global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_long(W4GemmArgs a) {
   typedef typename W4ScaleRaw<FMT, GROUP>::type SRaw;
   constexpr int kWave = NR * MB * 64;
   __shared__ __align__(16) float red[kWaves * kWave];
@@ -272,7 +343,7 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_k(W4GemmArgs a) {
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) {
         x[mb] = load8(xr[mb] + (in ? k : 0));
-        if (!in) x[mb] = static_cast<bf16>(0.f);
+        keep_if(x[mb], in);
       }
       if constexpr (NORM) {
         const bf16x8 gv = load8(static_cast<const bf16*>(a.g) + (in ? k : 0));
@@ -285,7 +356,8 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_k(W4GemmArgs a) {
             x[mb][e] = static_cast<bf16>(y);
             xl[mb][e] = static_cast<bf16>(y - static_cast<float>(x[mb][e]));
           }
-          if (!in) x[mb] = xl[mb] = static_cast<bf16>(0.f);
+          keep_if(x[mb], in);
+          keep_if(xl[mb], in);
         }
       }
 #pragma unroll
@@ -298,15 +370,12 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_k(W4GemmArgs a) {
     for (int mb = 0; mb < MB; ++mb) {
       floatx4 v = acc[j][mb];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] += __shfl_xor(v[e], 40, 64);
-        if ((lane & 40) == 0) red[wave * kWave + ((j * MB + mb) * 8 + 4 * (lane >> 4) + e) * 8 + r] = v[e];
-      }
+      for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], 40, 64);
+      if ((lane & 40) == 0) *reinterpret_cast<floatx4*>(red + wave * kWave + ((j * MB + mb) * 8 + r) * 8 + 4 * (lane >> 4)) = v;
     }
   if constexpr (NORM) {
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
-      // lane l: rows 4 (l / 16) + e of column l % 16
       const int e = lane & 3;
       float ss = e == 0 ? q2[mb][0] : e == 1 ? q2[mb][1] : e == 2 ? q2[mb][2] : q2[mb][3];
       ss += __shfl_xor(ss, 40, 64);
@@ -317,11 +386,12 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_k(W4GemmArgs a) {
   const int m = tid >> 3;
   const int64_t n = tile * kW4Rows + (tid & 7);
   if (m >= M || m >= MB * 8 || n >= a.N) return;
+  const float* at = red + (m / 8 * 8 + (tid & 7)) * 8 + (m & 7);
   float s0 = 0.f, s1 = 0.f, scale = a.alpha;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    s0 += red[w * kWave + tid];
-    if constexpr (NR == 2) s1 += red[w * kWave + MB * 64 + tid];
+    s0 += at[w * kWave];
+    if constexpr (NR == 2) s1 += at[w * kWave + MB * 64];
   }
   if constexpr (NORM) {
     float tot = 0.f;
@@ -329,28 +399,42 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_k(W4GemmArgs a) {
     for (int w = 0; w < kWaves; ++w) tot += ssq[w][m];
     scale *= rsqrtf(tot / static_cast<float>(K) + a.eps);
   }
-  w4_finish(a, m, n, s0, s1, scale);
+  w4_finish(a, m, n, s0, s1, scale, a.R ? static_cast<const uint16_t*>(a.R)[m * a.ldr + n] : 0);
 }
 
+template <int FMT, int GROUP, int MB, int NR, bool NORM, int CPW>
+hipError_t gemm_held(const W4GemmArgs& a, hipStream_t s) {
+  const int tiles = (a.N + kW4Rows - 1) / kW4Rows, rounds = (tiles + kCus - 1) / kCus;
+  hipLaunchKernelGGL((ld_gemm_w4_k<FMT, GROUP, MB, NR, NORM, CPW>), dim3((tiles + rounds - 1) / rounds), dim3(64 * kWaves), 0, s, a);
+  return hipGetLastError();
+}
+
+// At most 16 rows: held in registers where those suffice.
 template <int FMT, int GROUP, int MB, int NR, bool NORM>
-hipError_t gemm_launch(const W4GemmArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((ld_gemm_w4_k<FMT, GROUP, MB, NR, NORM>), dim3((a.N + kW4Rows - 1) / kW4Rows), dim3(64 * kWaves), 0, s, a);
+hipError_t gemm_few(const W4GemmArgs& a, hipStream_t s) {
+  const int cpw = (a.w.K + kW4Chunk * kWaves - 1) / (kW4Chunk * kWaves);  // chunks a wave
+  constexpr int kMost = 8 / (MB * (NORM || NR == 2 ? 2 : 1));
+  if (cpw <= 1) return gemm_held<FMT, GROUP, MB, NR, NORM, 1>(a, s);
+  if (cpw <= 2) return gemm_held<FMT, GROUP, MB, NR, NORM, 2>(a, s);
+  if constexpr (kMost >= 4)
+    if (cpw <= 4) return gemm_held<FMT, GROUP, MB, NR, NORM, 4>(a, s);
+  if constexpr (kMost >= 8)
+    if (cpw <= 8) return gemm_held<FMT, GROUP, MB, NR, NORM, 8>(a, s);
+  hipLaunchKernelGGL((ld_gemm_w4_long<FMT, GROUP, MB, NR, NORM>), dim3((a.N + kW4Rows - 1) / kW4Rows), dim3(64 * kWaves), 0, s, a);
   return hipGetLastError();
 }
 
 template <int FMT, int GROUP, int MB>
 hipError_t gemm_mb(const W4GemmArgs& a, hipStream_t s) {
-  if constexpr (MB <= 2)
-    if (a.g) return a.act == kDecActSwiglu ? gemm_launch<FMT, GROUP, MB, 2, true>(a, s) : gemm_launch<FMT, GROUP, MB, 1, true>(a, s);
-  if (a.g) return hipErrorInvalidValue;
-  return a.act == kDecActSwiglu ? gemm_launch<FMT, GROUP, MB, 2, false>(a, s) : gemm_launch<FMT, GROUP, MB, 1, false>(a, s);
+  const bool glu = a.act == kDecActSwiglu;
+  if (a.g) return glu ? gemm_few<FMT, GROUP, MB, 2, true>(a, s) : gemm_few<FMT, GROUP, MB, 1, true>(a, s);
+  return glu ? gemm_few<FMT, GROUP, MB, 2, false>(a, s) : gemm_few<FMT, GROUP, MB, 1, false>(a, s);
 }
 
 template <int FMT, int GROUP>
 hipError_t gemm_t(const W4GemmArgs& a, hipStream_t s) {
-  if (a.M < 1 || a.M > kW4MaxM) return hipErrorInvalidValue;
-  return a.M <= 8 ? gemm_mb<FMT, GROUP, 1>(a, s) : a.M <= 16 ? gemm_mb<FMT, GROUP, 2>(a, s)
-       : a.M <= 32 ? gemm_mb<FMT, GROUP, 4>(a, s) : gemm_mb<FMT, GROUP, 8>(a, s);
+  if (a.M < 1) return hipErrorInvalidValue;
+  return a.M <= 8 ? gemm_mb<FMT, GROUP, 1>(a, s) : gemm_mb<FMT, GROUP, 2>(a, s);
 }
 
 template <int FMT, int GROUP>
@@ -376,11 +460,10 @@ hipError_t launch_w4_pack(const W4PackArgs& a, hipStream_t s) { return pack_or_l
 hipError_t launch_w4_load(const W4PackArgs& a, hipStream_t s) { return pack_or_load(a, s); }
 
 // Rows and K whose norm a projection can take in.
-bool w4_gemm_fuses_norm(int64_t M, int64_t K) { return M <= 16 && K <= 8192; }
-
-size_t w4_gemm_ws_bytes(int64_t, int64_t, int64_t, int) { return 0; }
+bool w4_gemm_fuses_norm(int64_t M, int64_t K) { return M <= kW4FewRows && K <= 8192; }
 
 hipError_t launch_gemm_w4(const W4GemmArgs& a, hipStream_t s) {
+  if (a.M > kW4FewRows) return launch_gemm_w4_rows(a, s);
   if (a.w.format == LD_W4_E2M1) return gemm_t<LD_W4_E2M1, 32>(a, s);
   return a.w.group == 32 ? gemm_t<LD_W4_INT4, 32>(a, s) : a.w.group == 64 ? gemm_t<LD_W4_INT4, 64>(a, s)
                                                         : gemm_t<LD_W4_INT4, 128>(a, s);

@@ -1,0 +1,161 @@
+// Projections of 17 to 64 rows by 4-bit weights.  Layout: W4View in ld_w4.h.
+#include "w4_codes.h"
+
+namespace ld {
+namespace {
+
+// A block of 16 rows and 32 k as the operand that a product takes: lane 16 g + n has row n's
+// k = 8 g .. 8 g + 7.  Blocks [ceil(K / 256)][2][4][MB]; rows and k past the last are zeros.
+__global__ __launch_bounds__(256) void ld_w4_rows_k(W4GemmArgs a, int mb_count, int blocks) {
+  const int lane = threadIdx.x & 63, b = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (b >= blocks) return;
+  const int m = b % mb_count * 16 + (lane & 15), k = b / mb_count * 32 + 8 * (lane >> 4);
+  bf16x8 x = load8(static_cast<const bf16*>(a.A) + static_cast<int64_t>(min(m, a.M - 1)) * a.lda + (k < a.w.K ? k : 0));
+  keep_if(x, m < a.M && k < a.w.K);
+  static_cast<bf16x8*>(a.ws)[static_cast<int64_t>(b) * 64 + lane] = x;
+}
+
+// MB blocks of 16 rows against CG groups of 16 rows of W (two tiles; SwiGLU: half the groups
+// gate rows, half up rows), the workgroup's eight waves taking its chunks in turn, so that
+// the rows are read once a workgroup and used for CG products.  Lanes 8 apart swap the
+// halves of two tiles: then a product's 16 columns are 16 rows of W with the same 32 k.
+template <int FMT, int GROUP, int MB, int CG>
+__global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_rows(W4GemmArgs a) {
+  typedef typename W4ScaleRaw<FMT, GROUP>::type SRaw;
+  constexpr int kWave = CG * MB * 256;  // sums of a wave
+  __shared__ __align__(16) float red[kWaves / 2 * kWave];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int M = a.M, C = (a.w.K + kW4Chunk - 1) / kW4Chunk, n16 = lane & 15, g = lane >> 4;
+  const bool glu = a.act == kDecActSwiglu;
+  const int tiles = (a.w.N + kW4Rows - 1) / kW4Rows, part_tiles = glu ? a.N / kW4Rows : tiles;
+  const int groups = glu ? CG / 2 : CG;       // of columns of C
+  const int first = blockIdx.x * groups * 2;  // tile
+  floatx4 acc[CG][MB];
+#pragma unroll
+  for (int i = 0; i < CG; ++i)
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) acc[i][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  u32x4 w[CG][2];  // as loaded two tiles, then two halves
+  SRaw sw[CG][2];
+  auto load_w = [&](int i, int c) {
+    const bool is_up = glu && i >= CG / 2;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int t = min(first + (is_up ? i - CG / 2 : i) * 2 + e, part_tiles - 1) + (is_up ? part_tiles : 0);
+      const int64_t block = static_cast<int64_t>(t) * C + c;
+      w[i][e] = reinterpret_cast<const u32x4*>(a.w.codes)[block * 64 + lane];
+      sw[i][e] = static_cast<const SRaw*>(a.w.scales)[block * 16 + n16];
+    }
+  };
+  auto swap_halves = [&](int i) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const uint32_t q0 = w[i][0][s], q1 = w[i][1][s];
+      w[i][0][s] = swap_in<0xc>(q0, q1);
+      w[i][1][s] = swap_in<0x3>(q1, q0);
+    }
+    const SRaw s0 = sw[i][0], s1 = sw[i][1];
+    sw[i][0] = swap_in<0xc>(s0, s1);
+    sw[i][1] = swap_in<0x3>(s1, s0);
+  };
+  const bf16x8* rows = static_cast<const bf16x8*>(a.ws) + lane;
+  bf16x8 x[2][2][MB];  // two steps, the next two
+  auto load_x = [&](bf16x8 (&to)[2][MB], int pair) {  // pair of steps, four a chunk
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) to[s][mb] = rows[(static_cast<int64_t>(pair * 2 + s) * MB + mb) * 64];
+  };
+  if (wave < C) {
+    load_x(x[0], wave * 4);
+#pragma unroll
+    for (int i = 0; i < CG; ++i) load_w(i, wave);
+  }
+  for (int c = wave; c < C; c += kWaves) {
+    const int next = c + kWaves < C ? c + kWaves : c;  // (the last chunk's again, not used)
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      load_x(x[(p + 1) & 1], p < 3 ? c * 4 + p + 1 : next * 4);
+#pragma unroll
+      for (int i = 0; i < CG; ++i) {
+        if (p == 0) swap_halves(i);
+        w4_pair<FMT, GROUP, MB>(p & 1, w[i][p >> 1], sw[i][p >> 1], x[p & 1], acc[i]);
+        if (p == 3) load_w(i, next);
+      }
+    }
+  }
+  // the last four waves' sums, then all on the first four's; lane: rows 4 g + e of column n16
+  float* mine = red + (wave & 3) * kWave;
+#pragma unroll
+  for (int half = 1; half >= 0; --half) {
+    if (wave >> 2 == half) {
+#pragma unroll
+      for (int i = 0; i < CG; ++i)
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+          floatx4* at = reinterpret_cast<floatx4*>(mine + ((i * MB + mb) * 16 + n16) * 16 + 4 * g);
+          *at = half ? acc[i][mb] : acc[i][mb] + *at;
+        }
+    }
+    __syncthreads();
+  }
+  const int cols = groups * 16, outs = cols * MB * 16;
+  for (int e = tid; e < outs; e += 64 * kWaves) {
+    // columns first: neighbouring threads store neighbouring elements
+    const int col = e % cols, m = e / cols, i = col / 16;
+    const int64_t n = static_cast<int64_t>(first) * kW4Rows + col;
+    if (m >= M || n >= a.N) continue;
+    const float* at = red + ((i * MB + m / 16) * 16 + col % 16) * 16 + m % 16;
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int v = 0; v < kWaves / 2; ++v) s0 += at[v * kWave];
+    if (glu) {
+#pragma unroll
+      for (int v = 0; v < kWaves / 2; ++v) s1 += at[v * kWave + CG / 2 * MB * 256];
+    }
+    w4_finish(a, m, n, s0, s1, a.alpha, a.R ? static_cast<const uint16_t*>(a.R)[m * a.ldr + n] : 0);
+  }
+}
+
+template <int FMT, int GROUP, int MB, int CG>
+hipError_t rows_launch(const W4GemmArgs& a, hipStream_t s) {
+  const int cols = (a.act == kDecActSwiglu ? CG / 2 : CG) * 16;
+  hipLaunchKernelGGL((ld_gemm_w4_rows<FMT, GROUP, MB, CG>), dim3((a.N + cols - 1) / cols), dim3(64 * kWaves), 0, s, a);
+  return hipGetLastError();
+}
+
+// The fewest groups a workgroup with which one round of workgroups does.
+template <int FMT, int GROUP, int MB>
+hipError_t rows_mb(const W4GemmArgs& a, hipStream_t s) {
+  const int groups = (a.w.N + 15) / 16;
+  if (groups <= kCus && a.act != kDecActSwiglu) return rows_launch<FMT, GROUP, MB, 1>(a, s);
+  if (groups <= 2 * kCus) return rows_launch<FMT, GROUP, MB, 2>(a, s);
+  if (groups <= 4 * kCus) return rows_launch<FMT, GROUP, MB, 4>(a, s);
+  return rows_launch<FMT, GROUP, MB, 6>(a, s);
+}
+
+template <int FMT, int GROUP>
+hipError_t rows_t(const W4GemmArgs& a, hipStream_t s) {
+  return a.M <= 32 ? rows_mb<FMT, GROUP, 2>(a, s) : a.M <= 48 ? rows_mb<FMT, GROUP, 3>(a, s) : rows_mb<FMT, GROUP, 4>(a, s);
+}
+
+}  // namespace
+
+size_t w4_gemm_ws_bytes(int64_t M, int64_t K) {
+  if (M <= kW4FewRows) return 0;
+  return static_cast<size_t>((M + 15) / 16 * 16) * ((K + kW4Chunk - 1) / kW4Chunk * kW4Chunk) * 2;
+}
+
+hipError_t launch_gemm_w4_rows(const W4GemmArgs& a, hipStream_t s) {
+  if (a.M <= kW4FewRows || a.M > kW4MaxM || a.g || !a.ws) return hipErrorInvalidValue;
+  const int mb = (a.M + 15) / 16, blocks = (a.w.K + kW4Chunk - 1) / kW4Chunk * 8 * mb;
+  hipLaunchKernelGGL(ld_w4_rows_k, dim3((blocks + 3) / 4), dim3(256), 0, s, a, mb, blocks);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (a.w.format == LD_W4_E2M1) return rows_t<LD_W4_E2M1, 32>(a, s);
+  return a.w.group == 32 ? rows_t<LD_W4_INT4, 32>(a, s) : a.w.group == 64 ? rows_t<LD_W4_INT4, 64>(a, s)
+                                                        : rows_t<LD_W4_INT4, 128>(a, s);
+}
+
+}  // namespace ld

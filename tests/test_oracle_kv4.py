@@ -33,7 +33,7 @@ def test_codes_and_values():
 def test_scale(a, e):
     x = np.zeros(32)
     x[7] = -a
-    assert kv4.need(x) == (255 if e is None else e + 127)
+    assert kv4.need(x) == (255 if e is None else e + 127) == kv4.quantise(x)[1][0]
 
 
 @pytest.mark.parametrize("dh", [64, 128])
