@@ -1616,7 +1616,7 @@ int run_gemm_w4(const W4View& w, const void* A, int64_t lda, const void* g, floa
     a.alpha = alpha;
     a.act = act;
     a.ws = ws;
-    ProfScope ps(a.M > kW4FewRows ? "ld_gemm_w4_rows" : "ld_gemm_w4_k", s);
+    ProfScope ps("ld_gemm_w4", s);
     const hipError_t e = launch_gemm_w4(a, s);
     if (e != hipSuccess) return fail(LD_E_HIP, "w4 projection: %s", hipGetErrorString(e));
     const double rows = w.N, K = w.K, scale = (w.format == LD_W4_E2M1 ? 1.0 : 2.0) / w.group;

@@ -413,14 +413,19 @@ hipError_t gemm_held(const W4GemmArgs& a, hipStream_t s) {
 template <int FMT, int GROUP, int MB, int NR, bool NORM>
 hipError_t gemm_few(const W4GemmArgs& a, hipStream_t s) {
   const int cpw = (a.w.K + kW4Chunk * kWaves - 1) / (kW4Chunk * kWaves);  // chunks a wave
+  // One or two tiles a CU over long rows: no more is gained by holding rows than is lost by
+  // taking the tiles in turn.  Us of one row, held and not: 4096 x 11008 9.2, 6.1; 2048 x 5504
+  // 3.7, 3.1; 2048 x 16384 7.2, 6.3.  (22016 x 4096 14.7, 22.2; 12288 x 4096 9.6, 19.4.)
+  const int tiles = (a.N + kW4Rows - 1) / kW4Rows;
+  const bool held = cpw <= 2 || MB > 1 || tiles > 2 * kCus;
   constexpr int kMost = 8 / (MB * (NORM || NR == 2 ? 2 : 1));
   if (cpw <= 1) return gemm_held<FMT, GROUP, MB, NR, NORM, 1>(a, s);
   if (cpw <= 2) return gemm_held<FMT, GROUP, MB, NR, NORM, 2>(a, s);
   if constexpr (kMost >= 4)
-    if (cpw <= 4) return gemm_held<FMT, GROUP, MB, NR, NORM, 4>(a, s);
+    if (held && cpw <= 4) return gemm_held<FMT, GROUP, MB, NR, NORM, 4>(a, s);
   if constexpr (kMost >= 8)
-    if (cpw <= 8) return gemm_held<FMT, GROUP, MB, NR, NORM, 8>(a, s);
-  hipLaunchKernelGGL((ld_gemm_w4_long<FMT, GROUP, MB, NR, NORM>), dim3((a.N + kW4Rows - 1) / kW4Rows), dim3(64 * kWaves), 0, s, a);
+    if (held && cpw <= 8) return gemm_held<FMT, GROUP, MB, NR, NORM, 8>(a, s);
+  hipLaunchKernelGGL((ld_gemm_w4_long<FMT, GROUP, MB, NR, NORM>), dim3(tiles), dim3(64 * kWaves), 0, s, a);
   return hipGetLastError();
 }
 
@@ -463,7 +468,12 @@ hipError_t launch_w4_load(const W4PackArgs& a, hipStream_t s) { return pack_or_l
 bool w4_gemm_fuses_norm(int64_t M, int64_t K) { return M <= kW4FewRows && K <= 8192; }
 
 hipError_t launch_gemm_w4(const W4GemmArgs& a, hipStream_t s) {
-  if (a.M > kW4FewRows) return launch_gemm_w4_rows(a, s);
+  // From 9 rows on reading them costs as much as the codes where they are long, and laid
+  // out in memory once they are used for more columns.  Us of 16 rows, held and laid out: 4096
+  // x 11008 22.2, 10.2; 2048 x 5504 9.9, 6.6; 16384 x 8192 25.2, 21.3; 22016 x 4096 18.0, 15.4;
+  // 12288 x 4096 12.0, 12.3; 6144 x 2048 4.8, 6.3.  Of 8: 4096 x 11008 12.8, 10.1, 8192 x 5504 10.7,
+  // 11.2, 2048 x 16384 10.0, 11.8.
+  if (a.M > kW4FewRows || (a.M > 8 && !a.g && (a.w.K > 4096 || a.w.N > 16384))) return launch_gemm_w4_rows(a, s);
   if (a.w.format == LD_W4_E2M1) return gemm_t<LD_W4_E2M1, 32>(a, s);
   return a.w.group == 32 ? gemm_t<LD_W4_INT4, 32>(a, s) : a.w.group == 64 ? gemm_t<LD_W4_INT4, 64>(a, s)
                                                         : gemm_t<LD_W4_INT4, 128>(a, s);

@@ -1,4 +1,4 @@
-// Projections of 17 to 64 rows by 4-bit weights.  Layout: W4View in ld_w4.h.
+// Projections of 9 to 64 rows by 4-bit weights.  Layout: W4View in ld_w4.h.
 #include "w4_codes.h"
 
 namespace ld {
@@ -137,18 +137,18 @@ hipError_t rows_mb(const W4GemmArgs& a, hipStream_t s) {
 
 template <int FMT, int GROUP>
 hipError_t rows_t(const W4GemmArgs& a, hipStream_t s) {
-  return a.M <= 32 ? rows_mb<FMT, GROUP, 2>(a, s) : a.M <= 48 ? rows_mb<FMT, GROUP, 3>(a, s) : rows_mb<FMT, GROUP, 4>(a, s);
+  return a.M <= 16 ? rows_mb<FMT, GROUP, 1>(a, s) : a.M <= 32 ? rows_mb<FMT, GROUP, 2>(a, s) : a.M <= 48 ? rows_mb<FMT, GROUP, 3>(a, s) : rows_mb<FMT, GROUP, 4>(a, s);
 }
 
 }  // namespace
 
 size_t w4_gemm_ws_bytes(int64_t M, int64_t K) {
-  if (M <= kW4FewRows) return 0;
+  if (M <= 8) return 0;
   return static_cast<size_t>((M + 15) / 16 * 16) * ((K + kW4Chunk - 1) / kW4Chunk * kW4Chunk) * 2;
 }
 
 hipError_t launch_gemm_w4_rows(const W4GemmArgs& a, hipStream_t s) {
-  if (a.M <= kW4FewRows || a.M > kW4MaxM || a.g || !a.ws) return hipErrorInvalidValue;
+  if (a.M < 1 || a.M > kW4MaxM || a.g || !a.ws) return hipErrorInvalidValue;
   const int mb = (a.M + 15) / 16, blocks = (a.w.K + kW4Chunk - 1) / kW4Chunk * 8 * mb;
   hipLaunchKernelGGL(ld_w4_rows_k, dim3((blocks + 3) / 4), dim3(256), 0, s, a, mb, blocks);
   const hipError_t e = hipGetLastError();

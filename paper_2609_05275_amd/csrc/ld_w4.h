@@ -17,7 +17,7 @@ struct W4View {
 };
 constexpr int kW4Rows = 8, kW4Chunk = 256;
 constexpr int kW4MaxM = 64;
-constexpr int kW4FewRows = 16;  // in registers; more are first laid out in scratch
+constexpr int kW4FewRows = 16;  // held in registers; more are laid out in scratch first
 constexpr int kW4MinExp = -100;
 
 struct W4PackArgs {
@@ -44,6 +44,6 @@ hipError_t launch_w4_load(const W4PackArgs& a, hipStream_t s);
 bool w4_gemm_fuses_norm(int64_t M, int64_t K);
 size_t w4_gemm_ws_bytes(int64_t M, int64_t K);
 hipError_t launch_gemm_w4(const W4GemmArgs& a, hipStream_t s);
-hipError_t launch_gemm_w4_rows(const W4GemmArgs& a, hipStream_t s);  // more than kW4FewRows, without a gain
+hipError_t launch_gemm_w4_rows(const W4GemmArgs& a, hipStream_t s);  // without a gain
 
 }  // namespace ld

@@ -199,14 +199,15 @@ def test_nan_and_infinite(fmt, group):
     w[5, 300] = float("nan")
     bad = packed(fmt, group, w)
     out = torch.zeros(2, 11, 21, dtype=torch.bfloat16, device=DEV)
-    ld.ld_gemm_w4(clean, x.to(DEV), out[0])
-    ld.ld_gemm_w4(bad, x.to(DEV), out[1])
+    ws = torch.zeros(ld.ld_gemm_w4_ws_bytes(clean, 11), dtype=torch.uint8, device=DEV)
+    ld.ld_gemm_w4(clean, x.to(DEV), out[0], ws)
+    ld.ld_gemm_w4(bad, x.to(DEV), out[1], ws)
     assert bool(torch.isnan(out[1][:, 5]).all())
     keep = [i for i in range(21) if i != 5]
     assert torch.equal(out[0][:, keep], out[1][:, keep])
     y = x.clone()
     y[2, 7], y[9, 599] = float("nan"), float("inf")
-    ld.ld_gemm_w4(clean, y.to(DEV), out[1])
+    ld.ld_gemm_w4(clean, y.to(DEV), out[1], ws)
     assert not bool(torch.isfinite(out[1][[2, 9]]).any())
     keep = [i for i in range(11) if i not in (2, 9)]
     assert torch.equal(out[0][keep], out[1][keep])
