@@ -2822,7 +2822,7 @@ int ld_attn_decode_kv4(const ld_kv4* kv, int32_t n_heads, int32_t alibi, int32_t
 size_t ld_kv4_evict_ws_bytes(const ld_kv4* from, int32_t len, int32_t keep) {
   Kv4View v;
   if (check_kv4(from, &v) || len < 1 || len > from->s_max || keep < 1) return 0;
-  return kv4_evict_ws_bytes(v, len, keep);
+  return kv4_evict_ws_bytes(v, len);
 }
 
 int ld_kv4_evict(const ld_kv4* from, const ld_kv4* to, int32_t len, const int32_t* seq_len, int32_t keep,
@@ -2858,7 +2858,7 @@ int ld_kv4_evict(const ld_kv4* from, const ld_kv4* to, int32_t len, const int32_
   a.recent = recent;
   a.seq_len = seq_len;
   a.idx = idx;
-  const size_t need = kv4_evict_ws_bytes(a.from, len, keep);
+  const size_t need = kv4_evict_ws_bytes(a.from, len);
   if (need && (!ws || ws_bytes < need)) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
   if (need && (reinterpret_cast<uintptr_t>(ws) & 15)) return fail(LD_E_INVALID, "ws must be 16-byte aligned");
   a.ws = static_cast<uint32_t*>(ws);

@@ -691,77 +691,286 @@ __device__ __forceinline__ int evict_len(const Kv4EvictArgs& a, int b) {
   return n < 0 || n > a.len ? 0 : n;
 }
 
-// A workgroup takes a head: the rank of the last one that stays by four passes of 8
-// bits over counts, then the places of all that stay, in order.
-__global__ __launch_bounds__(1024) void ld_kv4_select_k(Kv4EvictArgs a) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t s_prefix, s_left;
-  __shared__ uint32_t wsum[2][16];
+// A place of counts gains the lanes that are `in`: those of the same place are added
+// together for the first three places of a wave, since sums are of few sizes and atomics on
+// one place go one after the other.
+__device__ __forceinline__ void count_places(uint32_t* counts, uint32_t place, bool in) {
+  uint64_t left = __ballot(in);
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    if (!left) return;
+    const int first = __ffsll(static_cast<unsigned long long>(left)) - 1;
+    const uint32_t of = __builtin_amdgcn_readlane(place, first);
+    const uint64_t same = __ballot(in && place == of) & left;
+    if (lane == first) atomicAdd(&counts[of], static_cast<uint32_t>(__popcll(same)));
+    left &= ~same;
+  }
+  if (left >> lane & 1) atomicAdd(&counts[place], 1u);
+}
+
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+constexpr int kSelEach = 8, kSelMost = kSelThreads * kSelEach;  // positions a workgroup holds
+// A rank's three digits, of 11, 11 and 10 bits.
+constexpr int kDigit0 = 2048, kDigit1 = 2048, kDigit2 = 1024, kDigits = kDigit0 + kDigit1 + kDigit2;
+
+struct SelShared {
+  uint32_t waves[kSelWaves];
+  uint32_t found[2];
+  uint32_t n[2][kSelEach * kSelWaves];
+};
+
+// Of N counts, the place of the left-th largest and how many are left there: found.  By all
+// threads, each N / 1024 places in falling order.
+template <int N>
+__device__ __forceinline__ void find_place(const uint32_t* counts, uint32_t left, SelShared& sh) {
+  constexpr int PER = N / kSelThreads;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint32_t c[PER], sum = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    c[i] = counts[N - 1 - (tid * PER + i)];
+    sum += c[i];
+  }
+  uint32_t upto = sum;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint32_t x = static_cast<uint32_t>(__shfl_up(static_cast<int>(upto), d, 64));
+    if (lane >= d) upto += x;
+  }
+  if (lane == 63) sh.waves[wave] = upto;
+  __syncthreads();
+  uint32_t before = upto - sum;
+#pragma unroll
+  for (int w = 0; w < kSelWaves; ++w) before += w < wave ? sh.waves[w] : 0;
+  if (before < left && left <= before + sum) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (before < left && left <= before + c[i]) {
+        sh.found[0] = N - 1 - (tid * PER + i);
+        sh.found[1] = left - before;
+      }
+      before += c[i];
+    }
+  }
+  __syncthreads();
+}
+
+// Writes the positions first + kSelThreads e + thread that stay, in their order, from idx
+// + at on: those with a rank above `least`, and the first `ties` of those at it.
+template <int EACH>
+__device__ __forceinline__ void emit(const uint32_t (&rank)[EACH], int first, int end, uint32_t least, uint32_t ties,
+                                     uint32_t at, int32_t* idx, SelShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const bool in = first + kSelThreads * e + tid < end;
+    const uint64_t mo = __ballot(in && rank[e] > least), ms = __ballot(in && rank[e] == least);
+    if (lane == 0) {
+      sh.n[0][e * kSelWaves + wave] = __popcll(mo);
+      sh.n[1][e * kSelWaves + wave] = __popcll(ms);
+    }
+  }
+  __syncthreads();
+  // numbers before each 64 positions: the first two waves add up, EACH / 4 of them a lane
+  constexpr int PER = EACH / 4;
+  if (wave < 2) {
+    uint32_t c[PER], sum = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      c[i] = sh.n[wave][lane * PER + i];
+      sum += c[i];
+    }
+    uint32_t upto = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const uint32_t x = static_cast<uint32_t>(__shfl_up(static_cast<int>(upto), d, 64));
+      if (lane >= d) upto += x;
+    }
+    uint32_t before = upto - sum;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      sh.n[wave][lane * PER + i] = before;
+      before += c[i];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const int i = first + kSelThreads * e + tid;
+    const bool over = i < end && rank[e] > least, same = i < end && rank[e] == least;
+    const uint64_t mo = __ballot(over), ms = __ballot(same);
+    const uint32_t o = sh.n[0][e * kSelWaves + wave] + __popcll(mo & below);
+    const uint32_t s = sh.n[1][e * kSelWaves + wave] + __popcll(ms & below);  // ties before
+    if (over || (same && s < ties)) idx[at + o + min(s, ties)] = i;
+  }
+}
+
+__device__ __forceinline__ uint32_t rank_digit(uint32_t u, int pass) {
+  return pass == 0 ? u >> 21 : pass == 1 ? u >> 10 & 2047 : u & 1023;
+}
+__device__ __forceinline__ uint32_t rank_above(uint32_t u, int pass) { return pass == 0 ? 0 : pass == 1 ? u >> 21 : u >> 10; }
+
+// Up to kSelMost positions: a workgroup takes a head and holds their ranks; the rank of the
+// last one that stays by three passes over counts of a digit.
+__global__ __launch_bounds__(kSelThreads) void ld_kv4_select_k(Kv4EvictArgs a) {
+  __shared__ uint32_t counts[kDigits];
+  __shared__ SelShared sh;
+  const int tid = threadIdx.x;
   const int h = blockIdx.x, b = blockIdx.y, n = evict_len(a, b);
   const int64_t head = static_cast<int64_t>(b) * a.from.KV + h;
   int32_t* idx = a.idx + head * a.keep;
   if (n <= a.keep) {
-    for (int i = tid; i < a.keep; i += 1024) idx[i] = i < n ? i : -1;
+    for (int i = tid; i < a.keep; i += kSelThreads) idx[i] = i < n ? i : -1;
     return;
   }
   const float* sums = a.from.sums + head * a.from.s_max;
   const int old = n - a.recent;
-  uint32_t left = a.keep - a.recent, prefix = 0, mask = 0;  // of those with the prefix `left` stay
-  for (int shift = 24; shift >= 0 && left; shift -= 8) {
-    for (int i = tid; i < 256; i += 1024) hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < old; i += 1024) {
-      const uint32_t u = evict_rank(sums[i]);
-      if ((u & mask) == prefix) atomicAdd(&hist[(u >> shift) & 255], 1u);
-    }
-    __syncthreads();
-    if (tid == 0) {
-      uint32_t more = 0;
-      int d = 255;
-      while (d > 0 && more + hist[d] < left) more += hist[d--];
-      s_prefix = prefix | static_cast<uint32_t>(d) << shift;
-      s_left = left - more;
-    }
-    __syncthreads();
-    prefix = s_prefix;
-    left = s_left;
-    mask |= 255u << shift;
-    __syncthreads();
+  for (int i = tid; i < a.recent; i += kSelThreads) idx[a.keep - a.recent + i] = old + i;
+  if (a.keep == a.recent) return;
+  uint32_t rank[kSelEach];
+#pragma unroll
+  for (int e = 0; e < kSelEach; ++e) {
+    const int i = tid + kSelThreads * e;
+    rank[e] = i < old ? evict_rank(sums[i]) : 0u;
   }
-  // those above the prefix stay, and the first `left` of those at it
-  const bool none = a.keep == a.recent;
-  uint32_t kept = 0, same = 0;
-  for (int i0 = 0; i0 < old; i0 += 1024) {
-    const int i = i0 + tid;
-    const uint32_t u = i < old ? evict_rank(sums[i]) : 0u;
-    const bool over = !none && i < old && u > prefix, eq = !none && i < old && u == prefix;
-    const uint64_t below = (1ull << lane) - 1, me = __ballot(eq);
-    if (lane == 0) wsum[0][wave] = __popcll(me);
-    __syncthreads();
-    uint32_t before = same, all_eq = 0;
-    for (int w = 0; w < 16; ++w) {
-      before += w < wave ? wsum[0][w] : 0;
-      all_eq += wsum[0][w];
+  for (int i = tid; i < kDigits; i += kSelThreads) counts[i] = 0;
+  __syncthreads();
+  uint32_t left = a.keep - a.recent, prefix = 0;  // of those with the prefix `left` stay
+#pragma unroll
+  for (int p = 0; p < 3; ++p) {
+    uint32_t* of = counts + (p == 0 ? 0 : p == 1 ? kDigit0 : kDigit0 + kDigit1);
+#pragma unroll
+    for (int e = 0; e < kSelEach; ++e) {
+      if (kSelThreads * e >= old) break;  // uniform
+      count_places(of, rank_digit(rank[e], p), tid + kSelThreads * e < old && rank_above(rank[e], p) == prefix);
     }
-    const bool stay = over || (eq && before + __popcll(me & below) < left);
-    const uint64_t mo = __ballot(stay);
-    if (lane == 0) wsum[1][wave] = __popcll(mo);
     __syncthreads();
-    uint32_t at = kept, all = 0;
-    for (int w = 0; w < 16; ++w) {
-      at += w < wave ? wsum[1][w] : 0;
-      all += wsum[1][w];
-    }
-    if (stay) idx[at + __popcll(mo & below)] = i;
-    kept += all;
-    same += all_eq;
+    if (p < 2)
+      find_place<2048>(of, left, sh);
+    else
+      find_place<kDigit2>(of, left, sh);
+    prefix = prefix << (p < 2 ? 11 : 10) | sh.found[0];
+    left = sh.found[1];
   }
-  for (int i = tid; i < a.recent; i += 1024) idx[a.keep - a.recent + i] = old + i;
+  emit<kSelEach>(rank, 0, old, prefix, left, 0, idx, sh);
+}
+
+// More positions: workgroups of kPiece of them, a launch for each digit, whose counts meet
+// in memory.  Scratch of a head: the three digits' counts; after each, the prefix so far and
+// how many are left at it; each piece's numbers above the last one that stays and equal to it.
+constexpr int kPiece = 4096, kPieceEach = kPiece / kSelThreads;
+constexpr int kFound = kDigits, kPieces = kDigits + 8;
+
+__global__ __launch_bounds__(256) void ld_kv4_select_zero_k(uint32_t* ws, int64_t stride) {
+  uint32_t* counts = ws + blockIdx.y * stride;
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < kDigits; i += gridDim.x * 256) counts[i] = 0;
+}
+
+// PASS 0 to 2: counts of that digit; 3: a piece's numbers; 4: places.
+template <int PASS>
+__global__ __launch_bounds__(kSelThreads) void ld_kv4_select_pass_k(Kv4EvictArgs a, int64_t stride) {
+  __shared__ uint32_t counts[PASS < 3 ? 2048 : 1];
+  __shared__ SelShared sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int piece = blockIdx.x, h = blockIdx.y, b = blockIdx.z, n = evict_len(a, b), pieces = gridDim.x;
+  const int64_t head = static_cast<int64_t>(b) * a.from.KV + h;
+  int32_t* idx = a.idx + head * a.keep;
+  const int old = n - a.recent, first = piece * kPiece;
+  if (n <= a.keep || a.keep == a.recent) {
+    if (PASS == 4)
+      for (int i = piece * kSelThreads + tid; i < a.keep; i += pieces * kSelThreads)
+        idx[i] = n <= a.keep ? (i < n ? i : -1) : old + i;
+    return;
+  }
+  if (PASS == 4)
+    for (int i = piece * kSelThreads + tid; i < a.recent; i += pieces * kSelThreads) idx[a.keep - a.recent + i] = old + i;
+  if (first >= old) return;
+  uint32_t* ws = a.ws + head * stride;
+  uint32_t* per_piece = ws + kPieces;
+  const float* sums = a.from.sums + head * a.from.s_max;
+  uint32_t rank[kPieceEach];
+#pragma unroll
+  for (int e = 0; e < kPieceEach; ++e) {
+    const int i = first + tid + kSelThreads * e;
+    rank[e] = i < old ? evict_rank(sums[i]) : 0u;
+  }
+  if constexpr (PASS < 3) {
+    counts[tid] = 0;
+    counts[tid + kSelThreads] = 0;
+  }
+  // what the pass before counted; a head's workgroups all find it, the first notes it
+  uint32_t left = a.keep - a.recent, prefix = 0;
+  if constexpr (PASS == 4) {
+    prefix = ws[kFound + 4];
+    left = ws[kFound + 5];
+  } else if constexpr (PASS > 0) {
+    if constexpr (PASS > 1) {
+      prefix = ws[kFound + 2 * (PASS - 2)];
+      left = ws[kFound + 2 * (PASS - 2) + 1];
+    }
+    if constexpr (PASS == 3)
+      find_place<kDigit2>(ws + kDigit0 + kDigit1, left, sh);
+    else
+      find_place<2048>(ws + (PASS == 2 ? kDigit0 : 0), left, sh);
+    prefix = prefix << (PASS == 3 ? 10 : 11) | sh.found[0];
+    left = sh.found[1];
+    if (piece == 0 && tid == 0) {
+      ws[kFound + 2 * (PASS - 1)] = prefix;
+      ws[kFound + 2 * (PASS - 1) + 1] = left;
+    }
+  }
+  if constexpr (PASS < 3) {
+    if (PASS == 0) __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kPieceEach; ++e) {
+      if (first + kSelThreads * e >= old) break;  // uniform
+      count_places(counts, rank_digit(rank[e], PASS),
+                   first + tid + kSelThreads * e < old && rank_above(rank[e], PASS) == prefix);
+    }
+    __syncthreads();
+    uint32_t* to = ws + (PASS == 0 ? 0 : PASS == 1 ? kDigit0 : kDigit0 + kDigit1);
+    for (int i = tid; i < (PASS == 2 ? kDigit2 : 2048); i += kSelThreads)
+      if (counts[i]) atomicAdd(&to[i], counts[i]);
+  } else if constexpr (PASS == 3) {
+    uint32_t over = 0, same = 0;
+#pragma unroll
+    for (int e = 0; e < kPieceEach; ++e) {
+      const bool in = first + tid + kSelThreads * e < old;
+      over += __popcll(__ballot(in && rank[e] > prefix));
+      same += __popcll(__ballot(in && rank[e] == prefix));
+    }
+    if (lane == 0) {
+      sh.n[0][wave] = over;
+      sh.n[1][wave] = same;
+    }
+    __syncthreads();
+    if (tid < 2) {
+      uint32_t all = 0;
+      for (int w = 0; w < kSelWaves; ++w) all += sh.n[tid][w];
+      per_piece[2 * piece + tid] = all;
+    }
+  } else {
+    // numbers of the pieces before
+    uint32_t over = 0, same = 0;
+    for (int i = lane; i < piece; i += 64) {
+      over += per_piece[2 * i];
+      same += per_piece[2 * i + 1];
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      over += static_cast<uint32_t>(__shfl_xor(static_cast<int>(over), d, 64));
+      same += static_cast<uint32_t>(__shfl_xor(static_cast<int>(same), d, 64));
+    }
+    same = min(same, left);
+    emit<kPieceEach>(rank, first, old, prefix, left - same, over + same, idx, sh);
+  }
 }
 
 // A wave takes a tile of 8 places of the smaller cache: their keys, values, scales
-// and sums.
+// and sums.  A position's values lie in 8 (4) lines of its tile, so that the values of a
+// cache are read as a whole where few positions stay.
 template <int DH>
 __global__ __launch_bounds__(256) void ld_kv4_gather_k(Kv4EvictArgs a) {
   constexpr int JN = DH / 32, TB = DH * 4;
@@ -779,24 +988,43 @@ __global__ __launch_bounds__(256) void ld_kv4_gather_k(Kv4EvictArgs a) {
   const uint8_t* sf = a.from.scales + head * 2 * a.from.s8 * JN;
   uint8_t* st = a.to.scales + head * 2 * a.to.s8 * JN;
   const int have = min(n - t0, 8);
-  // keys: DH / 16 lanes of 8 bytes a row
-  for (int e = lane; e < have * (DH / 16); e += 64) {
-    const int r = e / (DH / 16), o = e % (DH / 16) * 8;
-    *reinterpret_cast<u32x2*>(kt + static_cast<int64_t>(t0 + r) * (DH / 2) + o) =
-        *reinterpret_cast<const u32x2*>(kf + static_cast<int64_t>(idx[r]) * (DH / 2) + o);
-  }
-  // values: byte by byte
-  for (int e = lane; e < DH / 2; e += 64)
-    for (int r = 0; r < have; ++r) {
-      const int i = idx[r];
-      vt[static_cast<int64_t>(t0 >> 3) * TB + e * 8 + r] = vf[static_cast<int64_t>(i >> 3) * TB + e * 8 + (i & 7)];
+  // the tile's positions (past the last: the first again)
+  const int mine = idx[(lane & 7) < have ? lane & 7 : 0];
+  int pos[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) pos[r] = __builtin_amdgcn_readlane(mine, r);
+  // values: a lane 8 bytes of a tile, one of each position
+  const int e = lane * 8 % TB;  // (heads of 64: half the lanes)
+  uint32_t v[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) v[r] = vf[static_cast<int64_t>(pos[r] >> 3) * TB + e + (pos[r] & 7)];
+  // keys: a lane DH / 16 bytes of row lane / 8
+  typedef uint32_t KRow __attribute__((ext_vector_type(DH / 64)));
+  const int row = lane >> 3, src = __shfl(mine, row, 64);
+  const KRow k = *reinterpret_cast<const KRow*>(kf + static_cast<int64_t>(src) * (DH / 2) + (lane & 7) * (DH / 16));
+  // scales: a byte a lane, keys' then values'
+  const int sr = lane / JN & 7, sj = lane % JN, sp = lane / (8 * JN);
+  const int from_pos = __shfl(mine, sr, 64);
+  const bool scale = sp < 2 && sr < have;
+  uint8_t s = 0;
+  if (scale) s = sf[(static_cast<int64_t>(sp) * a.from.s8 + from_pos) * JN + sj];
+  float w = 0.f;
+  const bool sum = a.to.sums && lane < have;
+  if (sum) w = a.from.sums[head * a.from.s_max + mine];
+
+  if (row < have) *reinterpret_cast<KRow*>(kt + static_cast<int64_t>(t0 + row) * (DH / 2) + (lane & 7) * (DH / 16)) = k;
+  uint8_t* to = vt + static_cast<int64_t>(t0 >> 3) * TB + e;
+  if (lane * 8 < TB) {
+    if (have == 8) {
+      *reinterpret_cast<u32x2*>(to) = u32x2{v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24, v[4] | v[5] << 8 | v[6] << 16 | v[7] << 24};
+    } else {
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+        if (r < have) to[r] = static_cast<uint8_t>(v[r]);
     }
-  for (int e = lane; e < have * 2 * JN; e += 64) {
-    const int r = e / (2 * JN), part = e / JN % 2, jj = e % JN;
-    st[(static_cast<int64_t>(part) * a.to.s8 + t0 + r) * JN + jj] =
-        sf[(static_cast<int64_t>(part) * a.from.s8 + idx[r]) * JN + jj];
   }
-  if (a.to.sums && lane < have) a.to.sums[head * a.to.s_max + t0 + lane] = a.from.sums[head * a.from.s_max + idx[lane]];
+  if (scale) st[(static_cast<int64_t>(sp) * a.to.s8 + t0 + sr) * JN + sj] = s;
+  if (sum) a.to.sums[head * a.to.s_max + t0 + lane] = w;
 }
 
 // Workgroups in two dimensions: one takes 2^32 threads at most.
@@ -898,10 +1126,31 @@ hipError_t launch_kv4_sums(const Kv4AttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-size_t kv4_evict_ws_bytes(const Kv4View&, int64_t, int64_t) { return 0; }
+namespace {
+// Words of scratch a head, where its positions go in pieces.
+int64_t select_stride(int64_t len) { return len <= kSelMost ? 0 : kPieces + 2 * div_up(len, kPiece); }
+}  // namespace
+
+size_t kv4_evict_ws_bytes(const Kv4View& from, int64_t len) {
+  return static_cast<size_t>(from.n_seq) * from.KV * select_stride(len) * 4;
+}
 
 hipError_t launch_kv4_select(const Kv4EvictArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(ld_kv4_select_k, dim3(a.from.KV, a.from.n_seq), dim3(1024), 0, s, a);
+  const int64_t stride = select_stride(a.len);
+  if (!stride) {
+    hipLaunchKernelGGL(ld_kv4_select_k, dim3(a.from.KV, a.from.n_seq), dim3(kSelThreads), 0, s, a);
+    return hipGetLastError();
+  }
+  const dim3 grid(div_up(a.len, kPiece), a.from.KV, a.from.n_seq), block(kSelThreads);
+  const int64_t heads = static_cast<int64_t>(a.from.KV) * a.from.n_seq;
+  // (a launch takes 65535 in its second dimension)
+  for (int64_t h = 0; h < heads; h += 65535)
+    hipLaunchKernelGGL(ld_kv4_select_zero_k, dim3(4, heads - h < 65535 ? heads - h : 65535), dim3(256), 0, s, a.ws + h * stride, stride);
+  hipLaunchKernelGGL(ld_kv4_select_pass_k<0>, grid, block, 0, s, a, stride);
+  hipLaunchKernelGGL(ld_kv4_select_pass_k<1>, grid, block, 0, s, a, stride);
+  hipLaunchKernelGGL(ld_kv4_select_pass_k<2>, grid, block, 0, s, a, stride);
+  hipLaunchKernelGGL(ld_kv4_select_pass_k<3>, grid, block, 0, s, a, stride);
+  hipLaunchKernelGGL(ld_kv4_select_pass_k<4>, grid, block, 0, s, a, stride);
   return hipGetLastError();
 }
 

@@ -81,7 +81,7 @@ void plan_attn_decode_kv4(Kv4AttnArgs& a);
 hipError_t launch_attn_decode_kv4(const Kv4AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_decode_kv4_combine(const Kv4AttnArgs& a, hipStream_t s);
 hipError_t launch_kv4_sums(const Kv4AttnArgs& a, hipStream_t s);
-size_t kv4_evict_ws_bytes(const Kv4View& from, int64_t len, int64_t keep);
+size_t kv4_evict_ws_bytes(const Kv4View& from, int64_t len);
 hipError_t launch_kv4_select(const Kv4EvictArgs& a, hipStream_t s);
 hipError_t launch_kv4_gather(const Kv4EvictArgs& a, hipStream_t s);
 
