@@ -18,6 +18,8 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kKv4Waves = 8;  // of an attention workgroup
@@ -243,7 +245,7 @@ __global__ __launch_bounds__(256) void ld_kv4_load_k(Kv4LoadArgs a) {
 // --------------------------------------------------------------- attention
 
 // Keys of a chunk of a sequence of nk: a.chunk_keys, and where lengths are the device's
-// more in a sequence that would make more than a.n_chunks of them.
+// a.chunk_keys at least.
 __device__ __forceinline__ int kv4_chunk_keys(const Kv4AttnArgs& a, int nk) {
   if (!a.seq_pos) return a.chunk_keys;
   const uint32_t n = a.n_chunks, even = ((static_cast<uint32_t>(nk) + n - 1) / n + 63) & ~63u;
@@ -272,26 +274,90 @@ struct Kv4Parts {
   }
 };
 
+// A query row as the second operand of the scaled 16x16x128 product: lane 16 g + n has row n's
+// dimensions 16 g .. + 15 and 64 + 16 g .. + 15 as 8-bit floats, and in `scale` the scales of
+// dimensions 32 g .. + 31, bytes 0 and 1 of the two parts.  The first part has four of a bf16's
+// eight bits, the second the other four: all of it down to 2^-14 of the largest of 32
+// dimensions, and 2^-21 of that below.  Not finite: NaN.
+template <int DH>
+__device__ __forceinline__ void split_query(const bf16* q, int lane, i32x4 (&to)[2][2][64], uint32_t (&scale)[64]) {
+  const int g = lane >> 4;
+  uint32_t sb[2] = {127u, 127u};
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    i32x4 p1 = 0, p2 = 0;
+    if (half * 64 < DH) {
+      union {
+        bf16x8 v[2];
+        bf16x2 p[8];
+        ushortx2 u[8];
+      } x;
+      x.v[0] = *reinterpret_cast<const bf16x8*>(q + 64 * half + 16 * g);
+      x.v[1] = *reinterpret_cast<const bf16x8*>(q + 64 * half + 16 * g + 8);
+      ushortx2 m2{0, 0};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m2 = __builtin_elementwise_max(m2, x.u[i] & static_cast<unsigned short>(0x7fff));
+      uint32_t m = max(m2[0], m2[1]);
+      m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16, 64)));
+      // the largest to 128 .. 256 of the formats' 448
+      sb[half] = m >= 0x7f80u ? kNanScale : max(static_cast<int>(m >> 7) - 7, 16);
+      const float s1 = __builtin_bit_cast(float, min(sb[half], 254u) << 23), s2 = s1 * 0x1p-5f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        typedef short s16x2 __attribute__((ext_vector_type(2)));
+        s16x2 a{0, 0}, c{0, 0};
+        a = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(a, x.p[2 * i], s1, false);
+        a = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(a, x.p[2 * i + 1], s1, true);
+        const uint32_t ab = __builtin_bit_cast(uint32_t, a);
+        // what is left has four bits too
+        const bf16x2 r0 = x.p[2 * i] - __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(ab, s1, false);
+        const bf16x2 r1 = x.p[2 * i + 1] - __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(ab, s1, true);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, r0, s2, false);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, r1, s2, true);
+        p1[i] = static_cast<int>(ab);
+        p2[i] = __builtin_bit_cast(int, c);
+      }
+    }
+    to[0][half][lane] = p1;
+    to[1][half][lane] = p2;
+  }
+  // blocks 0, 1: first halves of lane groups 0 and 2; 2, 3: second halves
+  const int from = 32 * (g & 1) + (lane & 15);
+  const uint32_t s0 = static_cast<uint32_t>(__shfl(static_cast<int>(sb[0]), from, 64));
+  const uint32_t s1 = static_cast<uint32_t>(__shfl(static_cast<int>(sb[1]), from, 64));
+  const uint32_t s = g < 2 ? s0 : s1;
+  scale[lane] = s | (s == kNanScale ? kNanScale : s - 5) << 8;
+}
+
 // A workgroup of eight waves takes a chunk of keys of one key/value head for 16
-// rows (of its query heads' new rows); a wave 16 TT keys at a time, with its own running
+// rows (of its query heads' new rows); a wave 32 keys at a time, with its own running
 // maximum and sum; they meet once, to add up.
 //
-// Scores S^T = K Q^T and output O^T = V^T P^T on the matrix cores (16x16x32
-// bf16).  The A rows of score product t are the keys LK g + 4 t + r (row 4 g + r), LK =
-// 4 TT, so lane group g = lane / 16 of the result holds keys LK g + 4 t + r, r < 4, of its
-// query row: LK neighbouring keys, whole tiles of the cache's values.  They are the B
-// operand of O^T as they stand.  A lane's k of the scores are DH / 4 neighbouring
-// dimensions, DH / 8 bytes of a key, of one scale.
+// Scores S^T = K Q^T and output O^T = V^T P^T on the matrix cores.  The scores are scaled
+// 16x16x128 products whose first operand is the cache's codes and scales as they lie (16
+// bytes of a key a lane); the second is the queries' two 8-bit parts.  The output's are
+// 16x16x32 in bf16.  Row 4 g + r of score product t is key 8 g + 4 t + r, so lane group g =
+// lane / 16 of the results holds 8 neighbouring keys of its query row, whole tiles of the
+// cache's values: they are the second operand of O^T as they stand.
 //
 // Values are converted in pairs of dimensions, which share position and scale, and put
 // together over positions by byte permutes.  A probability goes in as three bf16 parts,
-// which are all of its 24 bits.
+// which are all of its 24 bits (two: 3% less time, 2^-17 of a weight lost).
+//
+// What bounds it: the issue of vector instructions, about 210 a turn of a wave.  So the
+// registers are kept to four waves of a SIMD (more loads in flight with two were slower),
+// the maximum is renewed only where it has to be, and NaN is looked for only in turns that
+// masks cut.  2 sequences of 131072 keys, 32 heads over 8 of 128 dimensions: 61 us, 4.7
+// TB/s of the cache (75 with the scores in bf16 and the sums rescaled each turn).  16 uneven
+// sequences of 32 heads, 68000 keys in all: 43 us (48).
 template <int DH, int NQ>
 __global__ __launch_bounds__(64 * kKv4Waves, 4) void ld_attn_decode_kv4_k(Kv4AttnArgs a) {
-  constexpr int NS = DH / 32, JN = DH / 32, MT = DH / 16, NW = kKv4Waves, TT = DH == 64 ? 4 : 2, LK = 4 * TT, WK = 16 * TT;
+  constexpr int JN = DH / 32, MT = DH / 16, NW = kKv4Waves, TT = 2, LK = 4 * TT, WK = 16 * TT;
   constexpr int VT = LK / 8, TB = DH * 4;  // value tiles a lane group; bytes of one
   __shared__ float ml[NW][NQ][2];
   __shared__ __align__(16) float red[NW][NQ][DH];
+  __shared__ __align__(16) i32x4 qs[2][2][64];  // the queries' parts as operands (in registers they would not fit)
+  __shared__ uint32_t qscale[64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
   const Kv4View& c = a.kv;
@@ -339,10 +405,9 @@ __global__ __launch_bounds__(64 * kKv4Waves, 4) void ld_attn_decode_kv4_k(Kv4Att
   // Keys k0 .. k0 + WK - 1 (past the last key: key 0, masked later): row n of
   // product t, dimensions DH / 4 g + 0 .. DH / 4 - 1.
   const int krow = LK * (n >> 2) + (n & 3);
-  typedef uint32_t KRaw __attribute__((ext_vector_type(NS)));
   typedef uint32_t VRaw __attribute__((ext_vector_type(4)));
   typedef uint32_t SRaw __attribute__((ext_vector_type(2 * JN)));
-  KRaw kr[TT];
+  i32x4 kr[TT];
   uint32_t sk[TT];
   union {
     VRaw q[JN / 2];
@@ -352,58 +417,132 @@ __global__ __launch_bounds__(64 * kKv4Waves, 4) void ld_attn_decode_kv4_k(Kv4Att
     SRaw q;
     uint32_t d[2 * JN];
   } sv[VT];  // [position][j] bytes
+  // (a wave's turn is where its scalar base is; what a lane adds does not change)
+  const uint32_t kg = g & (JN - 1), k_at = krow * (DH / 2) + 16 * kg, ks_at = krow * JN + kg;
+  const uint32_t v_at = LK / 8 * g * TB + n * (8 * JN), vs_at = LK * g * JN;
   auto load_keys = [&](int k0) {
-    const bool whole = k0 + WK <= nk;
+    if (k0 + WK <= nk) {
+      const uint8_t *kb = kc + static_cast<int64_t>(k0) * (DH / 2), *ksb = ks + static_cast<int64_t>(k0) * JN;
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-      int kk = k0 + krow + 4 * t;
-      if (!whole) kk = kk < nk ? kk : 0;
-      kr[t] = *reinterpret_cast<const KRaw*>(kc + static_cast<int64_t>(kk) * (DH / 2) + DH / 8 * g);
-      sk[t] = ks[static_cast<int64_t>(kk) * JN + (DH / 4 * g) / 32];
+      for (int t = 0; t < TT; ++t) {
+        kr[t] = *reinterpret_cast<const i32x4*>(kb + (k_at + 4 * t * (DH / 2)));
+        sk[t] = ksb[ks_at + 4 * t * JN];
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        int kk = k0 + krow + 4 * t;
+        kk = kk < nk ? kk : 0;
+        kr[t] = *reinterpret_cast<const i32x4*>(kc + static_cast<int64_t>(kk) * (DH / 2) + 16 * kg);
+        sk[t] = ks[static_cast<int64_t>(kk) * JN + kg];
+      }
     }
   };
   auto load_values = [&](int k0) {
+    if (k0 + WK <= nk) {
+      const uint8_t *vb = vc + static_cast<int64_t>(k0) * (DH / 2), *vsb = vs + static_cast<int64_t>(k0) * JN;
 #pragma unroll
-    for (int v = 0; v < VT; ++v) {
-      const int f = k0 + LK * g + 8 * v, fc = f < nk ? f : 0;
-      const uint8_t* at = vc + static_cast<int64_t>(fc >> 3) * TB + n * (8 * JN);
+      for (int v = 0; v < VT; ++v) {
 #pragma unroll
-      for (int i = 0; i < JN / 2; ++i) vr[v].q[i] = *reinterpret_cast<const VRaw*>(at + 16 * i);
-      sv[v].q = *reinterpret_cast<const SRaw*>(vs + static_cast<int64_t>(fc) * JN);
+        for (int i = 0; i < JN / 2; ++i) vr[v].q[i] = *reinterpret_cast<const VRaw*>(vb + (v_at + v * TB + 16 * i));
+        sv[v].q = *reinterpret_cast<const SRaw*>(vsb + (vs_at + 8 * v * JN));
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < VT; ++v) {
+        const int f = k0 + LK * g + 8 * v, fc = f < nk ? f : 0;
+        const uint8_t* at = vc + static_cast<int64_t>(fc >> 3) * TB + n * (8 * JN);
+#pragma unroll
+        for (int i = 0; i < JN / 2; ++i) vr[v].q[i] = *reinterpret_cast<const VRaw*>(at + 16 * i);
+        sv[v].q = *reinterpret_cast<const SRaw*>(vs + static_cast<int64_t>(fc) * JN);
+      }
     }
   };
 
   const uint32_t row = r0 + min(n, rows - 1), j = row % static_cast<uint32_t>(a.n_new);
   const int qh = h * G + row / static_cast<uint32_t>(a.n_new), qpos = p + j;
-  bf16x8 qf[NS];
-  {
-    const bf16* q = static_cast<const bf16*>(a.qkv) + (static_cast<int64_t>(b) * a.n_new + j) * a.ld_qkv +
-                    static_cast<int64_t>(qh) * DH;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(q + DH / 4 * g + 8 * s);
+  int k0 = k_first + wave * WK;
+  if (k0 < k_end) {
+    load_keys(k0);
+    load_values(k0);
   }
+  if (wave == 0)
+    split_query<DH>(static_cast<const bf16*>(a.qkv) + (static_cast<int64_t>(b) * a.n_new + j) * a.ld_qkv + static_cast<int64_t>(qh) * DH,
+                    lane, qs, qscale);
   const float al2 = a.alibi ? alibi_slope(qh, a.H) * kLog2e : 0.f, sl2 = a.scale * kLog2e;
 
-  float m = -INFINITY, l = 0.f;
+  // The scores are taken from a reference m, the largest score when it was last set: weights
+  // stay below 2^kSlack, and sums are scaled to a new one only when a score passes that.
+  constexpr float kSlack = 8.f;
+  float m = -INFINITY, mz = 0.f, l = 0.f;  // mz: m, or 0 where there is none
   floatx4 o[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  for (int k0 = k_first + wave * WK; k0 < k_end; k0 += WK * NW) {
-    load_keys(k0);
-    load_values(k0);
-    __builtin_amdgcn_sched_barrier(0);
+  // dimensions 32 jj .. + 31 of the output: values in pairs of dimensions, put together
+  // over positions
+  auto add_values = [&](int jj, const Kv4Parts<TT>& pw) {
+    bf16x8 lo[VT], hi[VT];
+#pragma unroll
+    for (int v = 0; v < VT; ++v) {
+      bf16x2 pr[8];
+      auto scale = [&](int q) {  // of position q, as the conversions take it
+        const uint32_t w = sv[v].d[q * JN / 4];
+        const int byte = q * JN % 4 + jj;
+        return __builtin_bit_cast(float, byte == 0 ? w << 23 : byte == 1 ? w << 15 : byte == 2 ? w << 7 : w >> 1);
+      };
+      pr[0] = pair_of<0>(vr[v].d[jj][0], scale(0));
+      pr[1] = pair_of<1>(vr[v].d[jj][0], scale(1));
+      pr[2] = pair_of<2>(vr[v].d[jj][0], scale(2));
+      pr[3] = pair_of<3>(vr[v].d[jj][0], scale(3));
+      pr[4] = pair_of<0>(vr[v].d[jj][1], scale(4));
+      pr[5] = pair_of<1>(vr[v].d[jj][1], scale(5));
+      pr[6] = pair_of<2>(vr[v].d[jj][1], scale(6));
+      pr[7] = pair_of<3>(vr[v].d[jj][1], scale(7));
+      u32x4 a0, a1;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t e = __builtin_bit_cast(uint32_t, pr[2 * i]), f = __builtin_bit_cast(uint32_t, pr[2 * i + 1]);
+        a0[i] = __builtin_amdgcn_perm(f, e, 0x05040100u);
+        a1[i] = __builtin_amdgcn_perm(f, e, 0x07060302u);
+      }
+      lo[v] = __builtin_bit_cast(bf16x8, a0);
+      hi[v] = __builtin_bit_cast(bf16x8, a1);
+    }
+#pragma unroll
+    for (int v = 0; v < VT; ++v)
+#pragma unroll
+      for (int part = 0; part < kKv4Parts; ++part) {
+        o[2 * jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo[v], pw.p[part][v], o[2 * jj], 0, 0, 0);
+        o[2 * jj + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi[v], pw.p[part][v], o[2 * jj + 1], 0, 0, 0);
+      }
+  };
+
+  __syncthreads();
+  const uint32_t q_scale = qscale[lane];
+  while (k0 < k_end) {
+    asm volatile("" ::: "memory");  // the queries are read each turn
     const int f = k0 + LK * g;  // the lane's keys
     float ss = sl2;             // of a product to a base-2 score
     floatx4 x[TT];
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-      x[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-      const float s = scale_byte<0>(sk[t]);
+    for (int t = 0; t < TT; ++t) x[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    // (heads of 64 leave the second half of the product's dimensions to zeros of the queries)
 #pragma unroll
-      for (int i = 0; i < NS; ++i)
-        x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16(kr[t][i], s), qf[i], x[t], 0, 0, 0);
+    for (int part = 0; part < 2; ++part) {
+      const i32x8 q = __builtin_shufflevector(qs[part][0][lane], qs[part][1][lane], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        const i32x8 k = __builtin_shufflevector(kr[t], kr[t], 0, 1, 2, 3, -1, -1, -1, -1);
+        const int s = static_cast<int>(DH == 64 && g >= 2 ? 127u : sk[t]);
+        if (part == 0)
+          x[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q, x[t], 4, 0, 0, s, 0, static_cast<int>(q_scale));
+        else
+          x[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q, x[t], 4, 0, 0, s, 1, static_cast<int>(q_scale));
+      }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    if (k0 + WK * NW < k_end) load_keys(k0 + WK * NW);  // (the values' when these are used)
     if (a.alibi) {
       const float far = al2 * static_cast<float>(qpos - f);
 #pragma unroll
@@ -420,38 +559,6 @@ __global__ __launch_bounds__(64 * kKv4Waves, 4) void ld_attn_decode_kv4_k(Kv4Att
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (f + 4 * t + r > qpos) x[t][r] = -INFINITY;
-    }
-    if (a.scores && n < rows) {
-      float* sc = a.scores + (head * R + r0 + n) * a.score_keys + f;
-#pragma unroll
-      for (int t = 0; t < TT; ++t) *reinterpret_cast<floatx4*>(sc + 4 * t) = x[t] * ss;
-    }
-    // the largest score: of the lane's products (their scale is positive), then of all
-    float mn = x[0][0];
-#pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) mn = fmaxf(mn, x[t][r]);
-    mn = fmaxf(m, mn * ss);
-    mn = fmaxf(mn, __shfl_xor(mn, 16, 64));
-    mn = fmaxf(mn, __shfl_xor(mn, 32, 64));
-    const float mz = mn == -INFINITY ? 0.f : mn;  // of nothing but -inf, whose weights are 0
-    if (__any(mn != m)) {
-      const float keep = __builtin_amdgcn_exp2f(m - mz);
-      l *= keep;
-#pragma unroll
-      for (int i = 0; i < MT; ++i) o[i] *= keep;
-    }
-    m = mn;
-#pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        x[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], ss, -mz));  // of a NaN score NaN
-        l += x[t][r];
-      }
-    bool bad = false;  // masked positions must not see NaN
-    if (cut) {
 #pragma unroll
       for (int v = 0; v < VT; ++v) {
         const int have = nk - f - 8 * v;  // positions of this tile; what is behind them may be anything
@@ -464,67 +571,77 @@ __global__ __launch_bounds__(64 * kKv4Waves, 4) void ld_attn_decode_kv4_k(Kv4Att
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          constexpr uint32_t one = JN == 4 ? 0x7f7f7f7fu : 0x7f7fu;
+          constexpr uint32_t one = JN == 4 ? 0x7f7f7f7fu : 0x7f7fu, full = JN == 4 ? ~0u : 0xffffu;
           const int at = q * JN / 4, sh = q * JN % 4 * 8;
-          constexpr uint32_t full = JN == 4 ? ~0u : 0xffffu;
           if (q >= have) sv[v].d[at] = (sv[v].d[at] & ~(full << sh)) | (one << sh);
-          const uint32_t z = ~sv[v].d[at];  // a byte of 255 is one of zero here
-          bad |= ((z - 0x01010101u) & ~z & 0x80808080u) != 0;
         }
       }
-      bad = __any(bad);
+      // Masked positions must not see NaN: here it goes to the rows that see its position,
+      // and the scale becomes one.
+#pragma unroll 1
+      for (int jj = 0; jj < JN; ++jj) {
+        int first = INT32_MAX;
+#pragma unroll
+        for (int v = 0; v < VT; ++v)
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const int at = q * JN / 4, sh = (q * JN % 4 + jj) * 8;
+            if (((sv[v].d[at] >> sh) & 255u) == kNanScale) {
+              first = min(first, f + 8 * v + q);
+              sv[v].d[at] ^= 0x80u << sh;
+            }
+          }
+        if (__any(first != INT32_MAX)) {
+          first = min(first, __shfl_xor(first, 16, 64));
+          first = min(first, __shfl_xor(first, 32, 64));
+          const float nan = first <= qpos ? __builtin_nanf("") : 0.f;
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+            if (i >> 1 == jj) o[i] += nan;
+        }
+      }
     }
+    if (a.scores && n < rows) {
+      float* sc = a.scores + (head * R + r0 + n) * a.score_keys + f;
+#pragma unroll
+      for (int t = 0; t < TT; ++t) *reinterpret_cast<floatx4*>(sc + 4 * t) = x[t] * ss;
+    }
+    // the largest of the lane's scores (their scale is positive)
+    float mx = x[0][0];
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[t][r]);
+    mx *= ss;
+    if (__any(mx > m + kSlack)) {
+      mx = fmaxf(m, mx);
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      mz = mx == -INFINITY ? 0.f : mx;  // of nothing but -inf, whose weights are 0
+      const float keep = __builtin_amdgcn_exp2f(m - mz);
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) o[i] *= keep;
+      m = mx;
+    }
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], ss, -mz));  // of a NaN score NaN
+        l += x[t][r];
+      }
+    __builtin_amdgcn_sched_barrier(0);
     Kv4Parts<TT> pw;
     pw.split(x);
 #pragma unroll
     for (int jj = 0; jj < JN; ++jj) {
-      if (bad) {  // NaN scales go with the weights of the rows that see them
-        floatx4 y[TT];
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int v = t >> 1, q = 4 * (t & 1) + r, at = q * JN / 4, sh = (q * JN % 4 + jj) * 8;
-            const bool nan = ((sv[v].d[at] >> sh) & 255u) == kNanScale;
-            y[t][r] = nan && f + 4 * t + r <= qpos ? __builtin_nanf("") : x[t][r];
-            if (nan) sv[v].d[at] ^= 0x80u << sh;  // 127: one
-          }
-        pw.split(y);
-      }
-#pragma unroll
-      for (int v = 0; v < VT; ++v) {
-        bf16x2 pr[8];
-#define LD_KV4_PAIR(q, B)                                                                          \
-  pr[q] = pair_of<B>(vr[v].d[jj][q / 4], __builtin_bit_cast(float, sv_shift(sv[v].d[q * JN / 4], q * JN % 4 + jj)))
-        auto sv_shift = [](uint32_t w, int byte) {
-          return byte == 0 ? w << 23 : byte == 1 ? w << 15 : byte == 2 ? w << 7 : w >> 1;
-        };
-        LD_KV4_PAIR(0, 0);
-        LD_KV4_PAIR(1, 1);
-        LD_KV4_PAIR(2, 2);
-        LD_KV4_PAIR(3, 3);
-        LD_KV4_PAIR(4, 0);
-        LD_KV4_PAIR(5, 1);
-        LD_KV4_PAIR(6, 2);
-        LD_KV4_PAIR(7, 3);
-#undef LD_KV4_PAIR
-        union {
-          bf16x8 v8;
-          uint32_t u[4];
-        } lo, hi;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t e = __builtin_bit_cast(uint32_t, pr[2 * i]), f2 = __builtin_bit_cast(uint32_t, pr[2 * i + 1]);
-          lo.u[i] = __builtin_amdgcn_perm(f2, e, 0x05040100u);
-          hi.u[i] = __builtin_amdgcn_perm(f2, e, 0x07060302u);
-        }
-#pragma unroll
-        for (int part = 0; part < kKv4Parts; ++part) {
-          o[2 * jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo.v8, pw.p[part][v], o[2 * jj], 0, 0, 0);
-          o[2 * jj + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi.v8, pw.p[part][v], o[2 * jj + 1], 0, 0, 0);
-        }
-      }
+      add_values(jj, pw);
+      __builtin_amdgcn_sched_barrier(0);  // (else all conversions go first, and spill)
     }
+    k0 += WK * NW;
+    if (k0 < k_end) load_values(k0);
+    __builtin_amdgcn_sched_barrier(0);
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
@@ -1079,7 +1196,10 @@ hipError_t combine_t(const Kv4AttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-constexpr int64_t kKv4MinChunk = 256, kKv4Wgs = 2048;
+// Workgroups that run at once, two on each of the 256 compute units; the most that a launch
+// without row tiles makes; keys of a workgroup's turn, and the fewest of a chunk where lengths
+// are the device's.
+constexpr int64_t kKv4AtOnce = 512, kKv4Wgs = 4 * kKv4AtOnce, kKv4Turn = 256, kKv4Uneven = 512;
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -1094,8 +1214,16 @@ int64_t attn_kv4_heads(const Kv4View& kv, int64_t H, int64_t n_new) {
 }
 
 int64_t attn_kv4_max_chunks(int64_t heads, int64_t keys) {
-  const int64_t by_keys = div_up(keys, kKv4MinChunk), by_wgs = div_up(kKv4Wgs, heads);
+  const int64_t by_keys = div_up(keys, kKv4Turn), by_wgs = div_up(kKv4Wgs, heads);
   return by_keys < by_wgs ? by_keys : by_wgs;
+}
+
+// What n chunks cost a launch, in tenths of the time that a turn takes with the compute units
+// full: of a workgroup alone on its unit, six; a round's start and its sums, ten; the launch
+// that joins chunks, six.
+static int64_t chunk_cost(int64_t heads, int64_t keys, int64_t n) {
+  const int64_t wgs = heads * n, turns = div_up(div_up(keys, n), kKv4Turn);
+  return div_up(wgs, kKv4AtOnce) * (turns * (2 * wgs <= kKv4AtOnce ? 6 : 10) + 10) + (n > 1 ? 6 : 0);
 }
 
 // A turn writes whole products' scores, 64 keys at most.
@@ -1106,9 +1234,22 @@ void plan_attn_decode_kv4(Kv4AttnArgs& a) {
   a.group = a.H / a.kv.KV;
   a.tiles = (a.group * a.n_new + 15) / 16;
   const int64_t heads = attn_kv4_heads(a.kv, a.H, a.n_new);
-  int64_t n = attn_kv4_max_chunks(heads, keys);
-  a.chunk_keys = static_cast<int32_t>(div_up(div_up(keys, n), 64) * 64);
-  a.n_chunks = static_cast<int32_t>(div_up(keys, a.chunk_keys));
+  const int64_t most = attn_kv4_max_chunks(heads, keys);
+  if (a.seq_pos) {
+    const int64_t n = div_up(keys, kKv4Uneven);
+    a.n_chunks = static_cast<int32_t>(n < most ? n : most);
+    a.chunk_keys = static_cast<int32_t>(kKv4Uneven);
+  } else {
+    int64_t best = INT64_MAX, n = 1;
+    for (int64_t half = 1; half <= 2 * kKv4Wgs / kKv4AtOnce; ++half) {
+      int64_t c = half * kKv4AtOnce / 2 / heads;
+      c = c < 1 ? 1 : c > most ? most : c;
+      const int64_t cost = chunk_cost(heads, keys, c);
+      if (cost < best) best = cost, n = c;
+    }
+    a.chunk_keys = static_cast<int32_t>(div_up(div_up(keys, n), 64) * 64);
+    a.n_chunks = static_cast<int32_t>(div_up(keys, a.chunk_keys));
+  }
   a.score_keys = attn_kv4_score_keys(keys);
 }
 
