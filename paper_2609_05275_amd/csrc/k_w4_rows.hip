@@ -36,28 +36,15 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_rows(W4GemmArgs a) {
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) acc[i][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  u32x4 w[CG][2];  // as loaded two tiles, then two halves
+  u32x4 w[CG][2];  // halves of a chunk
   SRaw sw[CG][2];
-  auto load_w = [&](int i, int c) {
+  auto load_w = [&](int i, int c, int half) {
     const bool is_up = glu && i >= CG / 2;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int t = min(first + (is_up ? i - CG / 2 : i) * 2 + e, part_tiles - 1) + (is_up ? part_tiles : 0);
-      const int64_t block = static_cast<int64_t>(t) * C + c;
-      w[i][e] = reinterpret_cast<const u32x4*>(a.w.codes)[block * 64 + lane];
-      sw[i][e] = static_cast<const SRaw*>(a.w.scales)[block * 16 + n16];
-    }
-  };
-  auto swap_halves = [&](int i) {
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const uint32_t q0 = w[i][0][s], q1 = w[i][1][s];
-      w[i][0][s] = swap_in<0xc>(q0, q1);
-      w[i][1][s] = swap_in<0x3>(q1, q0);
-    }
-    const SRaw s0 = sw[i][0], s1 = sw[i][1];
-    sw[i][0] = swap_in<0xc>(s0, s1);
-    sw[i][1] = swap_in<0x3>(s1, s0);
+    const int t = min(first + (is_up ? i - CG / 2 : i) * 2 + (n16 >> 3), part_tiles - 1) + (is_up ? part_tiles : 0);
+    const int64_t block = static_cast<int64_t>(t) * C + c;
+    const int at = 8 * half + (n16 & 7);
+    w[i][half] = reinterpret_cast<const u32x4*>(a.w.codes)[block * 64 + 16 * g + at];
+    sw[i][half] = static_cast<const SRaw*>(a.w.scales)[block * 16 + at];
   };
   const bf16x8* rows = static_cast<const bf16x8*>(a.ws) + lane;
   bf16x8 x[2][2][MB];  // two steps, the next two
@@ -70,7 +57,9 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_rows(W4GemmArgs a) {
   if (wave < C) {
     load_x(x[0], wave * 4);
 #pragma unroll
-    for (int i = 0; i < CG; ++i) load_w(i, wave);
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int i = 0; i < CG; ++i) load_w(i, wave, half);
   }
   for (int c = wave; c < C; c += kWaves) {
     const int next = c + kWaves < C ? c + kWaves : c;  // (the last chunk's again, not used)
@@ -79,9 +68,8 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_rows(W4GemmArgs a) {
       load_x(x[(p + 1) & 1], p < 3 ? c * 4 + p + 1 : next * 4);
 #pragma unroll
       for (int i = 0; i < CG; ++i) {
-        if (p == 0) swap_halves(i);
         w4_pair<FMT, GROUP, MB>(p & 1, w[i][p >> 1], sw[i][p >> 1], x[p & 1], acc[i]);
-        if (p == 3) load_w(i, next);
+        if (p & 1) load_w(i, next, p >> 1);
       }
     }
   }
