@@ -38,13 +38,16 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_rows(W4GemmArgs a) {
 
   u32x4 w[CG][2];  // halves of a chunk
   SRaw sw[CG][2];
+  // a lane's bytes from the first tile's block, its rows being in this one or the next
+  const uint32_t in_w = 256 * g + 16 * (n16 & 7), in_s = n16 & 7;
+  const uint32_t next_w = n16 >> 3 ? C * 1024u : 0u, next_s = n16 >> 3 ? C * 16u : 0u;
   auto load_w = [&](int i, int c, int half) {
     const bool is_up = glu && i >= CG / 2;
-    const int t = min(first + (is_up ? i - CG / 2 : i) * 2 + (n16 >> 3), part_tiles - 1) + (is_up ? part_tiles : 0);
-    const int64_t block = static_cast<int64_t>(t) * C + c;
-    const int at = 8 * half + (n16 & 7);
-    w[i][half] = reinterpret_cast<const u32x4*>(a.w.codes)[block * 64 + 16 * g + at];
-    sw[i][half] = static_cast<const SRaw*>(a.w.scales)[block * 16 + at];
+    const int t = first + (is_up ? i - CG / 2 : i) * 2, last = part_tiles - 1;
+    const int64_t block = static_cast<int64_t>(min(t, last) + (is_up ? part_tiles : 0)) * C + c;
+    const bool pair = t < last;  // (past the last tile: the last again, not stored)
+    w[i][half] = *reinterpret_cast<const u32x4*>(a.w.codes + block * 1024 + 128 * half + (in_w + (pair ? next_w : 0u)));
+    sw[i][half] = (static_cast<const SRaw*>(a.w.scales) + block * 16 + 8 * half)[in_s + (pair ? next_s : 0u)];
   };
   const bf16x8* rows = static_cast<const bf16x8*>(a.ws) + lane;
   bf16x8 x[2][2][MB];  // two steps, the next two
@@ -66,6 +69,9 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_rows(W4GemmArgs a) {
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
       load_x(x[(p + 1) & 1], p < 3 ? c * 4 + p + 1 : next * 4);
+      // (else the compiler moves the loads to their use: 33 rows, 4096 x 11008 e2m1, 24.5 us for
+      // 17.4; the largest blocks have no registers for it)
+      if constexpr (MB * CG < 18) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < CG; ++i) {
         w4_pair<FMT, GROUP, MB>(p & 1, w[i][p >> 1], sw[i][p >> 1], x[p & 1], acc[i]);

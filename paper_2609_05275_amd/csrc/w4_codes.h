@@ -67,18 +67,6 @@ __device__ __forceinline__ void keep_if(bf16x8& v, bool keep) {
   v = __builtin_bit_cast(bf16x8, t);
 }
 
-// `own`, in the lanes of the banks of BANKS what `other` is 8 lanes away.
-template <int BANKS, class X>
-__device__ __forceinline__ X swap_in(X own, X other) {
-  if constexpr (sizeof(X) == 8) {
-    const uint32_t lo = swap_in<BANKS>(static_cast<uint32_t>(own), static_cast<uint32_t>(other));
-    const uint32_t hi = swap_in<BANKS>(static_cast<uint32_t>(own >> 32), static_cast<uint32_t>(other >> 32));
-    return static_cast<X>(hi) << 32 | lo;
-  } else {  // row_ror:8
-    return static_cast<X>(__builtin_amdgcn_update_dpp(static_cast<int>(own), static_cast<int>(other), 0x128, 0xf, BANKS, false));
-  }
-}
-
 // Element (m, n) from its sums (SwiGLU: of the gate and the up row).
 __device__ __forceinline__ void w4_finish(const W4GemmArgs& a, int m, int64_t n, float s0, float s1, float scale, uint16_t resid) {
   float y;
