@@ -363,7 +363,7 @@ int ld_stack_decode_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights
  *
  * ld_w4: weights [n, k] in 4 bits, groups along k.
  *   format: LD_W4_E2M1 (group 32) or LD_W4_INT4 (group 32, 64 or 128).
- *   n >= 1; k >= 8, k % 8 == 0 (the last group may be a part of one).
+ *   1 <= n <= 2^30; 8 <= k <= 2^29, k % 8 == 0 (the last group may be a part of one).
  *   codes:  device, ld_w4_code_bytes, 16-byte aligned: [ceil(n / 8)][ceil(k / 256)][64][4]
  *           dwords.  Lane 16 g + 8 h + r, dword s holds row 8 t + r at k = 256 c + 128 h +
  *           32 s + 8 g + e, e < 8: e2m1 in bits 4 e .. 4 e + 3; int4 with e < 4 in bits 8 e ..
@@ -613,9 +613,10 @@ int ld_w4_load(const ld_w4* w, void* dst, int32_t ld, void* stream);
  *          multiple of 8; C = silu(u) v (R must be NULL)
  *   act 2: squared ReLU (R must be NULL).
  * A: device bf16 [M, k], rows lda apart (a multiple of 8), 16-byte aligned, as g; C: device
- * bf16 [M, N], rows ldc apart.  C may be R.  Weights are exact, sums float32, and the
- * activation takes the sums unrounded.  ws: device scratch of ld_gemm_w4_ws_bytes(w, M, act)
- * bytes (may be 0, then ws may be NULL; enough for fewer rows), 16-byte aligned. */
+ * bf16 [M, N], rows ldc apart.  C may be R; nothing else that is written may overlap what is
+ * read.  Weights are exact, sums float32, and the activation takes the sums unrounded.  ws:
+ * device scratch of ld_gemm_w4_ws_bytes(w, M, act) bytes (0 up to 8 rows, then ws may be
+ * NULL; enough for fewer rows), 16-byte aligned. */
 size_t ld_gemm_w4_ws_bytes(const ld_w4* w, int32_t M, int32_t act);
 int ld_gemm_w4(int32_t M, const void* A, int32_t lda, const void* g, float eps, const ld_w4* w, void* C, int32_t ldc,
                float alpha, const void* R, int32_t ldr, int32_t act, void* ws, size_t ws_bytes, void* stream);
@@ -634,7 +635,8 @@ int ld_kv4_load(const ld_kv4* kv, int32_t pos, int32_t n, const int32_t* seq_len
 
 /* ld_attn_decode over a 4-bit cache; arguments as in ld_attn_decode_kv8.  Where the cache
  * has sums, every position's weights are added to them.  Scores, softmax weights and sums
- * in float32.
+ * in float32; a query is exact down to 2^-14 of the largest of 32 of its dimensions, and to
+ * 2^-22 of that below.
  *   ws: device scratch of ld_attn_decode_kv4_ws_bytes(kv, n_heads, n_new) bytes (more for a
  *   cache with sums; enough for every pos and for fewer new rows; 0 on invalid arguments),
  *   16-byte aligned. */

@@ -1564,7 +1564,8 @@ int check_w4(const ld_w4* w, W4View* out) {
   if (w->format == LD_W4_E2M1 ? w->group != 32 : w->group != 32 && w->group != 64 && w->group != 128)
     return fail(LD_E_UNSUPPORTED, "w4 group must be 32 (int4: or 64, 128)");
   if (w->n < 1 || w->k < 8 || w->k % 8) return fail(LD_E_SHAPE, "need n >= 1, k >= 8, k %% 8 == 0");
-  if (w->n > 1 << 30 || w->k > 1 << 30) return fail(LD_E_SHAPE, "n or k above 2^30");
+  // (two tiles' codes stay in 32 bits)
+  if (w->n > 1 << 30 || w->k > 1 << 29) return fail(LD_E_SHAPE, "n above 2^30 or k above 2^29");
   *out = W4View{static_cast<uint8_t*>(w->codes), w->scales, w->format, w->group, w->n, w->k};
   return LD_OK;
 }

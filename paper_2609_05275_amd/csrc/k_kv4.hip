@@ -300,7 +300,7 @@ __device__ __forceinline__ void split_query(const bf16* q, int lane, i32x4 (&to)
       uint32_t m = max(m2[0], m2[1]);
       m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16, 64)));
       // the largest to 128 .. 256 of the formats' 448
-      sb[half] = m >= 0x7f80u ? kNanScale : max(static_cast<int>(m >> 7) - 7, 16);
+      sb[half] = m >= 0x7f80u ? kNanScale : max(static_cast<int>(m >> 7) - 7, 6);
       const float s1 = __builtin_bit_cast(float, min(sb[half], 254u) << 23), s2 = s1 * 0x1p-5f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -1226,8 +1226,8 @@ static int64_t chunk_cost(int64_t heads, int64_t keys, int64_t n) {
   return div_up(wgs, kKv4AtOnce) * (turns * (2 * wgs <= kKv4AtOnce ? 6 : 10) + 10) + (n > 1 ? 6 : 0);
 }
 
-// A turn writes whole products' scores, 64 keys at most.
-int64_t attn_kv4_score_keys(int64_t keys) { return div_up(keys, 64) * 64; }
+// A wave's turn writes the scores of 32 keys.
+int64_t attn_kv4_score_keys(int64_t keys) { return div_up(keys, 32) * 32; }
 
 void plan_attn_decode_kv4(Kv4AttnArgs& a) {
   const int64_t keys = static_cast<int64_t>(a.pos) + a.n_new;

@@ -32,7 +32,8 @@ def gemm(w, M=3, A=P, lda=200, g=None, eps=1e-5, Cm=P, ldc=48, alpha=1.0, R=None
 
 BAD_DESC = [(dict(format=2), INVALID), (dict(format=-1), INVALID), (dict(group=16), UNSUPPORTED),
             (dict(group=256), UNSUPPORTED), (dict(format=0, group=64), UNSUPPORTED), (dict(n=0), SHAPE), (dict(k=0), SHAPE),
-            (dict(k=204), SHAPE), (dict(n=2 ** 30 + 1), SHAPE), (dict(k=2 ** 30 + 8), SHAPE)]
+            (dict(k=204), SHAPE), (dict(n=2 ** 30 + 1), SHAPE), (dict(k=2 ** 30 + 8), SHAPE),
+            (dict(k=2 ** 29 + 8), SHAPE)]
 
 
 @pytest.mark.parametrize("kw,code", BAD_DESC, ids=[str(k) for k, _ in BAD_DESC])

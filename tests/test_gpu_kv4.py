@@ -364,6 +364,59 @@ def test_attn_far_scales():
     check(dev, q, [keys - 1])
 
 
+def outliers(dh, size, seed):
+    """Keys that are zero in two dimensions, where the queries have `size` times what they
+    have elsewhere: what the others lose beside it is all there is."""
+    rng = np.random.default_rng(seed)
+    dev = Dev(1, 1, dh, 300)
+    x = rows(rng, 1, 300, 2, 1, dh)
+    x[:, :, 0, :, 5] = 0.0
+    x[:, :, 0, :, dh - 3] = 0.0
+    dev.ref.store(x.double().numpy(), [0])
+    dev.upload()
+    q = rng.uniform(0.5, 1.0, (1, 2, 4, dh)) * rng.choice([-1.0, 1.0], (1, 2, 4, dh))
+    q[..., 5] *= size
+    q[..., dh - 3] *= -size
+    return dev, torch.from_numpy(q).to(torch.bfloat16)
+
+
+@DHS
+@pytest.mark.parametrize("size", [1.0, 2.0 ** 6, 2.0 ** 13, 2.0 ** -120, 2.0 ** -13])
+def test_attn_query_outliers(dh, size):
+    dev, q = outliers(dh, size, 3)
+    check(dev, q, [298])
+
+
+@DHS
+@pytest.mark.parametrize("small", [2.0 ** -100, 2.0 ** -112])
+def test_attn_small_queries(dh, small):
+    """Against keys as large: products around 1."""
+    rng = np.random.default_rng(8)
+    dev = Dev(1, 2, dh, 120)
+    x = rows(rng, 1, 120, 2, 2, dh)
+    x[:, :, 0] *= 1.0 / small
+    dev.ref.store(x.double().numpy(), [0])
+    dev.upload()
+    check(dev, rows(rng, 1, 3, 4, dh) * small, [117])
+
+
+@DHS
+@pytest.mark.parametrize("size", [2.0 ** 15, 2.0 ** 16])
+def test_attn_query_outliers_beyond(dh, size):
+    """Below 2^-14 of its 32 dimensions' largest, a query's may be off by 2^-22 of that: a
+    base-2 score by 1.45 / sqrt(dh) times the sum of |k| times it, which enters twice, in a
+    weight and in the norm (4^x - 1 < 2 x for the x < 1/2 here)."""
+    dev, q = outliers(dh, size, 4)
+    got = attend(dev, q, [298])
+    values, q64 = dev.ref.read(), q.double().numpy()
+    o, a, mag = kv8.attention(values, q64, [298], 0)
+    top = np.abs(q64).reshape(*q64.shape[:-1], dh // 32, 32).max(-1).repeat(32, -1)      # [1, n, H, dh]
+    off = 1.45 / np.sqrt(dh) * 2.0 ** -22 * (top @ np.abs(values[0, 0, 0]).T).max(-1)
+    assert off.max() < 0.5
+    w = 2 * off[..., None] * a
+    assert np.max(np.abs(got - o) / (bound(o, a, mag, dh, 300) + 1.01 * (1 + 2.0 ** -8) * w)) <= 1.0
+
+
 @DHS
 def test_attn_values_that_cancel(dh):
     """Equal weights on values that sum to almost nothing: what a weight rounded to
@@ -562,3 +615,34 @@ def test_past_32_bits(n_seq, kvh, s_max):
             a = w @ np.abs(x[:j + 1, 1, h]) / (w.sum() + pos * np.exp(-m))
             # the norm sums pos equal terms in waves and chunks of them: at most 2^13 in a row
             assert np.all(np.abs(got[j, h] - want) <= 2.0 ** -8 * np.abs(want) + a * (2 * 2.0 ** 13 * 2.0 ** -24 + 1e-4) + 1e-38)
+
+
+def test_two_captured_calls_share_a_workspace():
+    """Attention with sums over two caches, in graphs over one workspace."""
+    devs = [filled(*sh, sums=True)[0] for sh in ((2, 2, 64, 700, 1), (1, 2, 128, 2500, 2))]
+    calls, graphs = [], []
+    ws = torch.empty(max(ld.ld_attn_decode_kv4_ws_bytes(d.kv, 8, 3) for d in devs), dtype=torch.uint8, device=DEV)
+    rng = np.random.default_rng(6)
+    for d, keys in zip(devs, (700, 2500)):
+        n_seq, kvh, dh = d.kv.n_seq, d.kv.n_kv_heads, d.kv.d_head
+        qkv = rows(rng, n_seq * 3, (8 + 2 * kvh) * dh).to(DEV)
+        o = torch.zeros(n_seq * 3, 8 * dh, dtype=torch.bfloat16, device=DEV)
+        call = lambda d=d, qkv=qkv, o=o, keys=keys: ld.ld_attn_decode_kv4(d.kv, 8, keys - 3, 3, qkv, o, ws)  # noqa: E731
+        call()
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call()
+        calls.append((d, qkv, o, call))
+    for i in range(3):
+        for d, qkv, _, _ in calls:
+            qkv.copy_(rows(rng, *qkv.shape))
+            d.sums.zero_()
+        for g in graphs if i % 2 else graphs[::-1]:
+            g.replay()
+        torch.cuda.synchronize()
+        got = [(o.clone(), d.sums.clone()) for d, _, o, _ in calls]
+        for (d, _, o, call), (want_o, want_s) in zip(calls, got):
+            d.sums.zero_()
+            call()
+            assert torch.equal(o, want_o) and torch.equal(d.sums, want_s)

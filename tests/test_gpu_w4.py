@@ -279,3 +279,50 @@ def test_codes_past_32_bits():
     # (more tiles may be taken by another variant: the same sums in another order)
     e = bound(f64(x), w4.values(w4.E2M1, 32, f64(w)), f64(want), "none", 1.0, None, K)[1]
     assert np.all(np.abs(f64(out[:, -16:]) - f64(want)) <= 2 * e)
+
+
+def test_many_rows_by_codes_past_32_bits():
+    """The same with rows that are laid out: tiles of the last workgroups, and the last of all
+    alone."""
+    N, K, M = 540008, 16384, 20
+    d = device(w4.E2M1, 32, N, K)
+    d.tensors[0].zero_()
+    d.tensors[1].fill_(127)
+    rng = np.random.default_rng(2)
+    w = rand(rng, 24, K)
+    small = packed(w4.E2M1, 32, w)
+    d.tensors[0][-small.tensors[0].numel():] = small.tensors[0]
+    d.tensors[1][-small.tensors[1].numel():] = small.tensors[1]
+    x = rand(rng, M, K).to(DEV)
+    out, want = torch.zeros(M, N, dtype=torch.bfloat16, device=DEV), torch.zeros(M, 24, dtype=torch.bfloat16, device=DEV)
+    ws = torch.zeros(ld.ld_gemm_w4_ws_bytes(d, M), dtype=torch.uint8, device=DEV)
+    ld.ld_gemm_w4(d, x, out, ws)
+    ld.ld_gemm_w4(small, x, want, ws)
+    assert not bool(out[:, :-24].any())
+    e = bound(f64(x), w4.values(w4.E2M1, 32, f64(w)), f64(want), "none", 1.0, None, K)[1]
+    assert np.all(np.abs(f64(out[:, -24:]) - f64(want)) <= 2 * e)
+
+
+def test_two_captured_calls_share_a_workspace():
+    """What a call lays out in its workspace is its own rows, replay after replay."""
+    rng = np.random.default_rng(4)
+    ds = [packed(w4.INT4, 64, rand(rng, 200, K, scale=0.02)) for K in (776, 2048)]
+    xs = [rand(rng, M, K).to(DEV) for M, K in ((40, 776), (20, 2048))]
+    ws = torch.zeros(max(ld.ld_gemm_w4_ws_bytes(d, 64) for d in ds), dtype=torch.uint8, device=DEV)
+    cap, out = ([torch.zeros(x.shape[0], 200, dtype=torch.bfloat16, device=DEV) for x in xs] for _ in range(2))
+    graphs = []
+    for d, x, c in zip(ds, xs, cap):
+        ld.ld_gemm_w4(d, x, c, ws)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            ld.ld_gemm_w4(d, x, c, ws)
+    for i in range(3):
+        for x in xs:
+            x.copy_(rand(rng, *x.shape))
+        for g in graphs if i % 2 else graphs[::-1]:
+            g.replay()
+        torch.cuda.synchronize()
+        for d, x, o, c in zip(ds, xs, out, cap):
+            ld.ld_gemm_w4(d, x, o, ws)
+            assert torch.equal(o, c)
