@@ -23,6 +23,7 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kKv4Waves = 8;  // of an attention workgroup
+constexpr int kKv4Turn = 32 * kKv4Waves;  // keys of a turn of an attention workgroup
 constexpr int kKv4Parts = 3;  // bf16 parts of a weight, 8 of its 24 bits each
 constexpr int kCus = 256;
 constexpr uint32_t kNanScale = 255;
@@ -248,7 +249,7 @@ __global__ __launch_bounds__(256) void ld_kv4_load_k(Kv4LoadArgs a) {
 // a.chunk_keys at least.
 __device__ __forceinline__ int kv4_chunk_keys(const Kv4AttnArgs& a, int nk) {
   if (!a.seq_pos) return a.chunk_keys;
-  const uint32_t n = a.n_chunks, even = ((static_cast<uint32_t>(nk) + n - 1) / n + 63) & ~63u;
+  const uint32_t n = a.n_chunks, even = ((static_cast<uint32_t>(nk) + n - 1) / n + kKv4Turn - 1) & ~(kKv4Turn - 1u);
   return max(static_cast<int>(even), a.chunk_keys);
 }
 
@@ -1197,9 +1198,9 @@ hipError_t combine_t(const Kv4AttnArgs& a, hipStream_t s) {
 }
 
 // Workgroups that run at once, two on each of the 256 compute units; the most that a launch
-// without row tiles makes; keys of a workgroup's turn, and the fewest of a chunk where lengths
+// without row tiles makes; and the fewest keys of a chunk where lengths
 // are the device's.
-constexpr int64_t kKv4AtOnce = 512, kKv4Wgs = 4 * kKv4AtOnce, kKv4Turn = 256, kKv4Uneven = 512;
+constexpr int64_t kKv4AtOnce = 512, kKv4Wgs = 4 * kKv4AtOnce, kKv4Uneven = 512;
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -1247,7 +1248,7 @@ void plan_attn_decode_kv4(Kv4AttnArgs& a) {
       const int64_t cost = chunk_cost(heads, keys, c);
       if (cost < best) best = cost, n = c;
     }
-    a.chunk_keys = static_cast<int32_t>(div_up(div_up(keys, n), 64) * 64);
+    a.chunk_keys = static_cast<int32_t>(div_up(div_up(keys, n), kKv4Turn) * kKv4Turn);
     a.n_chunks = static_cast<int32_t>(div_up(keys, a.chunk_keys));
   }
   a.score_keys = attn_kv4_score_keys(keys);
