@@ -17,8 +17,18 @@ __global__ __launch_bounds__(256) void ld_w4_rows_k(W4GemmArgs a, int mb_count, 
 
 // MB blocks of 16 rows against CG groups of 16 rows of W (two tiles; SwiGLU: half the groups
 // gate rows, half up rows), the workgroup's eight waves taking its chunks in turn, so that
-// the rows are read once a workgroup and used for CG products.  Lanes 8 apart swap the
-// halves of two tiles: then a product's 16 columns are 16 rows of W with the same 32 k.
+// the rows are read once a workgroup and used for CG products.  A product's 16 columns are
+// 16 rows of W with the same 32 k: lanes 0-7 of 16 read one tile, lanes 8-15 the next, the same
+// half of a chunk, whole lines of 128 bytes.  A half's registers are loaded with the next
+// chunk's as soon as it is used.
+//
+// What bounds it: with few rows the codes (16 rows, 8192 x 16384: 16.5-17.7 us, 4 TB/s);
+// with many the vector instructions that make operands of the codes and put the integers'
+// scales on the sums, 4.6 to a matrix instruction, two waves a SIMD.  48 rows of gate and up,
+// 11008 x 4096 int4 in groups of 64: 22.3 us, 3 of them the laying out (101 with the rows in
+// LDS, 23.2 with halves exchanged between lanes).  Rows read as they lie, 64 bytes a row and
+// step, took 25.7 us for 17.4 (33 rows, 4096 x 11008 e2m1): rows a power of two apart meet in
+// few of the L2's channels.
 template <int FMT, int GROUP, int MB, int CG>
 __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_rows(W4GemmArgs a) {
   typedef typename W4ScaleRaw<FMT, GROUP>::type SRaw;
@@ -119,14 +129,21 @@ hipError_t rows_launch(const W4GemmArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The fewest groups a workgroup with which one round of workgroups does.
+// Groups a workgroup: with up to 32 rows two at most, so that registers leave room for a
+// second workgroup; with more rows the fewest with which one round of workgroups does, since
+// the rows are then read for as many columns as possible.  Us of 1, 2, 4 and 6 groups, int4 in
+// groups of 64: 24 rows, 24000 x 4096 24.2, 17.8, 22.3, 18.7, 4096 x 4096 7.2, 8.8, 11.5, 14.6; 33
+// rows, 24000 x 4096 31.4, 26.1, 26.7, 21.6, 12288 x 4096 18.6, 18.6, 15.4, 19.6, 4096 x 11008
+// 17.7, 19.5, 24.4, 33.7.
 template <int FMT, int GROUP, int MB>
 hipError_t rows_mb(const W4GemmArgs& a, hipStream_t s) {
   const int groups = (a.w.N + 15) / 16;
   if (groups <= kCus && a.act != kDecActSwiglu) return rows_launch<FMT, GROUP, MB, 1>(a, s);
-  if (groups <= 2 * kCus) return rows_launch<FMT, GROUP, MB, 2>(a, s);
-  if (groups <= 4 * kCus) return rows_launch<FMT, GROUP, MB, 4>(a, s);
-  return rows_launch<FMT, GROUP, MB, 6>(a, s);
+  if constexpr (MB > 2) {
+    if (groups > 4 * kCus) return rows_launch<FMT, GROUP, MB, 6>(a, s);
+    if (groups > 2 * kCus) return rows_launch<FMT, GROUP, MB, 4>(a, s);
+  }
+  return rows_launch<FMT, GROUP, MB, 2>(a, s);
 }
 
 template <int FMT, int GROUP>
