@@ -1234,7 +1234,7 @@ int check_host_counts(const Dims& D, const LayerMasks& lm, const std::vector<int
 
 // Scratch of a decoding step.
 struct DecLayout {
-  size_t h, rstd, qkv, att, z, uv, s, part_o, part_ml, scores, row_ml, skp, skp_bytes, total;
+  size_t h, rstd, qkv, att, z, uv, s, part_o, part_ml, scores, skp, skp_bytes, total;
 };
 
 size_t skinny_part_bytes(int64_t M, int64_t N, int64_t K) {
@@ -1291,10 +1291,7 @@ DecLayout dec_layout(const Dims& D, int64_t n_new, size_t pc, int64_t score_keys
   L.s = take(es * M * D.f);
   L.part_o = take(4 * pc * D.dh);
   L.part_ml = take(4 * pc * 2);
-  if (score_keys) {
-    L.scores = take(4 * M * D.H * score_keys);
-    L.row_ml = take(8 * M * D.H);
-  }
+  if (score_keys) L.scores = take(4 * M * D.H * score_keys);
   const int64_t shapes[4][2] = {{3 * D.d, D.d}, {D.d, D.d}, {D.fw, D.d}, {D.d, D.f}};
   if (dec_split_k(M, D.d))
     for (const auto& sh : shapes) L.skp_bytes = std::max(L.skp_bytes, skinny_fused_part_bytes(M, sh[0], sh[1]));
@@ -1492,21 +1489,20 @@ size_t kv4_part_rows(const Kv4View& v, int64_t n_heads, int64_t n_new) {
 
 // Scratch of ld_attn_decode_kv4: partial rows, and for sums the scores.
 struct Kv4Scratch {
-  size_t part_ml, scores, row_ml, total;
+  size_t part_ml, scores, total;
 };
 Kv4Scratch kv4_scratch(const Kv4View& v, int64_t n_heads, int64_t n_new) {
   const size_t pc = kv4_part_rows(v, n_heads, n_new), rows = static_cast<size_t>(v.n_seq) * n_heads * n_new;
   Kv4Scratch t{};
   t.part_ml = up(4 * pc * v.dh);
   t.scores = t.part_ml + up(4 * pc * 2);
-  t.row_ml = t.scores + (v.sums ? up(4 * rows * attn_kv4_score_keys(v.s8)) : 0);
-  t.total = t.row_ml + (v.sums ? up(8 * rows) : 0);
+  t.total = t.scores + (v.sums ? up(4 * rows * attn_kv4_score_keys(v.s8)) : 0);
   return t;
 }
 
 // Attention of qkv rows b n_new + j at positions pos + j (or seq_pos[b] + j) over a 4-bit
 // cache, and its weights into the sums; part_o and part_ml hold kv4_part_rows.
-int run_kv4_attn(const Kv4View& kv, const void* qkv, void* o, float* part_o, float* part_ml, float* scores, float* row_ml,
+int run_kv4_attn(const Kv4View& kv, const void* qkv, void* o, float* part_o, float* part_ml, float* scores,
                  int32_t n_heads, int32_t alibi, int32_t n_new, int32_t pos, const int32_t* seq_pos, hipStream_t s) {
   Kv4AttnArgs a{};
   a.kv = kv;
@@ -1516,7 +1512,6 @@ int run_kv4_attn(const Kv4View& kv, const void* qkv, void* o, float* part_o, flo
   a.part_o = part_o;
   a.part_ml = part_ml;
   a.scores = kv.sums ? scores : nullptr;
-  a.row_ml = row_ml;
   a.H = n_heads;
   a.n_new = n_new;
   a.pos = pos;
@@ -1533,16 +1528,12 @@ int run_kv4_attn(const Kv4View& kv, const void* qkv, void* o, float* part_o, flo
     ps.end(known * 4.0 * rows * kv.dh * keys,
            known * (kv.n_seq * keys * kv.KV * kv.dh * 17.0 / 16 + 4.0 * rows * kv.dh + scored));
   }
-  if (a.n_chunks > 1) {
-    ProfScope pc("ld_attn_decode_kv4_combine", s);
+  if (a.n_chunks > 1 || a.scores) {
+    ProfScope pc(a.n_chunks > 1 ? "ld_attn_decode_kv4_combine" : "ld_kv4_sums_k", s);
     if ((e = launch_attn_decode_kv4_combine(a, s)) != hipSuccess)
       return fail(LD_E_HIP, "attn decode kv4 combine: %s", hipGetErrorString(e));
-    pc.end(0, known * (4.0 * rows * (kv.dh + 2) * a.n_chunks + 2.0 * rows * kv.dh));
-  }
-  if (a.scores) {
-    ProfScope pu("ld_kv4_sums_k", s);
-    if ((e = launch_kv4_sums(a, s)) != hipSuccess) return fail(LD_E_HIP, "kv4 sums: %s", hipGetErrorString(e));
-    pu.end(0, known * (scored + 8.0 * kv.n_seq * kv.KV * keys));
+    const double parts = a.n_chunks > 1 ? 4.0 * rows * (kv.dh + 2) * a.n_chunks + 2.0 * rows * kv.dh : 0.0;
+    pc.end(0, known * (parts + (a.scores ? scored + 8.0 * kv.n_seq * kv.KV * keys : 0.0)));
   }
   return LD_OK;
 }
@@ -2234,8 +2225,7 @@ int stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w, co
       const int32_t H = static_cast<int32_t>(D.H);
       if (int rc = check_kv4_layer(D, &c.kv4[l], l, &v)) return rc;
       if (int rc = run_kv4_store(v, P(L.qkv), H, n_new, pos, seq_pos, s)) return rc;
-      if (int rc = run_kv4_attn(v, P(L.qkv), P(L.att), part_o, part_ml, reinterpret_cast<float*>(base + L.scores),
-                                reinterpret_cast<float*>(base + L.row_ml), H, alibi, n_new, pos, seq_pos, s))
+      if (int rc = run_kv4_attn(v, P(L.qkv), P(L.att), part_o, part_ml, reinterpret_cast<float*>(base + L.scores), H, alibi, n_new, pos, seq_pos, s))
         return rc;
     } else {
       DecAttnArgs at{};
@@ -2816,7 +2806,7 @@ int ld_attn_decode_kv4(const ld_kv4* kv, int32_t n_heads, int32_t alibi, int32_t
   if (ws_bytes < t.total) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, t.total);
   char* base = static_cast<char*>(ws);
   auto at = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
-  return run_kv4_attn(v, qkv, o, at(0), at(t.part_ml), at(t.scores), at(t.row_ml), n_heads, alibi, n_new, pos, seq_pos,
+  return run_kv4_attn(v, qkv, o, at(0), at(t.part_ml), at(t.scores), n_heads, alibi, n_new, pos, seq_pos,
                       as_stream(stream));
 }
 

@@ -261,6 +261,17 @@ __device__ __forceinline__ int kv4_chunk_keys(const Kv4AttnArgs& a, int nk) {
   return max(static_cast<int>(even), a.chunk_keys);
 }
 
+// Keys of a sequence (0: left out), and the chunks they fill.
+__device__ __forceinline__ int kv4_keys(const Kv4AttnArgs& a, int64_t b) {
+  if (!a.seq_pos) return a.pos + a.n_new;
+  const int p = a.seq_pos[b];
+  return p < 0 || p > a.pos ? 0 : p + a.n_new;
+}
+__device__ __forceinline__ int kv4_chunks(const Kv4AttnArgs& a, int nk) {
+  const int ck = kv4_chunk_keys(a, nk);
+  return (nk + ck - 1) / ck;
+}
+
 // A weight's bf16 parts, TT / 2 operands of 8 positions each.
 template <int TT>
 struct Kv4Parts {
@@ -386,12 +397,7 @@ __global__ __launch_bounds__(64 * kKv4Waves, 4) void ld_attn_decode_kv4_k(Kv4Att
   }
   chunk = (chunk + h + b) % a.n_chunks;
   const int G = a.group, R = G * a.n_new;
-  int p = a.pos;
-  if (a.seq_pos) {
-    p = a.seq_pos[b];
-    if (p < 0 || p > a.pos) p = -a.n_new;  // left out: no keys
-  }
-  const int nk = p + a.n_new, ck = kv4_chunk_keys(a, nk), k_first = chunk * ck;
+  const int nk = kv4_keys(a, b), p = nk - a.n_new, ck = kv4_chunk_keys(a, nk), k_first = chunk * ck;
   const int rows = min(R - r0, 16);
   const int64_t d = static_cast<int64_t>(a.H) * DH;
   // where row r of the head goes in the output
@@ -680,19 +686,14 @@ __global__ __launch_bounds__(64 * kKv4Waves, 4) void ld_attn_decode_kv4_k(Kv4Att
       L = __builtin_fmaf(wgt, ml[w][i][1], L);
       s = __builtin_fmaf(wgt, red[w][i][col], s);
     }
-    if (only) {
+    const int64_t pr = (head * R + r) * a.n_chunks + chunk;
+    if (only)
       out_at(r)[col] = static_cast<bf16>(s * (1.f / L));
-      if (a.scores && col == 0) {
-        a.row_ml[(head * R + r) * 2] = M;
-        a.row_ml[(head * R + r) * 2 + 1] = 1.f / L;
-      }
-    } else {
-      const int64_t pr = (head * R + r) * a.n_chunks + chunk;
+    else
       a.part_o[pr * DH + col] = s;
-      if (col == 0) {
-        a.part_ml[pr * 2] = M;
-        a.part_ml[pr * 2 + 1] = L;
-      }
+    if (col == 0 && (!only || a.scores)) {
+      a.part_ml[pr * 2] = M;
+      a.part_ml[pr * 2 + 1] = L;
     }
   }
 }
@@ -702,22 +703,18 @@ __global__ __launch_bounds__(64 * kKv4Waves, 4) void ld_attn_decode_kv4_k(Kv4Att
 // rows are all in flight; then the waves' sums, in their order.  A launch that waits: 2 to 3
 // us of a call, whatever the case.
 template <int DH, int W>
-__global__ __launch_bounds__(256) void ld_attn_decode_kv4_combine(Kv4AttnArgs a) {
+__device__ __forceinline__ void combine_rows(const Kv4AttnArgs& a, uint32_t block) {
   constexpr int CL = DH / 64, U = 4;
   typedef float FRow __attribute__((ext_vector_type(CL)));
   __shared__ float ml[W][2];
   __shared__ __align__(16) FRow red[W][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t id = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x, HN = a.H * a.n_new;
+  const uint32_t id = W == 1 ? block * 4 + wave : block, HN = a.H * a.n_new;
   if (id >= a.kv.n_seq * HN) return;
   const int w = W == 1 ? 0 : wave;
   const int64_t r = id, b = id / HN;
   const uint32_t h = id % HN / a.n_new, j = id % a.n_new;  // (HN is a multiple of n_new)
-  int chunks = a.n_chunks;
-  if (a.seq_pos) {
-    const int p = a.seq_pos[b], nk = p < 0 || p > a.pos ? 0 : p + a.n_new, ck = kv4_chunk_keys(a, nk);
-    chunks = (nk + ck - 1) / ck;
-  }
+  const int chunks = kv4_chunks(a, kv4_keys(a, b));
   if (chunks <= 1) return;  // written by the attention kernel
   const float* po = a.part_o + r * a.n_chunks * DH + lane * CL;
   const floatx2* pm = reinterpret_cast<const floatx2*>(a.part_ml) + r * a.n_chunks;
@@ -769,41 +766,82 @@ __global__ __launch_bounds__(256) void ld_attn_decode_kv4_combine(Kv4AttnArgs a)
       L = __builtin_fmaf(wgt, ml[u][1], L);
       acc += wgt * red[u][lane];
     }
-    M = m;
   }
   acc *= 1.f / L;
-  if (a.scores && lane == 0) {
-    a.row_ml[r * 2] = M;
-    a.row_ml[r * 2 + 1] = 1.f / L;
-  }
   bf16* out = static_cast<bf16*>(a.out) + (b * a.n_new + j) * (static_cast<int64_t>(a.H) * DH) +
               static_cast<int64_t>(h) * DH + lane * CL;
 #pragma unroll
   for (int cc = 0; cc < CL; ++cc) out[cc] = static_cast<bf16>(acc[cc]);
 }
 
-// sums += the weights of a head's rows, a thread a position, rows in their order: the weights
-// need the rows' norms, which are known when all chunks are done, so the scores go through
-// memory.  6 rows of 8 sequences' 16 heads at 1506 keys: 4.6 MB each way, 4.8 us traced.
-__global__ __launch_bounds__(256) void ld_kv4_sums_k(Kv4AttnArgs a) {
-  const int b = blockIdx.z, h = blockIdx.y, t = blockIdx.x * 256 + threadIdx.x, R = a.group * a.n_new;
-  int p = a.pos;
-  if (a.seq_pos) {
-    p = a.seq_pos[b];
-    if (p < 0 || p > a.pos) return;
+// sums += the weights of a head's rows, a thread four positions, rows in their order: the
+// weights need the rows' norms, which are known when all chunks are done, so the scores go
+// through memory.  The norms of 256 rows at a time are found first, a row by 16 lanes.
+constexpr int kSumKeys = 1024;  // of a workgroup
+__device__ __forceinline__ void add_sums(const Kv4AttnArgs& a, uint32_t block) {
+  __shared__ float norm[256][2];
+  const uint32_t tiles = (static_cast<uint32_t>(a.pos) + a.n_new + kSumKeys - 1) / kSumKeys;
+  const int64_t head = block / tiles;
+  if (head >= static_cast<int64_t>(a.kv.n_seq) * a.kv.KV) return;
+  const int tid = threadIdx.x, b = static_cast<int>(head / a.kv.KV), R = a.group * a.n_new;
+  const int nk = kv4_keys(a, b), p = nk - a.n_new, t0 = block % tiles * kSumKeys, t = t0 + 4 * tid, chunks = kv4_chunks(a, nk);
+  if (t0 >= nk) return;
+  const float* sc = a.scores + head * R * a.score_keys + (t < nk ? t : 0);
+  floatx4 s = 0.f, next = *reinterpret_cast<const floatx4*>(sc);
+  for (int r0 = 0; r0 < R; r0 += 256) {
+    const int rows = min(R - r0, 256);
+    if (r0) __syncthreads();
+    for (int i = tid >> 4; i < rows; i += 16) {
+      const floatx2* ml = reinterpret_cast<const floatx2*>(a.part_ml) + (head * R + r0 + i) * a.n_chunks;
+      float M = -INFINITY, L = 0.f;
+      for (int c = tid & 15; c < chunks; c += 16) {
+        const floatx2 x = ml[c];
+        const float m = fmaxf(M, x[0]);
+        // (a part whose every score was NaN has no maximum, but a NaN sum)
+        L = L * (M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - m)) +
+            x[1] * (x[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[0] - m));
+        M = m;
+      }
+      float m = M;
+#pragma unroll
+      for (int d = 1; d < 16; d *= 2) m = fmaxf(m, __shfl_xor(m, d, 64));
+      L *= M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - m);
+#pragma unroll
+      for (int d = 1; d < 16; d *= 2) L += __shfl_xor(L, d, 64);
+      if ((tid & 15) == 0) {
+        norm[i][0] = m;
+        norm[i][1] = 1.f / L;
+      }
+    }
+    __syncthreads();
+    for (int i = 0; i < rows; ++i) {
+      const int r = r0 + i, last = p + r % a.n_new;
+      const floatx4 x = next;
+      next = *reinterpret_cast<const floatx4*>(sc + min(r + 1, R - 1) * a.score_keys);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)  // (a masked position counts nothing, whatever the row holds)
+        s[u] += t + u > last ? 0.f : __builtin_amdgcn_exp2f(x[u] - norm[i][0]) * norm[i][1];
+    }
   }
-  if (t >= p + a.n_new) return;
-  const int64_t head = static_cast<int64_t>(b) * a.kv.KV + h;
-  const float* sc = a.scores + head * R * a.score_keys + t;
-  const float* rm = a.row_ml + head * R * 2;
-  float s = 0.f;
-  for (int r = 0; r < R; ++r) {
-    const float x = sc[r * a.score_keys];
-    // (a masked position counts nothing, whatever the row holds)
-    s += t > p + r % a.n_new ? 0.f : __builtin_amdgcn_exp2f(x - rm[2 * r]) * rm[2 * r + 1];
-  }
-  a.kv.sums[head * a.kv.s_max + t] += s;
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+    if (t + u < nk) a.kv.sums[head * a.kv.s_max + t + u] += s[u];
 }
+
+// Joins chunks, in the first `blocks` workgroups, and adds to the sums in those behind: one
+// launch for both (two: 2 us more).
+template <int DH, int W>
+__global__ __launch_bounds__(256) void ld_attn_decode_kv4_combine(Kv4AttnArgs a, uint32_t blocks) {
+  const uint32_t id = kv4_workgroup();
+  if (id < blocks)
+    combine_rows<DH, W>(a, id);
+  else
+    add_sums(a, id - blocks);
+}
+
+// Over one chunk: its rows are the result.  6 rows of 8 sequences' 16 heads at 1506 keys: 4.6
+// MB of scores, 4.8 us traced.
+__global__ __launch_bounds__(256) void ld_kv4_sums_k(Kv4AttnArgs a) { add_sums(a, kv4_workgroup()); }
 
 // ---------------------------------------------------------------- eviction
 
@@ -1161,6 +1199,8 @@ __global__ __launch_bounds__(256) void ld_kv4_gather_k(Kv4EvictArgs a) {
   if (sum) a.to.sums[head * a.to.s_max + t0 + lane] = w;
 }
 
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 // Workgroups in two dimensions: one takes 2^32 threads at most.
 dim3 kv4_grid(int64_t wgs) {
   constexpr int64_t kX = 1 << 20;
@@ -1206,10 +1246,15 @@ hipError_t attn_t(const Kv4AttnArgs& a, hipStream_t s) {
 template <int DH>
 hipError_t combine_t(const Kv4AttnArgs& a, hipStream_t s) {
   const int64_t rows = static_cast<int64_t>(a.kv.n_seq) * a.H * a.n_new;
-  if (a.n_chunks > 4 && rows <= 2048)
-    hipLaunchKernelGGL((ld_attn_decode_kv4_combine<DH, 4>), dim3(rows), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((ld_attn_decode_kv4_combine<DH, 1>), dim3((rows + 3) / 4), dim3(256), 0, s, a);
+  const int64_t sums = a.scores ? div_up(static_cast<int64_t>(a.pos) + a.n_new, kSumKeys) * a.kv.KV * a.kv.n_seq : 0;
+  if (a.n_chunks <= 1) {
+    hipLaunchKernelGGL(ld_kv4_sums_k, kv4_grid(sums), dim3(256), 0, s, a);
+  } else if (a.n_chunks > 4 && rows <= 2048) {
+    hipLaunchKernelGGL((ld_attn_decode_kv4_combine<DH, 4>), kv4_grid(rows + sums), dim3(256), 0, s, a, static_cast<uint32_t>(rows));
+  } else {
+    const int64_t blocks = div_up(rows, 4);
+    hipLaunchKernelGGL((ld_attn_decode_kv4_combine<DH, 1>), kv4_grid(blocks + sums), dim3(256), 0, s, a, static_cast<uint32_t>(blocks));
+  }
   return hipGetLastError();
 }
 
@@ -1217,8 +1262,6 @@ hipError_t combine_t(const Kv4AttnArgs& a, hipStream_t s) {
 // without row tiles makes; and the fewest keys of a chunk where lengths
 // are the device's.
 constexpr int64_t kKv4AtOnce = 512, kKv4Wgs = 4 * kKv4AtOnce, kKv4Uneven = 512;
-
-int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace
 
@@ -1276,12 +1319,6 @@ hipError_t launch_attn_decode_kv4(const Kv4AttnArgs& a, hipStream_t s) {
 
 hipError_t launch_attn_decode_kv4_combine(const Kv4AttnArgs& a, hipStream_t s) {
   return a.kv.dh == 128 ? combine_t<128>(a, s) : combine_t<64>(a, s);
-}
-
-hipError_t launch_kv4_sums(const Kv4AttnArgs& a, hipStream_t s) {
-  const int64_t keys = static_cast<int64_t>(a.pos) + a.n_new;
-  hipLaunchKernelGGL(ld_kv4_sums_k, dim3(div_up(keys, 256), a.kv.KV, a.kv.n_seq), dim3(256), 0, s, a);
-  return hipGetLastError();
 }
 
 namespace {

@@ -49,7 +49,6 @@ struct Kv4AttnArgs {
   float* part_o;   // [n_seq][H * n_new rows of the heads in turn][n_chunks][dh]
   float* part_ml;  // [n_seq][H * n_new][n_chunks][2]: base-2 max, sum
   float* scores;   // null, or [n_seq][H * n_new][score_keys]: base-2 scores, for the sums
-  float* row_ml;   // with them, [n_seq][H * n_new][2]: a row's max, 1 / sum
   int64_t score_keys;
   int32_t H, n_new, pos, group, n_chunks, chunk_keys;  // group = H / KV; chunk_keys: the least
   uint32_t tiles;  // of 16 rows a key/value head
@@ -75,12 +74,11 @@ hipError_t launch_kv4_load(const Kv4LoadArgs& a, hipStream_t s);
 int64_t attn_kv4_heads(const Kv4View& kv, int64_t H, int64_t n_new);
 int64_t attn_kv4_max_chunks(int64_t heads, int64_t keys);
 int64_t attn_kv4_score_keys(int64_t keys);
-// Fills in group, tiles and the chunks; the second launch is for several chunks, the
-// third adds the weights to kv.sums.
+// Fills in group, tiles and the chunks; the second launch, for several chunks or with scores,
+// joins the chunks and adds the weights to kv.sums.
 void plan_attn_decode_kv4(Kv4AttnArgs& a);
 hipError_t launch_attn_decode_kv4(const Kv4AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_decode_kv4_combine(const Kv4AttnArgs& a, hipStream_t s);
-hipError_t launch_kv4_sums(const Kv4AttnArgs& a, hipStream_t s);
 size_t kv4_evict_ws_bytes(const Kv4View& from, int64_t len);
 hipError_t launch_kv4_select(const Kv4EvictArgs& a, hipStream_t s);
 hipError_t launch_kv4_gather(const Kv4EvictArgs& a, hipStream_t s);
