@@ -1259,9 +1259,12 @@ hipError_t combine_t(const Kv4AttnArgs& a, hipStream_t s) {
 }
 
 // Workgroups that run at once, two on each of the 256 compute units; the most that a launch
-// without row tiles makes; and the fewest keys of a chunk where lengths
-// are the device's.
-constexpr int64_t kKv4AtOnce = 512, kKv4Wgs = 4 * kKv4AtOnce, kKv4Uneven = 512;
+// without row tiles makes; and the fewest keys of a chunk where lengths are the device's.
+// There a sequence is cut into as many chunks as the most allows, so that long ones leave no
+// tail.  Us for two, three, four and six rounds, up to 8192 keys of 16 sequences of 32 heads 41,
+// 42, 43, 44; 32768 of 8 of 8 42, 41, 47, 49; 4096 of 64 of 8 39, 38, 38, 43; 100000 of 16 of 8 207, 188,
+// 180, 177; 2056 of 32 of 16 22, 23, 25, 26.
+constexpr int64_t kKv4AtOnce = 512, kKv4Wgs = 3 * kKv4AtOnce, kKv4Uneven = 512;
 
 }  // namespace
 
