@@ -101,10 +101,10 @@ __device__ __forceinline__ uint32_t gather4(uint32_t x) {
 // are new; a token appended writes its bytes one by one.
 //
 // Bound by memory, in small calls by the launch: 1501 rows each of 3 sequences, 8 heads of 128,
-// store 6.3 us traced (23 MB, 3.7 TB/s), load 7.1; a row each of 32 sequences of 16 heads 2.8
-// and 5.1 traced, 6.7 together in a graph.  What the load writes goes past the caches (both
-// calls 13.2 -> 12.9 us, 16384 of 131072 positions that stayed 15.4 -> 13); rows loaded past
-// them by the store cost 0.7.
+// store 6.5 us traced (23 MB, 3.6 TB/s), both 11.7; a row each of 32 sequences of 16 heads 6.4
+// together.  What the load writes goes past the caches, in whole lines (both calls 11.7 us, in
+// half lines 12.9, through the caches 13.2; 131072 positions of 8 heads cut to 16384 and read
+// 56.5, 64.2, 66.7); rows loaded past them by the store cost 0.7.
 template <int DH>
 struct Kv4Lanes {
   static constexpr int PT = DH / 16, U = 64 / PT, TILES = U / 8, TB = DH * 4;  // TB: bytes of a tile of 8 values
@@ -243,12 +243,17 @@ __global__ __launch_bounds__(256) void ld_kv4_load_k(Kv4LoadArgs a) {
     q1 = half ? hn : got;
   }
   if (!in) return;
-  const float s = __builtin_bit_cast(float, sb << 23);
   const int64_t ld = 2ll * c.KV * DH;
   bf16* out = static_cast<bf16*>(a.out) + (static_cast<int64_t>(w.b) * a.n + t - a.pos) * ld +
-              (static_cast<int64_t>(w.part) * c.KV + w.h) * DH + 16 * c16;
-  __builtin_nontemporal_store(codes_to_bf16(q0, s), reinterpret_cast<bf16x8*>(out));
-  __builtin_nontemporal_store(codes_to_bf16(q1, s), reinterpret_cast<bf16x8*>(out + 8));
+              (static_cast<int64_t>(w.part) * c.KV + w.h) * DH + 8 * c16;
+  // a row's lanes write its first half, then its second: whole lines
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int from = lane - c16 + i * (PT / 2) + (c16 >> 1);
+    const uint32_t e0 = __shfl(static_cast<int>(q0), from, 64), e1 = __shfl(static_cast<int>(q1), from, 64);
+    const float s = __builtin_bit_cast(float, static_cast<uint32_t>(__shfl(static_cast<int>(sb), from, 64)) << 23);
+    __builtin_nontemporal_store(codes_to_bf16(c16 & 1 ? e1 : e0, s), reinterpret_cast<bf16x8*>(out + 8 * i * PT));
+  }
 }
 
 // --------------------------------------------------------------- attention
@@ -981,7 +986,7 @@ __device__ __forceinline__ uint32_t rank_above(uint32_t u, int pass) { return pa
 
 // Up to kSelMost positions: a workgroup takes a head and holds their ranks; the rank of the
 // last one that stays by three passes over counts of a digit.  Bound by the passes' barriers:
-// 9.2 us traced for 128 heads of 2048 positions (62 us with one thread looking through the
+// 8.9 us traced for 128 heads of 2048 positions (62 us with one thread looking through the
 // counts).
 __global__ __launch_bounds__(kSelThreads) void ld_kv4_select_k(Kv4EvictArgs a) {
   __shared__ uint32_t counts[kDigits];
@@ -1142,7 +1147,7 @@ __global__ __launch_bounds__(kSelThreads) void ld_kv4_select_pass_k(Kv4EvictArgs
 // A wave takes a tile of 8 places of the smaller cache: their keys, values, scales
 // and sums.  A position's values lie in 8 (4) lines of its tile, so that the values of a
 // cache are read as a whole where few positions stay: 16384 of 131072 positions of 8 heads of
-// 128 read 73 MB for 9, 24 us; 512 of 2048 of 128 heads 7.8.
+// 128 read 73 MB, 17 us traced (4.3 TB/s with 18 MB written); 512 of 2048 of 128 heads 7.5.
 template <int DH>
 __global__ __launch_bounds__(256) void ld_kv4_gather_k(Kv4EvictArgs a) {
   constexpr int JN = DH / 32, TB = DH * 4;

@@ -328,6 +328,15 @@ def test_attn_many_rows_in_chunks(dh):
     check(dev, rows(rng, 11, 8, 48, dh), pos, seq_pos=True)
 
 
+@pytest.mark.parametrize("keys,group,n,dh", [(9000, 40, 8, 64), (700, 33, 8, 128), (300, 300, 1, 64), (30000, 1, 1, 128)])
+@pytest.mark.parametrize("seq_pos", [False, True], ids=["known", "device"])
+def test_attn_sums_of_many_rows_and_chunks(keys, group, n, dh, seq_pos):
+    """More rows of a head than their norms are found for at a time, more chunks than lanes
+    look at at once."""
+    dev, rng = filled(2, 1, dh, keys, group, sums=True)
+    check(dev, rows(rng, 2, n, group, dh), [keys - n, None if seq_pos else keys - n], seq_pos=seq_pos)
+
+
 @pytest.mark.parametrize("n_seq,kvh,keys", [(8, 4, 3000), (16, 8, 1100)])
 def test_attn_uneven_in_a_full_grid(n_seq, kvh, keys):
     dev, rng = filled(n_seq, kvh, 64, keys, kvh)
