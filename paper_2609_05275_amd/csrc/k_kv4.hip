@@ -372,7 +372,7 @@ __device__ __forceinline__ void split_query(const bf16* q, int lane, i32x4 (&to)
 // What bounds it: the issue of vector instructions, about 210 a turn of a wave.  So the
 // registers are kept to four waves of a SIMD (more loads in flight with two were slower),
 // the maximum is renewed only where it has to be, and NaN is looked for only in turns that
-// masks cut.  2 sequences of 131072 keys, 32 heads over 8 of 128 dimensions: 59 us, 4.8
+// masks cut.  2 sequences of 131072 keys, 32 heads over 8 of 128 dimensions: 60 us, 4.8
 // TB/s of the cache (75 with the scores in bf16 and the sums rescaled each turn).  16 uneven
 // sequences of 32 heads, 68000 keys in all: 43 us (48).
 template <int DH, int NQ>
@@ -844,8 +844,8 @@ __global__ __launch_bounds__(256) void ld_attn_decode_kv4_combine(Kv4AttnArgs a,
     add_sums(a, id - blocks);
 }
 
-// Over one chunk: its rows are the result.  6 rows of 8 sequences' 16 heads at 1506 keys: 4.6
-// MB of scores, 4.8 us traced.
+// Over one chunk: its rows are the result.  (6 rows of 8 sequences' 16 heads at 1506 keys, with
+// the joining of two chunks: 4.6 MB of scores, 5.6 us traced.)
 __global__ __launch_bounds__(256) void ld_kv4_sums_k(Kv4AttnArgs a) { add_sums(a, kv4_workgroup()); }
 
 // ---------------------------------------------------------------- eviction
@@ -1034,7 +1034,7 @@ __global__ __launch_bounds__(kSelThreads) void ld_kv4_select_k(Kv4EvictArgs a) {
 // More positions: workgroups of kPiece of them, a launch for each digit, whose counts meet
 // in memory.  Scratch of a head: the three digits' counts; after each, the prefix so far and
 // how many are left at it; each piece's numbers above the last one that stays and equal to it.
-// Six launches of 4 to 7 us traced, 29 in all for 8 heads of 131072 positions (one workgroup
+// Six launches of 4 to 6 us traced, 30 in all for 8 heads of 131072 positions (one workgroup
 // a head took 320).
 constexpr int kPiece = 4096, kPieceEach = kPiece / kSelThreads;
 constexpr int kFound = kDigits, kPieces = kDigits + 8;
