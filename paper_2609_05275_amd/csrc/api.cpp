@@ -2740,6 +2740,7 @@ int ld_gemm_w4(int32_t M, const void* A, int32_t lda, const void* g, float eps, 
   const size_t need = w4_gemm_ws_bytes(M, v.K);
   if (need && (!ws || ws_bytes < need)) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
   if (need && (reinterpret_cast<uintptr_t>(ws) & 15)) return fail(LD_E_INVALID, "ws must be 16-byte aligned");
+  if (A == C) return fail(LD_E_INVALID, "C must not be A");
   return run_gemm_w4(v, A, lda, g, eps, C, ldc, R, ldr, M, N, alpha, act, ws, as_stream(stream));
 }
 

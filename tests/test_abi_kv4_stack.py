@@ -75,7 +75,8 @@ def test_null_buffers():
 @pytest.mark.parametrize("kw,code", [(dict(n=0), INVALID), (dict(n=9), INVALID), (dict(pos=-1), SHAPE),
                                      (dict(pos=100), SHAPE), (dict(pos=2 ** 31 - 1), SHAPE), (dict(x=None), INVALID),
                                      (dict(seq_pos=Raw(P + 2)), INVALID), (dict(ws=Raw(P, 1000)), WORKSPACE),
-                                     (dict(ws=None), INVALID)], ids=str)
+                                     (dict(ws=None), INVALID)],
+                         ids=["no rows", "nine rows", "pos", "pos at the end", "pos beyond 32 bits", "no x", "seq_pos", "little ws", "no ws"])
 def test_decode_arguments(kw, code):
     for call in (decode, decode_w4):
         with pytest.raises(ld.LdError) as e:

@@ -58,7 +58,7 @@ BAD_CALLS = [
     (gemm, dict(lda=192), SHAPE), (gemm, dict(lda=204), SHAPE), (gemm, dict(ldc=47), SHAPE), (gemm, dict(R=P, ldr=47), SHAPE),
     (gemm, dict(A=None), INVALID), (gemm, dict(Cm=None), INVALID), (gemm, dict(A=P + 2), INVALID), (gemm, dict(g=P + 2), INVALID),
     (gemm, dict(Cm=P + 1), INVALID), (gemm, dict(R=P + 1), INVALID), (gemm, dict(alpha=float("nan")), INVALID),
-    (gemm, dict(g=P, eps=0.0), INVALID),
+    (gemm, dict(g=P, eps=0.0), INVALID), (gemm, dict(A=P, Cm=P), INVALID),
 ]
 
 
