@@ -104,7 +104,8 @@ __device__ __forceinline__ uint32_t gather4(uint32_t x) {
 // store 6.5 us traced (23 MB, 3.6 TB/s), both 11.7; a row each of 32 sequences of 16 heads 6.4
 // together.  What the load writes goes past the caches, in whole lines (both calls 11.7 us, in
 // half lines 12.9, through the caches 13.2; 131072 positions of 8 heads cut to 16384 and read
-// 56.5, 64.2, 66.7); rows loaded past them by the store cost 0.7.
+// 56.5, 64.2, 66.7); rows loaded past them by the store cost 0.7 (in whole
+// lines, lanes holding dimensions DH / 2 apart, 11.6, but the appended rows 6.7).
 template <int DH>
 struct Kv4Lanes {
   static constexpr int PT = DH / 16, U = 64 / PT, TILES = U / 8, TB = DH * 4;  // TB: bytes of a tile of 8 values
