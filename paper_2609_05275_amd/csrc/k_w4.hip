@@ -475,7 +475,7 @@ bool w4_gemm_fuses_norm(int64_t M, int64_t K) { return M <= kW4FewRows && K <= 8
 
 hipError_t launch_gemm_w4(const W4GemmArgs& a, hipStream_t s) {
   // From 9 rows on reading them costs as much as the codes where they are long, and laid
-  // out in memory once they are used for more columns.  Us of 16 rows, held and laid out: 4096
+  // out in memory once (or not, if short) they are used for more columns.  Us of 16 rows, held and laid out: 4096
   // x 11008 22.2, 10.2; 2048 x 5504 9.9, 6.6; 16384 x 8192 25.2, 21.3; 22016 x 4096 18.0, 15.4;
   // 12288 x 4096 12.0, 12.3; 6144 x 2048 4.8, 6.3.  Of 8: 4096 x 11008 12.8, 10.1, 8192 x 5504 10.7,
   // 11.2, 2048 x 16384 10.0, 11.8.

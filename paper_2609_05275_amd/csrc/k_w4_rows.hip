@@ -27,9 +27,10 @@ __global__ __launch_bounds__(256) void ld_w4_rows_k(W4GemmArgs a, int mb_count, 
 // scales on the sums, 4.6 to a matrix instruction, two waves a SIMD.  48 rows of gate and up,
 // 11008 x 4096 int4 in groups of 64: 22.3 us, 3 of them the laying out (101 with the rows in
 // LDS, 23.2 with halves exchanged between lanes).  Rows read as they lie, 64 bytes a row and
-// step, took 25.7 us for 17.4 (33 rows, 4096 x 11008 e2m1): rows a power of two apart meet in
+// step, took 25.7 us for 17.4 (33 rows, 4096 x 11008 e2m1): rows far apart meet in
 // few of the L2's channels.
-template <int FMT, int GROUP, int MB, int CG>
+// LAID: the rows are ld_w4_rows_k's, else A's.
+template <int FMT, int GROUP, int MB, int CG, bool LAID>
 __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_rows(W4GemmArgs a) {
   typedef typename W4ScaleRaw<FMT, GROUP>::type SRaw;
   constexpr int kWave = CG * MB * 256;  // sums of a wave
@@ -59,13 +60,26 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_rows(W4GemmArgs a) {
     w[i][half] = *reinterpret_cast<const u32x4*>(a.w.codes + block * 1024 + 128 * half + (in_w + (pair ? next_w : 0u)));
     sw[i][half] = (static_cast<const SRaw*>(a.w.scales) + block * 16 + 8 * half)[in_s + (pair ? next_s : 0u)];
   };
-  const bf16x8* rows = static_cast<const bf16x8*>(a.ws) + lane;
+  const bf16x8* laid = static_cast<const bf16x8*>(a.ws) + lane;
+  const bf16* rows[MB];  // (past the last row: the last again, not stored)
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+    rows[mb] = static_cast<const bf16*>(a.A) + static_cast<int64_t>(min(16 * mb + n16, M - 1)) * a.lda + 8 * g;
   bf16x8 x[2][2][MB];  // two steps, the next two
   auto load_x = [&](bf16x8 (&to)[2][MB], int pair) {  // pair of steps, four a chunk
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int mb = 0; mb < MB; ++mb) to[s][mb] = rows[(static_cast<int64_t>(pair * 2 + s) * MB + mb) * 64];
+      for (int mb = 0; mb < MB; ++mb) {
+        if constexpr (LAID) {
+          to[s][mb] = laid[(static_cast<int64_t>(pair * 2 + s) * MB + mb) * 64];
+        } else {
+          const int k = pair * 64 + 32 * s;
+          const bool in = k + 8 * g < a.w.K;
+          to[s][mb] = load8(rows[mb] + (in ? k : -8 * g));
+          keep_if(to[s][mb], in);
+        }
+      }
   };
   if (wave < C) {
     load_x(x[0], wave * 4);
@@ -122,12 +136,18 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_rows(W4GemmArgs a) {
   }
 }
 
-template <int FMT, int GROUP, int MB, int CG>
+template <int FMT, int GROUP, int MB, int CG, bool LAID = true>
 hipError_t rows_launch(const W4GemmArgs& a, hipStream_t s) {
   const int cols = (a.act == kDecActSwiglu ? CG / 2 : CG) * 16;
-  hipLaunchKernelGGL((ld_gemm_w4_rows<FMT, GROUP, MB, CG>), dim3((a.N + cols - 1) / cols), dim3(64 * kWaves), 0, s, a);
+  hipLaunchKernelGGL((ld_gemm_w4_rows<FMT, GROUP, MB, CG, LAID>), dim3((a.N + cols - 1) / cols), dim3(64 * kWaves), 0, s, a);
   return hipGetLastError();
 }
+
+// Short rows are read where they lie, which saves a launch.  Us laid out and not, 2304 columns:
+// 24 rows of 512 4.8, 4.0, of 1024 5.0, 4.5, of 2048 5.9, 6.3; 40 of 768 5.5, 5.0, of 1024 5.6, 5.7; 64 of
+// 512 5.7, 5.7, of 768 5.8, 6.4; 16 of 2048, 24000 columns, 10.8, 11.8; from Python two launches
+// cost 3 more.
+bool w4_rows_laid(int64_t M, int64_t K) { return (M <= 32 ? 2 : (M + 15) / 16) * K > 2560; }
 
 // Groups a workgroup: with up to 32 rows two at most, so that registers leave room for a
 // second workgroup; with more rows the fewest with which one round of workgroups does, since
@@ -138,6 +158,10 @@ hipError_t rows_launch(const W4GemmArgs& a, hipStream_t s) {
 template <int FMT, int GROUP, int MB>
 hipError_t rows_mb(const W4GemmArgs& a, hipStream_t s) {
   const int groups = (a.w.N + 15) / 16;
+  if (!w4_rows_laid(a.M, a.w.K)) {
+    if (groups <= kCus && a.act != kDecActSwiglu) return rows_launch<FMT, GROUP, MB, 1, false>(a, s);
+    return rows_launch<FMT, GROUP, MB, 2, false>(a, s);
+  }
   if (groups <= kCus && a.act != kDecActSwiglu) return rows_launch<FMT, GROUP, MB, 1>(a, s);
   if constexpr (MB > 2) {
     if (groups > 4 * kCus) return rows_launch<FMT, GROUP, MB, 6>(a, s);
@@ -154,16 +178,18 @@ hipError_t rows_t(const W4GemmArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t w4_gemm_ws_bytes(int64_t M, int64_t K) {
-  if (M <= 8) return 0;
+  if (M <= 8 || !w4_rows_laid(M, K)) return 0;
   return static_cast<size_t>((M + 15) / 16 * 16) * ((K + kW4Chunk - 1) / kW4Chunk * kW4Chunk) * 2;
 }
 
 hipError_t launch_gemm_w4_rows(const W4GemmArgs& a, hipStream_t s) {
-  if (a.M < 1 || a.M > kW4MaxM || a.g || !a.ws) return hipErrorInvalidValue;
-  const int mb = (a.M + 15) / 16, blocks = (a.w.K + kW4Chunk - 1) / kW4Chunk * 8 * mb;
-  hipLaunchKernelGGL(ld_w4_rows_k, dim3((blocks + 3) / 4), dim3(256), 0, s, a, mb, blocks);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (a.M < 1 || a.M > kW4MaxM || a.g || (w4_rows_laid(a.M, a.w.K) && !a.ws)) return hipErrorInvalidValue;
+  if (w4_rows_laid(a.M, a.w.K)) {
+    const int mb = (a.M + 15) / 16, blocks = (a.w.K + kW4Chunk - 1) / kW4Chunk * 8 * mb;
+    hipLaunchKernelGGL(ld_w4_rows_k, dim3((blocks + 3) / 4), dim3(256), 0, s, a, mb, blocks);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   if (a.w.format == LD_W4_E2M1) return rows_t<LD_W4_E2M1, 32>(a, s);
   return a.w.group == 32 ? rows_t<LD_W4_INT4, 32>(a, s) : a.w.group == 64 ? rows_t<LD_W4_INT4, 64>(a, s)
                                                         : rows_t<LD_W4_INT4, 128>(a, s);

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2609_05275_amd as ld
-from tests.test_abi_kv8 import INVALID, SHAPE, UNSUPPORTED, OnDevice
+from tests.test_abi_kv8 import INVALID, SHAPE, UNSUPPORTED, WORKSPACE, OnDevice
 
 P = 1 << 20
 GOOD = dict(format=ld.LD_W4_INT4, group=64, n=48, k=200)
@@ -70,6 +70,14 @@ def test_call_refused(call, kw, code):
 def test_swiglu_rows():
     assert gemm(desc(n=40), act=1) == SHAPE
     assert gemm(desc(n=47), act=1) == SHAPE
+
+
+def test_workspace():
+    w = desc(k=4000)
+    n = ld.ld_gemm_w4_ws_bytes(w, 20)
+    assert n > 0 and gemm(w, M=20, lda=4000, ws=None, Cm=2 * P) == WORKSPACE
+    assert gemm(w, M=20, lda=4000, wsb=n - 1, Cm=2 * P) == WORKSPACE and gemm(w, M=20, lda=4000, ws=P + 8, Cm=2 * P) == INVALID
+    assert ld.ld_gemm_w4_ws_bytes(w, 8) == ld.ld_gemm_w4_ws_bytes(desc(k=640), 64) == 0
 
 
 def test_norm_of_long_rows():

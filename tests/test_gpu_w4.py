@@ -184,6 +184,23 @@ def test_layer_shapes(fmt, group, M, N, K, act):
     run(fmt, group, M, N, K, act=act, norm=M <= 16)
 
 
+@FORMATS
+@pytest.mark.parametrize("M", [17, 33, 49, 64])
+@pytest.mark.parametrize("K", [640, 648, 848, 856, 1272, 1288, 2568, 4104])
+def test_rows_as_they_lie_and_laid_out(fmt, group, M, K):
+    """Both sides of where rows are laid out first, the last chunk a part of one."""
+    run(fmt, group, M, 41, K, resid=True, extra=1)
+    run(fmt, group, M, 32, K, act="swiglu")
+
+
+@pytest.mark.parametrize("fmt,group", [(w4.E2M1, 32), (w4.INT4, 64)], ids=["e2m1", "int4_64"])
+@pytest.mark.parametrize("M,N,K", [(20, 4105, 2568), (40, 4105, 1032), (40, 8209, 1032), (60, 16401, 776), (64, 4121, 264), (33, 16401, 264),
+                                   (12, 16393, 520), (12, 16393, 2568)])
+def test_columns_of_laid_out_rows(fmt, group, M, N, K):
+    """One to six groups of columns a workgroup, the last workgroup's partly behind N."""
+    run(fmt, group, M, N, K, act="relu2" if M == 60 else "none")
+
+
 def test_in_place_residual():
     for M in (1, 9, 50):
         run(w4.INT4, 64, M, 72, 512, resid=True, alpha=0.7, inplace=True)
