@@ -25,20 +25,13 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kKv4Waves = 8;  // of an attention workgroup
 constexpr int kKv4Turn = 32 * kKv4Waves;  // keys of a turn of an attention workgroup
 constexpr int kKv4Parts = 3;  // bf16 parts of a weight, 8 of its 24 bits each
-constexpr int kCus = 256;
 constexpr uint32_t kNanScale = 255;
 constexpr int kKv4MaxExp = 125;  // 6 2^125 is finite
 
 // ------------------------------------------------------------- conversions
 
-// The scale in byte b of w as the conversions take it: they look at a float's
-// exponent alone, so the neighbours' bits may stay where sign and mantissa are.
-template <int B>
-__device__ __forceinline__ float scale_byte(uint32_t w) {
-  return __builtin_bit_cast(float, B == 0 ? w << 23 : B == 1 ? w << 15 : B == 2 ? w << 7 : w >> 1);
-}
-
-// Two codes of byte B times a scale.
+// Two codes of byte B times a scale, of which the conversion looks at the exponent alone: a
+// scale's byte may be shifted there with its neighbours' bits where sign and mantissa are.
 template <int B>
 __device__ __forceinline__ bf16x2 pair_of(uint32_t w, float scale) {
   return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B);

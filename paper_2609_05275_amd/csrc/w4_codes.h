@@ -10,7 +10,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
-typedef unsigned short ushortx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 8;  // of a workgroup
@@ -52,7 +51,6 @@ __device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t w, float scale) {
 template <int FMT, int GROUP>
 struct W4Scales {
   static constexpr int kPer = 128 / GROUP;                           // of a lane's row in half a chunk
-  static constexpr int kBytes = kPer * (FMT == LD_W4_E2M1 ? 1 : 2);
 };
 
 // ------------------------------------------------------------- projections
