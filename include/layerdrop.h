@@ -612,6 +612,7 @@ int ld_w4_load(const ld_w4* w, void* dst, int32_t ld, void* stream);
  *   act 1: SwiGLU; W holds the gate rows 0..N-1, then the up rows: N = w->n / 2, a
  *          multiple of 8; C = silu(u) v (R must be NULL)
  *   act 2: squared ReLU (R must be NULL).
+ * A NaN among a sum's terms makes its element NaN, whatever the activation.
  * A: device bf16 [M, k], rows lda apart (a multiple of 8), 16-byte aligned, as g; C: device
  * bf16 [M, N], rows ldc apart.  C may be R; nothing else that is written may overlap what is
  * read.  Weights are exact, sums float32, and the activation takes the sums unrounded.  ws:

@@ -71,8 +71,8 @@ __device__ __forceinline__ void w4_finish(const W4GemmArgs& a, int m, int64_t n,
   if (a.act == kDecActSwiglu) {
     y = swiglu_fwd_f(scale * s0, scale * s1);
   } else if (a.act == kDecActRelu2) {
-    const float z = fmaxf(scale * s0, 0.f);
-    y = z * z;
+    const float z = scale * s0;
+    y = z < 0.f ? 0.f : z * z;  // (of NaN NaN; a maximum with 0 would drop it)
   } else {
     y = scale * s0;
     if (a.R) y += static_cast<float>(__builtin_bit_cast(bf16, resid));
