@@ -320,7 +320,7 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_long(W4GemmArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int K = a.w.K, M = a.M, C = (K + kW4Chunk - 1) / kW4Chunk;
   const int r = lane & 7, lk = 128 * ((lane >> 3) & 1) + 8 * (lane >> 4);
-  const int64_t tile = blockIdx.x, up = a.N / kW4Rows;
+  const int64_t tile = a.wg0 + static_cast<int>(blockIdx.x), up = a.N / kW4Rows;
   const bf16* xr[MB];
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb) xr[mb] = static_cast<const bf16*>(a.A) + static_cast<int64_t>(min(mb * 8 + r, M - 1)) * a.lda;
@@ -431,8 +431,9 @@ hipError_t gemm_few(const W4GemmArgs& a, hipStream_t s) {
     if (held && cpw <= 4) return gemm_held<FMT, GROUP, MB, NR, NORM, 4>(a, s);
   if constexpr (kMost >= 8)
     if (held && cpw <= 8) return gemm_held<FMT, GROUP, MB, NR, NORM, 8>(a, s);
-  hipLaunchKernelGGL((ld_gemm_w4_long<FMT, GROUP, MB, NR, NORM>), dim3(tiles), dim3(64 * kWaves), 0, s, a);
-  return hipGetLastError();
+  return w4_launches(a, tiles, [&](const W4GemmArgs& part, dim3 grid) {
+    hipLaunchKernelGGL((ld_gemm_w4_long<FMT, GROUP, MB, NR, NORM>), grid, dim3(64 * kWaves), 0, s, part);
+  });
 }
 
 template <int FMT, int GROUP, int MB>

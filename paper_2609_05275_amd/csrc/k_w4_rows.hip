@@ -6,10 +6,10 @@ namespace {
 
 // A block of 16 rows and 32 k as the operand that a product takes: lane 16 g + n has row n's
 // k = 8 g .. 8 g + 7.  Blocks [ceil(K / 256)][2][4][MB]; rows and k past the last are zeros.
-__global__ __launch_bounds__(256) void ld_w4_rows_k(W4GemmArgs a, int mb_count, int blocks) {
-  const int lane = threadIdx.x & 63, b = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (b >= blocks) return;
-  const int m = b % mb_count * 16 + (lane & 15), k = b / mb_count * 32 + 8 * (lane >> 4);
+// A workgroup takes four blocks of the same rows (blockIdx.y): half a chunk.
+__global__ __launch_bounds__(256) void ld_w4_rows_k(W4GemmArgs a, int mb_count) {
+  const int lane = threadIdx.x & 63, kb = blockIdx.x * 4 + (threadIdx.x >> 6), b = kb * mb_count + blockIdx.y;
+  const int m = blockIdx.y * 16 + (lane & 15), k = kb * 32 + 8 * (lane >> 4);
   bf16x8 x = load8(static_cast<const bf16*>(a.A) + static_cast<int64_t>(min(m, a.M - 1)) * a.lda + (k < a.w.K ? k : 0));
   keep_if(x, m < a.M && k < a.w.K);
   static_cast<bf16x8*>(a.ws)[static_cast<int64_t>(b) * 64 + lane] = x;
@@ -40,7 +40,7 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_rows(W4GemmArgs a) {
   const bool glu = a.act == kDecActSwiglu;
   const int tiles = (a.w.N + kW4Rows - 1) / kW4Rows, part_tiles = glu ? a.N / kW4Rows : tiles;
   const int groups = glu ? CG / 2 : CG;       // of columns of C
-  const int first = blockIdx.x * groups * 2;  // tile
+  const int first = (a.wg0 + static_cast<int>(blockIdx.x)) * groups * 2;  // tile
   floatx4 acc[CG][MB];
 #pragma unroll
   for (int i = 0; i < CG; ++i)
@@ -139,8 +139,9 @@ __global__ __launch_bounds__(64 * kWaves) void ld_gemm_w4_rows(W4GemmArgs a) {
 template <int FMT, int GROUP, int MB, int CG, bool LAID = true>
 hipError_t rows_launch(const W4GemmArgs& a, hipStream_t s) {
   const int cols = (a.act == kDecActSwiglu ? CG / 2 : CG) * 16;
-  hipLaunchKernelGGL((ld_gemm_w4_rows<FMT, GROUP, MB, CG, LAID>), dim3((a.N + cols - 1) / cols), dim3(64 * kWaves), 0, s, a);
-  return hipGetLastError();
+  return w4_launches(a, (a.N + cols - 1) / cols, [&](const W4GemmArgs& part, dim3 grid) {
+    hipLaunchKernelGGL((ld_gemm_w4_rows<FMT, GROUP, MB, CG, LAID>), grid, dim3(64 * kWaves), 0, s, part);
+  });
 }
 
 // Short rows are read where they lie, which saves a launch.  Us laid out and not, 2304 columns:
@@ -185,8 +186,8 @@ size_t w4_gemm_ws_bytes(int64_t M, int64_t K) {
 hipError_t launch_gemm_w4_rows(const W4GemmArgs& a, hipStream_t s) {
   if (a.M < 1 || a.M > kW4MaxM || a.g || (w4_rows_laid(a.M, a.w.K) && !a.ws)) return hipErrorInvalidValue;
   if (w4_rows_laid(a.M, a.w.K)) {
-    const int mb = (a.M + 15) / 16, blocks = (a.w.K + kW4Chunk - 1) / kW4Chunk * 8 * mb;
-    hipLaunchKernelGGL(ld_w4_rows_k, dim3((blocks + 3) / 4), dim3(256), 0, s, a, mb, blocks);
+    const int mb = (a.M + 15) / 16, chunks = (a.w.K + kW4Chunk - 1) / kW4Chunk;
+    hipLaunchKernelGGL(ld_w4_rows_k, dim3(2 * chunks, mb), dim3(256), 0, s, a, mb);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

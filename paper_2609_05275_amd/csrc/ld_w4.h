@@ -31,6 +31,7 @@ struct W4PackArgs {
 // kDecActSwiglu: W holds the gate rows 0 .. N - 1, then the up rows.
 struct W4GemmArgs {
   W4View w;
+  int32_t wg0;  // a launch's first workgroup, where they go in several (w4_launches)
   const void *A, *g, *R;
   void* C;
   int64_t lda, ldc, ldr;

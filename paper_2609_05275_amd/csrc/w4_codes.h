@@ -15,6 +15,21 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kWaves = 8;  // of a workgroup
 constexpr int kCus = 256;
 
+// A launch takes fewer than 2^32 threads, and 2^30 rows of weights may need more: launches of
+// 2^17 workgroups, one but for a million columns and more.  (The number in two dimensions, with a
+// test for those past the last: one row, 4096 x 11008, 6.2 -> 6.4 us.)
+constexpr int64_t kW4Wgs = 1 << 17;
+template <class F>
+hipError_t w4_launches(W4GemmArgs a, int64_t wgs, F launch) {
+  for (int64_t first = 0; first < wgs; first += kW4Wgs) {
+    a.wg0 = static_cast<int32_t>(first);
+    launch(a, dim3(static_cast<uint32_t>(wgs - first < kW4Wgs ? wgs - first : kW4Wgs)));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 // ------------------------------------------------------------- conversions
 
 // The scale in byte B of w as the conversions take it: they look at a float's
