@@ -616,8 +616,9 @@ int ld_w4_load(const ld_w4* w, void* dst, int32_t ld, void* stream);
  * A: device bf16 [M, k], rows lda apart (a multiple of 8), 16-byte aligned, as g; C: device
  * bf16 [M, N], rows ldc apart.  C may be R; nothing else that is written may overlap what is
  * read.  Weights are exact, sums float32, and the activation takes the sums unrounded.  ws:
- * device scratch of ld_gemm_w4_ws_bytes(w, M, act) bytes (0 for few or short rows, then ws
- * may be NULL; enough for fewer rows), 16-byte aligned. */
+ * device scratch of ld_gemm_w4_ws_bytes(w, M, act) bytes, 16-byte aligned, enough for fewer
+ * rows too.  It is 0 where rows are few or short (then ws may be NULL); a call with a gain
+ * needs none. */
 size_t ld_gemm_w4_ws_bytes(const ld_w4* w, int32_t M, int32_t act);
 int ld_gemm_w4(int32_t M, const void* A, int32_t lda, const void* g, float eps, const ld_w4* w, void* C, int32_t ldc,
                float alpha, const void* R, int32_t ldr, int32_t act, void* ws, size_t ws_bytes, void* stream);

@@ -1297,7 +1297,7 @@ DecLayout dec_layout(const Dims& D, int64_t n_new, size_t pc, int64_t score_keys
     for (const auto& sh : shapes) L.skp_bytes = std::max(L.skp_bytes, skinny_fused_part_bytes(M, sh[0], sh[1]));
   if (w4)
     for (int i = 0; i < 4; ++i)
-      L.skp_bytes = std::max(L.skp_bytes, w4_gemm_ws_bytes(std::min<int64_t>(M, kW4MaxM), shapes[i][1]));
+      L.skp_bytes = std::max(L.skp_bytes, w4_gemm_ws_bytes(std::min<int64_t>(M, kW4MaxM), shapes[i][0], shapes[i][1], false));
   if (L.skp_bytes) L.skp = take(L.skp_bytes);
   L.total = o;
   return L;
@@ -2713,7 +2713,7 @@ size_t ld_gemm_w4_ws_bytes(const ld_w4* w, int32_t M, int32_t act) {
   W4View v;
   if (check_w4(w, &v) || M < 1 || M > kW4MaxM || act < kDecActNone || act > kDecActRelu2) return 0;
   size_t most = 0;
-  for (int32_t m = 1; m <= M; ++m) most = std::max(most, w4_gemm_ws_bytes(m, v.K));
+  for (int32_t m = 1; m <= M; ++m) most = std::max(most, w4_gemm_ws_bytes(m, v.N, v.K, false));
   return most;
 }
 
@@ -2737,7 +2737,7 @@ int ld_gemm_w4(int32_t M, const void* A, int32_t lda, const void* g, float eps, 
     return fail(LD_E_INVALID, "C and R must be 2-byte aligned");
   if (!std::isfinite(alpha)) return fail(LD_E_INVALID, "alpha not finite");
   if (g && !(eps > 0.f)) return fail(LD_E_INVALID, "eps must be > 0");
-  const size_t need = w4_gemm_ws_bytes(M, v.K);
+  const size_t need = w4_gemm_ws_bytes(M, v.N, v.K, g != nullptr);
   if (need && (!ws || ws_bytes < need)) return fail(LD_E_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
   if (need && (reinterpret_cast<uintptr_t>(ws) & 15)) return fail(LD_E_INVALID, "ws must be 16-byte aligned");
   if (A == C) return fail(LD_E_INVALID, "C must not be A");

@@ -474,13 +474,17 @@ hipError_t launch_w4_load(const W4PackArgs& a, hipStream_t s) { return pack_or_l
 // Rows and K whose norm a projection can take in.
 bool w4_gemm_fuses_norm(int64_t M, int64_t K) { return M <= kW4FewRows && K <= 8192; }
 
+// From 9 rows on reading them costs as much as the codes where they are long, and laid
+// out in memory once (or not, if short) they are used for more columns.  Us of 16 rows, held and laid out: 4096
+// x 11008 22.2, 10.2; 2048 x 5504 9.9, 6.6; 16384 x 8192 25.2, 21.3; 22016 x 4096 18.0, 15.4;
+// 12288 x 4096 12.0, 12.3; 6144 x 2048 4.8, 6.3.  Of 8: 4096 x 11008 12.8, 10.1, 8192 x 5504 10.7,
+// 11.2, 2048 x 16384 10.0, 11.8.
+bool w4_gemm_by_rows(int64_t M, int64_t N, int64_t K, bool norm) {
+  return M > kW4FewRows || (M > 8 && !norm && (K > 4096 || N > 16384));
+}
+
 hipError_t launch_gemm_w4(const W4GemmArgs& a, hipStream_t s) {
-  // From 9 rows on reading them costs as much as the codes where they are long, and laid
-  // out in memory once (or not, if short) they are used for more columns.  Us of 16 rows, held and laid out: 4096
-  // x 11008 22.2, 10.2; 2048 x 5504 9.9, 6.6; 16384 x 8192 25.2, 21.3; 22016 x 4096 18.0, 15.4;
-  // 12288 x 4096 12.0, 12.3; 6144 x 2048 4.8, 6.3.  Of 8: 4096 x 11008 12.8, 10.1, 8192 x 5504 10.7,
-  // 11.2, 2048 x 16384 10.0, 11.8.
-  if (a.M > kW4FewRows || (a.M > 8 && !a.g && (a.w.K > 4096 || a.w.N > 16384))) return launch_gemm_w4_rows(a, s);
+  if (w4_gemm_by_rows(a.M, a.w.N, a.w.K, a.g != nullptr)) return launch_gemm_w4_rows(a, s);
   if (a.w.format == LD_W4_E2M1) return gemm_t<LD_W4_E2M1, 32>(a, s);
   return a.w.group == 32 ? gemm_t<LD_W4_INT4, 32>(a, s) : a.w.group == 64 ? gemm_t<LD_W4_INT4, 64>(a, s)
                                                         : gemm_t<LD_W4_INT4, 128>(a, s);

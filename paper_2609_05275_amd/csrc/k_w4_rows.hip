@@ -178,8 +178,8 @@ hipError_t rows_t(const W4GemmArgs& a, hipStream_t s) {
 
 }  // namespace
 
-size_t w4_gemm_ws_bytes(int64_t M, int64_t K) {
-  if (M <= 8 || !w4_rows_laid(M, K)) return 0;
+size_t w4_gemm_ws_bytes(int64_t M, int64_t N, int64_t K, bool norm) {
+  if (!w4_gemm_by_rows(M, N, K, norm) || !w4_rows_laid(M, K)) return 0;
   return static_cast<size_t>((M + 15) / 16 * 16) * ((K + kW4Chunk - 1) / kW4Chunk * kW4Chunk) * 2;
 }
 

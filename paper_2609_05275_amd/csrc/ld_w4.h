@@ -43,7 +43,10 @@ struct W4GemmArgs {
 hipError_t launch_w4_pack(const W4PackArgs& a, hipStream_t s);
 hipError_t launch_w4_load(const W4PackArgs& a, hipStream_t s);
 bool w4_gemm_fuses_norm(int64_t M, int64_t K);
-size_t w4_gemm_ws_bytes(int64_t M, int64_t K);
+// Whether M rows go to launch_gemm_w4_rows, N rows of W; and the scratch in which they are
+// laid out then, if they are.
+bool w4_gemm_by_rows(int64_t M, int64_t N, int64_t K, bool norm);
+size_t w4_gemm_ws_bytes(int64_t M, int64_t N, int64_t K, bool norm);
 hipError_t launch_gemm_w4(const W4GemmArgs& a, hipStream_t s);
 hipError_t launch_gemm_w4_rows(const W4GemmArgs& a, hipStream_t s);  // without a gain
 
