@@ -419,21 +419,23 @@ hipError_t gemm_held(const W4GemmArgs& a, hipStream_t s) {
 template <int FMT, int GROUP, int MB, int NR, bool NORM>
 hipError_t gemm_few(const W4GemmArgs& a, hipStream_t s) {
   const int cpw = (a.w.K + kW4Chunk * kWaves - 1) / (kW4Chunk * kWaves);  // chunks a wave
-  // One or two tiles a CU over long rows: no more is gained by holding rows than is lost by
-  // taking the tiles in turn.  Us of one row, held and not: 4096 x 11008 9.2, 6.1; 2048 x 5504
-  // 3.7, 3.1; 2048 x 16384 7.2, 6.3.  (22016 x 4096 14.7, 22.2; 12288 x 4096 9.6, 19.4.)
-  const int tiles = (a.N + kW4Rows - 1) / kW4Rows;
-  const bool held = cpw <= 2 || MB > 1 || tiles > 2 * kCus;
-  constexpr int kMost = 8 / (MB * (NORM || NR == 2 ? 2 : 1));
   if (cpw <= 1) return gemm_held<FMT, GROUP, MB, NR, NORM, 1>(a, s);
   if (cpw <= 2) return gemm_held<FMT, GROUP, MB, NR, NORM, 2>(a, s);
-  if constexpr (kMost >= 4)
-    if (held && cpw <= 4) return gemm_held<FMT, GROUP, MB, NR, NORM, 4>(a, s);
-  if constexpr (kMost >= 8)
-    if (held && cpw <= 8) return gemm_held<FMT, GROUP, MB, NR, NORM, 8>(a, s);
-  return w4_launches(a, tiles, [&](const W4GemmArgs& part, dim3 grid) {
-    hipLaunchKernelGGL((ld_gemm_w4_long<FMT, GROUP, MB, NR, NORM>), grid, dim3(64 * kWaves), 0, s, part);
-  });
+  if constexpr (MB == 1 || NORM) {
+    // One or two tiles a CU over long rows: no more is gained by holding rows than is lost by
+    // taking the tiles in turn.  Us of one row, held and not: 4096 x 11008 9.2, 6.1; 2048 x 5504
+    // 3.7, 3.1; 2048 x 16384 7.2, 6.3.  (22016 x 4096 14.7, 22.2; 12288 x 4096 9.6, 19.4.)
+    const int tiles = (a.N + kW4Rows - 1) / kW4Rows;
+    constexpr int kMost = MB > 1 ? 2 : NORM || NR == 2 ? 4 : 8;  // chunks a wave's registers hold
+    if constexpr (kMost >= 4)
+      if (tiles > 2 * kCus && cpw <= 4) return gemm_held<FMT, GROUP, MB, NR, NORM, 4>(a, s);
+    if constexpr (kMost >= 8)
+      if (tiles > 2 * kCus && cpw <= 8) return gemm_held<FMT, GROUP, MB, NR, NORM, 8>(a, s);
+    return w4_launches(a, tiles, [&](const W4GemmArgs& part, dim3 grid) {
+      hipLaunchKernelGGL((ld_gemm_w4_long<FMT, GROUP, MB, NR, NORM>), grid, dim3(64 * kWaves), 0, s, part);
+    });
+  }
+  return hipErrorInvalidValue;  // more than 8 rows without a gain come here with up to 4096 k (w4_gemm_by_rows)
 }
 
 template <int FMT, int GROUP, int MB>

@@ -160,7 +160,8 @@ template <int FMT, int GROUP, int MB>
 hipError_t rows_mb(const W4GemmArgs& a, hipStream_t s) {
   const int groups = (a.w.N + 15) / 16;
   if (!w4_rows_laid(a.M, a.w.K)) {
-    if (groups <= kCus && a.act != kDecActSwiglu) return rows_launch<FMT, GROUP, MB, 1, false>(a, s);
+    if constexpr (MB > 1)  // (up to 16 short rows come here with many columns alone)
+      if (groups <= kCus && a.act != kDecActSwiglu) return rows_launch<FMT, GROUP, MB, 1, false>(a, s);
     return rows_launch<FMT, GROUP, MB, 2, false>(a, s);
   }
   if (groups <= kCus && a.act != kDecActSwiglu) return rows_launch<FMT, GROUP, MB, 1>(a, s);

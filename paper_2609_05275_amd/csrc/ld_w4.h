@@ -17,7 +17,7 @@ struct W4View {
 };
 constexpr int kW4Rows = 8, kW4Chunk = 256;
 constexpr int kW4MaxM = 64;
-constexpr int kW4FewRows = 16;  // held in registers; more are laid out in scratch first
+constexpr int kW4FewRows = 16;  // the most of launch_gemm_w4's own kernels; they may take a norm
 constexpr int kW4MinExp = -100;
 
 struct W4PackArgs {
