@@ -411,7 +411,8 @@ typedef struct {
 } ld_weights_w4;
 
 /* ld_stack_eval with the keys and values of positions 0..S-1 written to 4-bit caches
- * (bf16 only), as ld_stack_eval_kv8 writes 8-bit ones. */
+ * (bf16 only), as ld_stack_eval_kv8 writes 8-bit ones.  x and ws (here and in the two
+ * decoding calls below) 16-byte aligned. */
 int ld_stack_eval_kv4(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
                       const float* r_eval, void* x, const ld_kv4* kv, void* ws, size_t ws_bytes, void* stream);
 

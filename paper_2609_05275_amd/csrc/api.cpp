@@ -1978,6 +1978,13 @@ struct StackCaches {
   const ld_kv4* kv4;
 };
 
+// The rows and scratch of the calls over 4-bit caches: their kernels read both 16 bytes a lane.
+int check_kv4_alignment(const StackCaches& c, const void* x, const void* ws) {
+  if (c.kv4 && ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(ws)) & 15))
+    return fail(LD_E_INVALID, "x and ws must be 16-byte aligned");
+  return LD_OK;
+}
+
 int stack_eval(const ld_config* cfg, int32_t n_layers, const ld_weights* w, const uint8_t* active,
                const float* r_eval, void* x, const StackCaches& c, void* ws, size_t ws_bytes, void* stream) {
   Dims D;
@@ -1985,6 +1992,7 @@ int stack_eval(const ld_config* cfg, int32_t n_layers, const ld_weights* w, cons
   if (n_layers < 1 || n_layers > 1024) return fail(LD_E_INVALID, "n_layers outside [1, 1024]");
   if (!w || !x || !ws) return fail(LD_E_INVALID, "NULL pointer");
   if ((c.kv || c.kv8 || c.kv4) && D.dtype != LD_BF16) return fail(LD_E_UNSUPPORTED, "KV caches are bf16 only");
+  if (int rc = check_kv4_alignment(c, x, ws)) return rc;
   if (c.kv && c.s_max < D.S) return fail(LD_E_SHAPE, "s_max %d < seq %lld", c.s_max, static_cast<long long>(D.S));
   for (int32_t l = 0; l < n_layers; ++l) {
     if (active && !active[l]) continue;
@@ -2091,6 +2099,7 @@ int stack_decode(const ld_config* cfg, int32_t n_layers, const ld_weights* w, co
   if (D.dtype != LD_BF16) return fail(LD_E_UNSUPPORTED, "decoding is bf16 only");
   if (n_layers < 1 || n_layers > 1024) return fail(LD_E_INVALID, "n_layers outside [1, 1024]");
   if ((!w && !w4) || !x || (!c.kv && !c.kv8 && !c.kv4) || !ws) return fail(LD_E_INVALID, "NULL pointer");
+  if (int rc = check_kv4_alignment(c, x, ws)) return rc;
   if (n_new < 1 || n_new > kDecMaxRows) return fail(LD_E_INVALID, "n_new outside [1, %d]", kDecMaxRows);
   if (pos < 0) return fail(LD_E_SHAPE, "pos %d < 0", pos);
   if (reinterpret_cast<uintptr_t>(seq_pos) & 3) return fail(LD_E_INVALID, "seq_pos must be 4-byte aligned");
