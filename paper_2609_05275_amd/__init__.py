@@ -282,6 +282,23 @@ def weights(w):
     return ld_weights(*[_ptr(w[k], k) for k in WEIGHT_KEYS])
 
 
+def _stack_weights(cfg, ws_list, active, ptr=None):
+    """The layers' weights for a call that reads those of the active ones (_u8_array), whose
+    tensors are checked as _check_layer_tensors does, or by ptr(tensor, name, dtype, numel)."""
+    dt, n = _TORCH_OF.get(cfg.dtype), _weight_numel(cfg)
+
+    def need_ptr(t, name, dtype, numel):
+        if type(t) is torch.Tensor and t.dtype is dtype and t.numel() == numel and t.is_cuda and t.is_contiguous():
+            return t.data_ptr()     # the usual case, 0.1 us sooner
+        _need(t, name, dtype, numel)
+        return _ptr(t, name)
+
+    ptr = ptr or need_ptr
+    return (ld_weights * len(ws_list))(*[ld_weights(*[ptr(w[k], k, dt, n[k]) for k in WEIGHT_KEYS])
+                                         if active is None or active[l] else weights(w)
+                                         for l, w in enumerate(ws_list)])
+
+
 def grads(g):
     return ld_grads(*[_ptr(g[k], "grad " + k) for k in WEIGHT_KEYS])
 
@@ -413,8 +430,8 @@ def ld_stack_eval(cfg, ws_list, x, ws, active=None, r_eval=None, kv=None, s_max=
     """Forward-only evaluation form over the active layers; kv: list of
     per-layer caches (None entries allowed for inactive layers)."""
     L = len(ws_list)
-    wa = (ld_weights * L)(*[weights(w) for w in ws_list])
     act, rr, kk = _u8_array(active, L), _f32_array(r_eval, L), _ptr_array(kv, L)
+    wa = _stack_weights(cfg, ws_list, act)
     _check(_lib.ld_stack_eval(C.byref(cfg), L, wa, act, rr, _ptr(x), kk, s_max, _ptr(ws),
                               ws.numel() * ws.element_size(), _stream(stream)))
 
@@ -426,8 +443,8 @@ def ld_decode_ws_bytes(cfg, n_new, s_max):
 def ld_stack_decode(cfg, ws_list, x, kv, s_max, pos, n_new, ws, active=None, r_eval=None,
                     stream=None):
     L = len(ws_list)
-    wa = (ld_weights * L)(*[weights(w) for w in ws_list])
     act, rr, kk = _u8_array(active, L), _f32_array(r_eval, L), _ptr_array(kv, L)
+    wa = _stack_weights(cfg, ws_list, act)
     _check(_lib.ld_stack_decode(C.byref(cfg), L, wa, act, rr, _ptr(x), kk, s_max, pos, n_new,
                                 _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
@@ -524,6 +541,10 @@ def _kv8_ptr(t, name, device, dtype=None, numel=None):
     return _ptr(t, name)
 
 
+def _stack_weights_on(cfg, ws_list, active, device):
+    return _stack_weights(cfg, ws_list, active, lambda t, name, dtype, numel: _kv8_ptr(t, name, device, dtype, numel))
+
+
 def _kv8_rows(kv, n_heads, n_new, qkv, device):
     return _kv8_ptr(qkv, "qkv", device, torch.bfloat16,
                     kv.n_seq * n_new * (n_heads + 2 * kv.n_kv_heads) * kv.d_head)
@@ -578,8 +599,8 @@ def ld_stack_eval_kv8(cfg, ws_list, x, ws, kv, active=None, r_eval=None, stream=
     """ld_stack_eval that writes 8-bit caches; kv: a kv8() per layer (None
     allowed for inactive layers)."""
     L = len(ws_list)
-    wa = (ld_weights * L)(*[weights(w) for w in ws_list])
     act, rr, (kk, dev) = _u8_array(active, L), _f32_array(r_eval, L), _kv8_array(kv, L)
+    wa = _stack_weights_on(cfg, ws_list, act, dev)
     px = _kv8_ptr(x, "x", dev, torch.bfloat16, cfg.batch * cfg.seq * cfg.d_model)
     _check(_lib.ld_stack_eval_kv8(C.byref(cfg), L, wa, act, rr, px, kk, _kv8_ptr(ws, "ws", dev),
                                   ws.numel() * ws.element_size(), _stream(stream, dev)))
@@ -594,8 +615,8 @@ def ld_stack_decode_kv8(cfg, ws_list, x, kv, pos, n_new, ws, seq_pos=None, activ
     """ld_stack_decode over 8-bit caches; seq_pos: int32 [batch] positions on
     the device (at most pos), where they differ or the call is captured."""
     L = len(ws_list)
-    wa = (ld_weights * L)(*[weights(w) for w in ws_list])
     act, rr, (kk, dev) = _u8_array(active, L), _f32_array(r_eval, L), _kv8_array(kv, L)
+    wa = _stack_weights_on(cfg, ws_list, act, dev)
     px = _kv8_ptr(x, "x", dev, torch.bfloat16, cfg.batch * n_new * cfg.d_model)
     _check(_lib.ld_stack_decode_kv8(C.byref(cfg), L, wa, act, rr, px, kk, pos,
                                     _kv8_ptr(seq_pos, "seq_pos", dev, torch.int32, cfg.batch), n_new,
@@ -783,9 +804,10 @@ def ld_kv4_evict(src, dst, length, keep, recent, idx, ws=None, seq_len=None, str
 
 
 def weights_w4(w):
-    """ld_weights_w4 from a dict keyed by WEIGHT_KEYS: gains as device tensors,
-    matrices as w4()s."""
-    return ld_weights_w4(_ptr(w["g_attn"], "g_attn"), _ptr(w["g_mlp"], "g_mlp"),
+    """ld_weights_w4 from a dict keyed by WEIGHT_KEYS: gains as device tensors
+    (bfloat16, of as many elements as w_qkv has k), matrices as w4()s."""
+    d, dev = w["w_qkv"].k, w["w_qkv"].device
+    return ld_weights_w4(*[_kv8_ptr(w[k], k, dev, torch.bfloat16, d) for k in ("g_attn", "g_mlp")],
                          *[w[k] for k in ("w_qkv", "w_o", "w_gate_up", "w_down")])
 
 
@@ -805,8 +827,8 @@ def ld_stack_eval_kv4(cfg, ws_list, x, ws, kv, active=None, r_eval=None, stream=
     """ld_stack_eval that writes 4-bit caches; kv: a kv4() per layer (None
     allowed for inactive layers)."""
     L = len(ws_list)
-    wa = (ld_weights * L)(*[weights(w) for w in ws_list])
     act, rr, (kk, dev) = _u8_array(active, L), _f32_array(r_eval, L), _kv4_array(kv, L)
+    wa = _stack_weights_on(cfg, ws_list, act, dev)
     px = _kv8_ptr(x, "x", dev, torch.bfloat16, cfg.batch * cfg.seq * cfg.d_model)
     pw, wsb = _ws(ws, dev)
     _check(_lib.ld_stack_eval_kv4(C.byref(cfg), L, wa, act, rr, px, kk, pw, wsb, _stream(stream, dev)))
@@ -816,8 +838,10 @@ def ld_decode_kv4_ws_bytes(cfg, n_new, s_max, sums=False):
     return _lib.ld_decode_kv4_ws_bytes(C.byref(cfg), n_new, s_max, int(sums))
 
 
-def _stack_decode_4(call, cfg, wa, L, x, kv, pos, n_new, ws, seq_pos, active, r_eval, stream):
+def _stack_decode_4(call, weights_of, cfg, ws_list, x, kv, pos, n_new, ws, seq_pos, active, r_eval, stream):
+    L = len(ws_list)
     act, rr, (kk, dev) = _u8_array(active, L), _f32_array(r_eval, L), _kv4_array(kv, L)
+    wa = weights_of(cfg, ws_list, act, dev)
     px = _kv8_ptr(x, "x", dev, torch.bfloat16, cfg.batch * n_new * cfg.d_model)
     pw, wsb = _ws(ws, dev)
     _check(call(C.byref(cfg), L, wa, act, rr, px, kk, pos, _kv8_ptr(seq_pos, "seq_pos", dev, torch.int32, cfg.batch),
@@ -827,21 +851,23 @@ def _stack_decode_4(call, cfg, wa, L, x, kv, pos, n_new, ws, seq_pos, active, r_
 def ld_stack_decode_kv4(cfg, ws_list, x, kv, pos, n_new, ws, seq_pos=None, active=None, r_eval=None,
                         stream=None):
     """ld_stack_decode over 4-bit caches; seq_pos as in ld_stack_decode_kv8."""
-    L = len(ws_list)
-    _stack_decode_4(_lib.ld_stack_decode_kv4, cfg, (ld_weights * L)(*[weights(w) for w in ws_list]), L, x, kv, pos,
-                    n_new, ws, seq_pos, active, r_eval, stream)
+    _stack_decode_4(_lib.ld_stack_decode_kv4, _stack_weights_on, cfg, ws_list, x, kv, pos, n_new, ws, seq_pos,
+                    active, r_eval, stream)
+
+
+def _stack_weights_w4(cfg, ws_list, active, device):
+    for w in ws_list:
+        for k in ("w_qkv", "w_o", "w_gate_up", "w_down"):
+            _kv8_device(w[k])
+    return (ld_weights_w4 * len(ws_list))(*[weights_w4(w) for w in ws_list])
 
 
 def ld_stack_decode_w4(cfg, ws_list, x, kv, pos, n_new, ws, seq_pos=None, active=None, r_eval=None,
                        stream=None):
     """ld_stack_decode_kv4 with the layers' matrices in 4 bits; ws_list: a dict
     for weights_w4() per layer."""
-    L = len(ws_list)
-    for w in ws_list:
-        for k in ("w_qkv", "w_o", "w_gate_up", "w_down"):
-            _kv8_device(w[k])
-    _stack_decode_4(_lib.ld_stack_decode_w4, cfg, (ld_weights_w4 * L)(*[weights_w4(w) for w in ws_list]), L, x, kv, pos,
-                    n_new, ws, seq_pos, active, r_eval, stream)
+    _stack_decode_4(_lib.ld_stack_decode_w4, _stack_weights_w4, cfg, ws_list, x, kv, pos, n_new, ws, seq_pos,
+                    active, r_eval, stream)
 
 
 def ld_rmsnorm_fwd(x, g, y, rstd, eps=1e-5, stream=None):
