@@ -297,7 +297,9 @@ struct Kv4Parts {
 // dimensions 16 g .. + 15 and 64 + 16 g .. + 15 as 8-bit floats, and in `scale` the scales of
 // dimensions 32 g .. + 31, bytes 0 and 1 of the two parts.  The first part has four of a bf16's
 // eight bits, the second the other four: all of it down to 2^-14 of the largest of 32
-// dimensions, and 2^-21 of that below.  Not finite: NaN.
+// dimensions, and to half a step of the second part, 2^-22 of that, below.  (Where the largest
+// is below 2^-114 its scale is held at 2^-121 and the second part's steps are 2^-135; a bf16 is a
+// multiple of 2^-133.)  Not finite: NaN.
 template <int DH>
 __device__ __forceinline__ void split_query(const bf16* q, int lane, i32x4 (&to)[2][2][64], uint32_t (&scale)[64]) {
   const int g = lane >> 4;
