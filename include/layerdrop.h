@@ -637,9 +637,8 @@ int ld_kv4_store(const ld_kv4* kv, int32_t n_heads, int32_t n_new, int32_t pos, 
 int ld_kv4_load(const ld_kv4* kv, int32_t pos, int32_t n, const int32_t* seq_len, void* out, void* stream);
 
 /* ld_attn_decode over a 4-bit cache; arguments as in ld_attn_decode_kv8.  Where the cache
- * has sums, every position's weights are added to them.  Scores, softmax weights and sums
- * in float32; a query is exact down to 2^-14 of the largest of 32 of its dimensions, and to
- * 2^-22 of that below.
+ * has sums, every position's weights are added to them.  Queries, keys and values are taken as
+ * they are; scores, softmax weights and sums are float32.
  *   ws: device scratch of ld_attn_decode_kv4_ws_bytes(kv, n_heads, n_new) bytes (more for a
  *   cache with sums; enough for every pos and for fewer new rows; 0 on invalid arguments),
  *   16-byte aligned. */

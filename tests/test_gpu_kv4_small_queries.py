@@ -10,9 +10,8 @@ pytestmark = pytest.mark.gpu
 @DHS
 @pytest.mark.parametrize("small", [2.0 ** -113, 2.0 ** -115, 2.0 ** -119, 2.0 ** -123])
 def test_small_queries(dh, small):
-    """The parts of a query whose scale would pass the smallest one: a bf16 is a multiple
-    of 2^-133 and the second part's steps are 2^-135 then, so nothing of it is lost, subnormal
-    numbers (half of the smallest size's below 2^-126 / 2^-123) among them."""
+    """Against keys as large: products around 1, subnormal queries (below 2^-126) among
+    them."""
     rng = np.random.default_rng(8)
     dev = Dev(1, 2, dh, 120)
     x = rows(rng, 1, 120, 2, 2, dh)
