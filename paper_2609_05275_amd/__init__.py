@@ -282,21 +282,30 @@ def weights(w):
     return ld_weights(*[_ptr(w[k], k) for k in WEIGHT_KEYS])
 
 
-def _stack_weights(cfg, ws_list, active, ptr=None):
+def _stack_weights(cfg, ws_list, active, other=None, device=None):
     """The layers' weights for a call that reads those of the active ones (_u8_array), whose
-    tensors are checked as _check_layer_tensors does, or by ptr(tensor, name, dtype, numel)."""
+    tensors are checked as _check_layer_tensors does, or by other(tensor, name, dtype,
+    numel) where they are not as expected and on `device`."""
     dt, n = _TORCH_OF.get(cfg.dtype), _weight_numel(cfg)
-
-    def need_ptr(t, name, dtype, numel):
-        if type(t) is torch.Tensor and t.dtype is dtype and t.numel() == numel and t.is_cuda and t.is_contiguous():
-            return t.data_ptr()     # the usual case, 0.1 us sooner
-        _need(t, name, dtype, numel)
-        return _ptr(t, name)
-
-    ptr = ptr or need_ptr
-    return (ld_weights * len(ws_list))(*[ld_weights(*[ptr(w[k], k, dt, n[k]) for k in WEIGHT_KEYS])
-                                         if active is None or active[l] else weights(w)
-                                         for l, w in enumerate(ws_list)])
+    sizes = [(k, n[k]) for k in WEIGHT_KEYS]
+    out = (ld_weights * len(ws_list))()
+    for l, w in enumerate(ws_list):
+        if active is not None and not active[l]:
+            out[l] = weights(w)
+            continue
+        p = []
+        for k, m in sizes:
+            t = w[k]
+            if type(t) is torch.Tensor and t.dtype is dt and t.numel() == m and t.is_contiguous() and \
+                    (t.is_cuda if other is None else t.get_device() == device):
+                p.append(t.data_ptr())     # the usual case, 0.3 us a layer sooner
+            elif other is not None:
+                p.append(other(t, k, dt, m))
+            else:
+                _need(t, k, dt, m)
+                p.append(_ptr(t, k))
+        out[l] = ld_weights(*p)
+    return out
 
 
 def grads(g):
@@ -542,7 +551,8 @@ def _kv8_ptr(t, name, device, dtype=None, numel=None):
 
 
 def _stack_weights_on(cfg, ws_list, active, device):
-    return _stack_weights(cfg, ws_list, active, lambda t, name, dtype, numel: _kv8_ptr(t, name, device, dtype, numel))
+    return _stack_weights(cfg, ws_list, active, lambda t, name, dtype, numel: _kv8_ptr(t, name, device, dtype, numel),
+                          device)
 
 
 def _kv8_rows(kv, n_heads, n_new, qkv, device):
