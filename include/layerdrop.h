@@ -373,8 +373,9 @@ int ld_stack_decode_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights
  *           [8 (r)][128 / group] bytes (e2m1) or bf16 (int4).
  *
  * ld_kv4: a key/value cache in 4 bits, a scale for each 32 dimensions of each
- * position.  n_kv_heads may divide the call's n_heads, as in ld_kv8.  Nothing a position
- * holds depends on another, so rows that are taken back (a draft's) leave nothing behind.
+ * position.  n_kv_heads may divide the call's n_heads, as in ld_kv8 (the stack's calls take
+ * caches of cfg->n_heads heads).  Nothing a position holds depends on another, so rows that are
+ * taken back (a draft's) leave nothing behind in codes and scales.
  *   d_head: 64 or 128.  1 <= s_max <= 2^30 positions.  n_seq, 2 n_kv_heads, n_heads <= 65535.
  *   codes:  device, ld_kv4_code_bytes, 16-byte aligned.  With S8 = s_max rounded up to 8,
  *           sequence b's head h has at (b n_kv_heads + h) S8 d_head bytes its keys [S8]
@@ -384,9 +385,10 @@ int ld_stack_decode_kv8(const ld_config* cfg, int32_t n_layers, const ld_weights
  *   scales: device, ld_kv4_scale_bytes, 16-byte aligned: bytes [n_seq][n_kv_heads][2]
  *           [S8][d_head / 32], keys' then values'.
  *   sums:   NULL, or device float32 [n_seq][n_kv_heads][s_max]: the attention weight each
- *           position has drawn.  A store sets its rows' to 0; every ld_attn_decode_kv4 adds
- *           to each position it sees its softmax weights, of the head's queries and the
- *           call's new rows in that order (a draft's too).
+ *           position has drawn.  A store sets its rows' to 0 (so after a prompt all are);
+ *           every ld_attn_decode_kv4 adds to each position it sees its softmax weights, of
+ *           the head's queries and the call's new rows in that order.  What a draft's or
+ *           rejected rows added to the positions before them stays.
  * The memory need not be initialised: nothing is read behind the last position. */
 typedef enum { LD_W4_E2M1 = 0, LD_W4_INT4 = 1 } ld_w4_format;
 
@@ -661,7 +663,9 @@ int ld_attn_decode_kv4(const ld_kv4* kv, int32_t n_heads, int32_t alibi, int32_t
  *   aligned.
  * A position's number in `to` is its place there, and decoding goes on at place
  * min(n, keep).  Attention without position encoding is over the rows that stayed;
- * with the ALiBi bias distances are those of the places, smaller than they were. */
+ * with the ALiBi bias distances are those of the places, smaller than they were.
+ * Sums come from the decoding calls alone.  Right after a prompt they are all 0 and equal, so
+ * that of the positions before the last `recent` the first ones would stay. */
 size_t ld_kv4_evict_ws_bytes(const ld_kv4* from, int32_t len, int32_t keep);
 int ld_kv4_evict(const ld_kv4* from, const ld_kv4* to, int32_t len, const int32_t* seq_len, int32_t keep,
                  int32_t recent, int32_t* idx, void* ws, size_t ws_bytes, void* stream);

@@ -309,12 +309,15 @@ struct Kv4Parts {
 // together over positions by byte permutes.  A probability goes in as three bf16 parts,
 // which are all of its 24 bits (two: 3% less time, 2^-17 of a weight lost).
 //
-// What bounds it: about 260 vector and 32 matrix instructions a turn of a wave.  So the
-// registers are kept to four waves of a SIMD (more loads in flight with two were slower),
-// the maximum is renewed only where it has to be, and NaN is looked for only in turns that
-// masks cut.  2 sequences of 131072 keys, 32 heads over 8 of 128 dimensions: 58 us, 4.9
-// TB/s of the cache (scaled score products 57; the sums rescaled each turn 75).  16 uneven
-// sequences of 32 heads, 68000 keys in all: 42 us (scaled 40.6).
+// What bounds it: the chain of a turn, about 260 vector and 32 matrix instructions that wait
+// for each other and for memory, which the four waves of a SIMD hide in part: over the long
+// case below vector units are 0.52 and matrix units 0.24 busy, a fifth fewer vector
+// instructions (scaled score products) took 2% less time, and caches that the last-level cache
+// holds 10% less.  So the registers are kept to four waves of a SIMD (more loads in flight with
+// two were slower), the maximum is renewed only where it has to be, and NaN is looked for only in
+// turns that masks cut.  2 sequences of 131072 keys, 32 heads over 8 of 128 dimensions: 58 us, 4.9
+// TB/s of the cache (the sums rescaled each turn 75).  16 uneven sequences of 32 heads, 68000
+// keys in all: 42 us.
 template <int DH, int NQ>
 __global__ __launch_bounds__(64 * kKv4Waves, 4) void ld_attn_decode_kv4_k(Kv4AttnArgs a) {
   constexpr int JN = DH / 32, MT = DH / 16, NW = kKv4Waves, TT = 2, LK = 4 * TT, WK = 16 * TT;
@@ -1202,7 +1205,7 @@ hipError_t combine_t(const Kv4AttnArgs& a, hipStream_t s) {
 // There a sequence is cut into as many chunks as the most allows, so that long ones leave no
 // tail.  Us for two, three, four and six rounds, up to 8192 keys of 16 sequences of 32 heads 41,
 // 42, 43, 44; 32768 of 8 of 8 42, 41, 47, 49; 4096 of 64 of 8 39, 38, 38, 43; 100000 of 16 of 8 207, 188,
-// 180, 177; 2056 of 32 of 16 22, 23, 25, 26.
+// 180, 177; 2056 of 32 of 16 22, 23, 25, 26.  (With scaled score products, 2 to 3% less.)
 constexpr int64_t kKv4AtOnce = 512, kKv4Wgs = 3 * kKv4AtOnce, kKv4Uneven = 512;
 
 }  // namespace

@@ -14,7 +14,8 @@ namespace {
 
 // A wave takes a block of 8 rows and 256 k; lanes and dwords as the codes lie, so
 // that a group's values are in lanes 16 apart and in neighbouring dwords.  Done once for
-// weights that are kept; bound by the bf16 rows.
+// weights that are kept.  22016 x 4096, 225 MB: e2m1 49 us, 4.6 TB/s; int4 62 to 66, a division
+// an element; read back 55 to 59, rows written in pieces of 64 bytes.
 template <int FMT, int GROUP>
 __global__ __launch_bounds__(256) void ld_w4_pack_k(W4PackArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

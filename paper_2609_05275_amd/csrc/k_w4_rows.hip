@@ -22,12 +22,13 @@ __global__ __launch_bounds__(256) void ld_w4_rows_k(W4GemmArgs a, int mb_count) 
 // half of a chunk, whole lines of 128 bytes.  A half's registers are loaded with the next
 // chunk's as soon as it is used.
 //
-// What bounds it: with few rows the codes (16 rows, 8192 x 16384: 16.5-17.7 us, 4 TB/s);
-// with many the vector instructions that make operands of the codes and put the integers'
-// scales on the sums, 4.6 to a matrix instruction, two waves a SIMD.  48 rows of gate and up,
-// 11008 x 4096 int4 in groups of 64: 22.3 us, 3 of them the laying out (101 with the rows in
-// LDS, 23.2 with halves exchanged between lanes).  Rows read as they lie, 64 bytes a row and
-// step, took 25.7 us for 17.4 (33 rows, 4096 x 11008 e2m1): rows far apart meet in
+// What bounds it: with few rows the codes (16 rows, 8192 x 16384: 16.5-17.7 us, 4 TB/s).  With
+// more no unit is full: two waves a SIMD wait for codes, for rows and for each other, and over
+// K of 4096 a wave has two chunks between the first loads and the exchange of 72 KB of
+// sums.  48 rows of gate and up, 11008 x 4096 int4 in groups of 64: 21 us, 3 of them the laying
+// out, vector units 0.24 and matrix units 0.13 busy (101 with the rows in LDS, 23.2 with halves
+// exchanged between lanes); 64 rows, 16384 x 16384: 54 us, 0.34 and 0.24.  Rows read as they lie, 64
+// bytes a row and step, took 25.7 us for 17.4 (33 rows, 4096 x 11008 e2m1): rows far apart meet in
 // few of the L2's channels.
 // LAID: the rows are ld_w4_rows_k's, else A's.
 template <int FMT, int GROUP, int MB, int CG, bool LAID>
