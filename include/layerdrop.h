@@ -618,7 +618,9 @@ int ld_w4_load(const ld_w4* w, void* dst, int32_t ld, void* stream);
  * A NaN among a sum's terms makes its element NaN, whatever the activation.
  * A: device bf16 [M, k], rows lda apart (a multiple of 8), 16-byte aligned, as g; C: device
  * bf16 [M, N], rows ldc apart.  C may be R; nothing else that is written may overlap what is
- * read.  Weights are exact, sums float32, and the activation takes the sums unrounded.  ws:
+ * read.  Weights are exact, sums float32, and the activation takes the sums unrounded.
+ * (LD_W4_INT4: a group's products are summed before their scale, which overflows from inputs of
+ * 2^118 on.)  ws:
  * device scratch of ld_gemm_w4_ws_bytes(w, M, act) bytes, 16-byte aligned, enough for fewer
  * rows too.  It is 0 where rows are few or short (then ws may be NULL); a call with a gain
  * needs none. */
